@@ -294,6 +294,73 @@ int embed_backward(const void* dx0, const int64_t* ids, int64_t T, int64_t V, in
                    void* dtable, void* workspace, void* stream);
 
 /* ------------------------------------------------------------------------------------------
+ * Token mixing by linear attention, and the norm of queries and keys in front of it (or of the softmax attention above).
+ * Not part of the layer the paper benchmarks.  Two arguments are shared, device arrays of batch int64 each, NULL for none:
+ *   lengths   tokens of each batch row (values below 0 count as 0, above seq as seq; NULL: seq for all).  The rest of a row is
+ *             padding: nothing there is read for any result, whatever it holds, and outputs and gradients there are written as 0.
+ *   start     position of each row's first token (NULL: 0).  A row that is generated token by token has seq = 1 and start = the
+ *             tokens before it.
+ * batch and seq are any positive numbers; head_dim 32, 64 or 128; tensors may exceed 4 GiB.
+ * ------------------------------------------------------------------------------------------ */
+
+/* RMS norm of every query and key head, then the rotary embedding:
+ *   y = RoPE(x * rstd * gamma; position start[b] + t),  rstd = (mean over the head of x^2 + eps)^(-1/2)
+ * with gamma_q [head_dim] for the heads of q, gamma_k for those of k; angle and pairings as in dlayer_cfg, angles evaluated in
+ * fp64.  q, q_out [B*S, Hq, dh], k, k_out [B*S, Hkv, dh], gains bf16; rstd_q [B*S, Hq], rstd_k [B*S, Hkv] f32, written for the
+ * backward, or both NULL.  q_out may alias q, k_out k.  Hq need not be a multiple of Hkv.                    */
+int qk_norm_rope_forward(const void* q, const void* k, const void* gamma_q, const void* gamma_k, const int64_t* start,
+                         const int64_t* lengths, int64_t batch, int64_t seq, int64_t n_q_heads, int64_t n_kv_heads,
+                         int64_t head_dim, float eps, float rope_base, int32_t rope_layout, void* q_out, void* k_out,
+                         float* rstd_q, float* rstd_k, void* stream);
+
+/* Gradient of qk_norm_rope_forward given dq_out, dk_out, its inputs q, k (unchanged since) and the saved rstd: with dz = dq_out or dk_out
+ * rotated back and xhat = x * rstd,
+ *   dgamma = sum over tokens and heads of dz * xhat;  dx = rstd * (dz * gamma - xhat * mean(dz * gamma * xhat))
+ * dq may alias dq_out, dk dk_out.  dgamma_q, dgamma_k [head_dim] bf16; accumulate_dgamma as in dlayer_backward.
+ * workspace: qk_norm_rope_backward_workspace_bytes(...), at most 8 * head_dim KiB.                              */
+size_t qk_norm_rope_backward_workspace_bytes(int64_t batch, int64_t seq, int64_t n_q_heads, int64_t n_kv_heads,
+                                             int64_t head_dim);
+int qk_norm_rope_backward(const void* q, const void* k, const void* gamma_q, const void* gamma_k, const float* rstd_q,
+                          const float* rstd_k, const void* dq_out, const void* dk_out, const int64_t* start,
+                          const int64_t* lengths, int64_t batch, int64_t seq, int64_t n_q_heads, int64_t n_kv_heads,
+                          int64_t head_dim, float rope_base, int32_t rope_layout, void* dq, void* dk, void* dgamma_q,
+                          void* dgamma_k, int accumulate_dgamma, void* workspace, void* stream);
+
+/* Linear attention with a decay for each KV head.  For batch row b and KV head j, with the state S [dh, dh] (rows along k,
+ * columns along v) and lambda = exp(log_decay[j]):
+ *   S_t = lambda S_(t-1) + k_t v_t^T,  S_(-1) = state_in;   o_t^h = scale S_t^T q_t^h   for the query heads h of group j
+ * that is o_t^h = scale (sum over s <= t of lambda^(t-s) (q_t^h . k_s) v_s + lambda^(t+1) state_in^T q_t^h).
+ * q, o [B*S, Hq, dh], k, v [B*S, Hkv, dh] bf16; log_decay [Hkv] f32 on the device, not above 0 (0: nothing is forgotten,
+ * minus infinity: nothing is remembered), a constant of the model: it gets no gradient.  State in and out [B, Hkv, dh, dh] f32:
+ * state_in NULL for zeros, state_out (the state after a row's last token) NULL if not wanted; state_out may alias state_in.
+ * Sequences are worked on in chunks on the matrix units, the states between them are fp32.
+ * workspace: linear_attention_workspace_bytes(...).                                                          */
+size_t linear_attention_workspace_bytes(int64_t batch, int64_t seq, int64_t n_q_heads, int64_t n_kv_heads,
+                                        int64_t head_dim);
+int linear_attention_forward(const void* q, const void* k, const void* v, const float* log_decay, const int64_t* lengths,
+                             const float* state_in, int64_t batch, int64_t seq, int64_t n_q_heads, int64_t n_kv_heads,
+                             int64_t head_dim, float scale, void* o, float* state_out, void* workspace, void* stream);
+
+/* Gradient of linear_attention_forward given d_o [B*S, Hq, dh] bf16 and d_state_out [B, Hkv, dh, dh] f32 (NULL for zeros):
+ * with R_t = lambda R_(t+1) + scale sum_h q_t^h d_o_t^hT (sum over the query heads h of group j; the last token adds d_state_out),
+ *   dq_t^h = scale S_t d_o_t^h,  dk_t = R_t v_t,  dv_t = R_t^T k_t,  d_state_in = lambda R_0
+ * q, k, v, log_decay, lengths and state_in are those of the forward; nothing is saved between the two, the states are formed again.
+ * d_state_in may be NULL, and may alias d_state_out.  The outputs must not overlap the bf16 inputs.
+ * workspace: linear_attention_backward_workspace_bytes(...).                                                 */
+size_t linear_attention_backward_workspace_bytes(int64_t batch, int64_t seq, int64_t n_q_heads, int64_t n_kv_heads,
+                                                 int64_t head_dim);
+int linear_attention_backward(const void* q, const void* k, const void* v, const float* log_decay, const int64_t* lengths,
+                              const float* state_in, const void* d_o, const float* d_state_out, int64_t batch,
+                              int64_t seq, int64_t n_q_heads, int64_t n_kv_heads, int64_t head_dim, float scale,
+                              void* dq, void* dk, void* dv, float* d_state_in, void* workspace, void* stream);
+
+/* linear_attention_forward for one more token of every row (seq 1), the state updated in place: q, o [B, Hq, dh], k, v [B, Hkv, dh],
+ * state [B, Hkv, dh, dh] f32.  A row of length 0 takes no token: its o is 0 and its state stays as it is.    */
+int linear_attention_step(const void* q, const void* k, const void* v, const float* log_decay, const int64_t* lengths,
+                          float* state, int64_t batch, int64_t n_q_heads, int64_t n_kv_heads, int64_t head_dim,
+                          float scale, void* o, void* stream);
+
+/* ------------------------------------------------------------------------------------------
  * Optimizer step.  The paper's Training Pipeline paragraph speaks of training steps and names no
  * optimizer; the reading taken is the usual one for this model family: clipping of the gradients by
  * their global norm, then AdamW (Adam with decoupled weight decay).  Parameters and gradients are

@@ -17,6 +17,9 @@ EXPORTED_SYMBOLS = (
     "linear_forward", "qkv_rope_workspace_bytes", "qkv_rope_forward", "linear_swiglu_forward", "linear_swiglu_backward_workspace_bytes",
     "linear_swiglu_backward", "linear_backward_workspace_bytes", "linear_backward", "linear_wgrad_group", "rope_apply",
     "attention_forward", "attention_backward_workspace_bytes", "attention_backward",
+    "qk_norm_rope_forward", "qk_norm_rope_backward_workspace_bytes", "qk_norm_rope_backward",
+    "linear_attention_workspace_bytes", "linear_attention_forward", "linear_attention_backward_workspace_bytes", "linear_attention_backward",
+    "linear_attention_step",
     "swiglu_forward", "swiglu_backward", "embed_forward", "embed_backward_workspace_bytes", "embed_backward",
     "grad_sq_norm_workspace_bytes", "grad_sq_norm", "adamw_step", "issue_rate_probe", "gemm_route", "attention_backward_pieces",
 )
@@ -88,6 +91,14 @@ def _load():
         "attention_forward": (C.c_int, [vp, vp, vp, i64, i64, i64, i64, i64, vp, vp, vp]),
         "attention_backward_workspace_bytes": (sz, [i64, i64, i64, i64, i64]),
         "attention_backward": (C.c_int, [vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, i64, vp, vp, vp, vp, vp]),
+        "qk_norm_rope_forward": (C.c_int, [vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, i64, f32, f32, i32, vp, vp, vp, vp, vp]),
+        "qk_norm_rope_backward_workspace_bytes": (sz, [i64, i64, i64, i64, i64]),
+        "qk_norm_rope_backward": (C.c_int, [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, i64, f32, i32, vp, vp, vp, vp, C.c_int, vp, vp]),
+        "linear_attention_workspace_bytes": (sz, [i64, i64, i64, i64, i64]),
+        "linear_attention_forward": (C.c_int, [vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, i64, f32, vp, vp, vp, vp]),
+        "linear_attention_backward_workspace_bytes": (sz, [i64, i64, i64, i64, i64]),
+        "linear_attention_backward": (C.c_int, [vp, vp, vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, i64, f32, vp, vp, vp, vp, vp, vp]),
+        "linear_attention_step": (C.c_int, [vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, f32, vp, vp]),
         "swiglu_forward": (C.c_int, [vp, vp, i64, vp, vp]),
         "swiglu_backward": (C.c_int, [vp, vp, vp, i64, vp, vp, vp]),
         "embed_forward": (C.c_int, [vp, vp, i64, i64, i64, vp, vp]),
@@ -280,6 +291,51 @@ def attention_backward(q, k, v, o, d_o, lse, batch, seq, n_q_heads, n_kv_heads, 
     _check(lib.attention_backward(_p(q), _p(k), _p(v), _p(o), _p(d_o), _p(lse), batch, seq, n_q_heads,
                                   n_kv_heads, head_dim, _p(dq), _p(dk), _p(dv), _p(workspace),
                                   _stream(stream)), "attention_backward")
+
+
+def qk_norm_rope_forward(q, k, gamma_q, gamma_k, start, lengths, batch, seq, n_q_heads, n_kv_heads, head_dim, eps, rope_base,
+                         rope_layout, q_out, k_out, rstd_q, rstd_k, stream=None):
+    _check(lib.qk_norm_rope_forward(_p(q), _p(k), _p(gamma_q), _p(gamma_k), _p(start), _p(lengths), batch, seq, n_q_heads, n_kv_heads,
+                                    head_dim, eps, rope_base, rope_layout, _p(q_out), _p(k_out), _p(rstd_q), _p(rstd_k),
+                                    _stream(stream)), "qk_norm_rope_forward")
+
+
+def qk_norm_rope_backward_workspace_bytes(batch, seq, n_q_heads, n_kv_heads, head_dim) -> int:
+    return lib.qk_norm_rope_backward_workspace_bytes(batch, seq, n_q_heads, n_kv_heads, head_dim)
+
+
+def qk_norm_rope_backward(q, k, gamma_q, gamma_k, rstd_q, rstd_k, dq_out, dk_out, start, lengths, batch, seq, n_q_heads, n_kv_heads,
+                          head_dim, rope_base, rope_layout, dq, dk, dgamma_q, dgamma_k, accumulate_dgamma, workspace, stream=None):
+    _check(lib.qk_norm_rope_backward(_p(q), _p(k), _p(gamma_q), _p(gamma_k), _p(rstd_q), _p(rstd_k), _p(dq_out), _p(dk_out), _p(start),
+                                     _p(lengths), batch, seq, n_q_heads, n_kv_heads, head_dim, rope_base, rope_layout, _p(dq), _p(dk),
+                                     _p(dgamma_q), _p(dgamma_k), int(accumulate_dgamma), _p(workspace), _stream(stream)),
+           "qk_norm_rope_backward")
+
+
+def linear_attention_workspace_bytes(batch, seq, n_q_heads, n_kv_heads, head_dim) -> int:
+    return lib.linear_attention_workspace_bytes(batch, seq, n_q_heads, n_kv_heads, head_dim)
+
+
+def linear_attention_forward(q, k, v, log_decay, lengths, state_in, batch, seq, n_q_heads, n_kv_heads, head_dim, scale, o, state_out,
+                             workspace, stream=None):
+    _check(lib.linear_attention_forward(_p(q), _p(k), _p(v), _p(log_decay), _p(lengths), _p(state_in), batch, seq, n_q_heads, n_kv_heads,
+                                        head_dim, scale, _p(o), _p(state_out), _p(workspace), _stream(stream)), "linear_attention_forward")
+
+
+def linear_attention_backward_workspace_bytes(batch, seq, n_q_heads, n_kv_heads, head_dim) -> int:
+    return lib.linear_attention_backward_workspace_bytes(batch, seq, n_q_heads, n_kv_heads, head_dim)
+
+
+def linear_attention_backward(q, k, v, log_decay, lengths, state_in, d_o, d_state_out, batch, seq, n_q_heads, n_kv_heads, head_dim,
+                              scale, dq, dk, dv, d_state_in, workspace, stream=None):
+    _check(lib.linear_attention_backward(_p(q), _p(k), _p(v), _p(log_decay), _p(lengths), _p(state_in), _p(d_o), _p(d_state_out), batch,
+                                         seq, n_q_heads, n_kv_heads, head_dim, scale, _p(dq), _p(dk), _p(dv), _p(d_state_in),
+                                         _p(workspace), _stream(stream)), "linear_attention_backward")
+
+
+def linear_attention_step(q, k, v, log_decay, lengths, state, batch, n_q_heads, n_kv_heads, head_dim, scale, o, stream=None):
+    _check(lib.linear_attention_step(_p(q), _p(k), _p(v), _p(log_decay), _p(lengths), _p(state), batch, n_q_heads, n_kv_heads, head_dim,
+                                     scale, _p(o), _stream(stream)), "linear_attention_step")
 
 
 def swiglu_forward(g, u, n, a, stream=None):

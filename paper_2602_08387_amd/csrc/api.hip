@@ -610,6 +610,104 @@ int attention_backward(const void* q, const void* k, const void* v, const void* 
                               workspace, (hipStream_t)stream);
 }
 
+static int qk_norm_shape_ok(const char* who, int64_t batch, int64_t seq, int64_t Hq, int64_t Hkv, int64_t dh) {
+  REQUIRE(batch > 0 && seq > 0 && Hq > 0 && Hkv > 0, "%s: non-positive dimension", who);
+  REQUIRE(dh == 32 || dh == 64 || dh == 128, "%s: head_dim must be 32, 64 or 128", who);
+  REQUIRE(batch < ((int64_t)1 << 31) && seq < ((int64_t)1 << 31) && Hq < 65536 && Hkv < 65536 && batch * seq < ((int64_t)1 << 40),
+          "%s: batch, seq or head count too large", who);
+  return 0;
+}
+
+int qk_norm_rope_forward(const void* q, const void* k, const void* gamma_q, const void* gamma_k, const int64_t* start,
+                         const int64_t* lengths, int64_t batch, int64_t seq, int64_t n_q_heads, int64_t n_kv_heads, int64_t head_dim,
+                         float eps, float rope_base, int32_t rope_layout, void* q_out, void* k_out, float* rstd_q, float* rstd_k,
+                         void* stream) {
+  TRY(qk_norm_shape_ok("qk_norm_rope_forward", batch, seq, n_q_heads, n_kv_heads, head_dim));
+  REQUIRE(eps >= 0.f && rope_base > 0.f, "qk_norm_rope_forward: eps must be >= 0 and rope_base > 0");
+  REQUIRE(rope_layout == 0 || rope_layout == 1, "qk_norm_rope_forward: rope_layout must be 0 or 1");
+  REQUIRE_PTR(q); REQUIRE_PTR(k); REQUIRE_PTR(gamma_q); REQUIRE_PTR(gamma_k); REQUIRE_PTR(q_out); REQUIRE_PTR(k_out);
+  REQUIRE((rstd_q == nullptr) == (rstd_k == nullptr), "qk_norm_rope_forward: rstd_q and rstd_k go together");
+  TRY(check_device());
+  return launch_qk_norm_rope_fwd(QkNormCall{q, k, gamma_q, gamma_k, rstd_q, rstd_k, start, lengths, batch, seq, n_q_heads, n_kv_heads,
+                                            head_dim, rope_base, rope_layout}, eps, q_out, k_out, (hipStream_t)stream);
+}
+
+size_t qk_norm_rope_backward_workspace_bytes(int64_t batch, int64_t seq, int64_t n_q_heads, int64_t n_kv_heads, int64_t head_dim) {
+  if (qk_norm_shape_ok("qk_norm_rope_backward_workspace_bytes", batch, seq, n_q_heads, n_kv_heads, head_dim)) return 0;
+  return qk_norm_rope_bwd_workspace(batch * seq, n_q_heads, n_kv_heads, head_dim);
+}
+
+int qk_norm_rope_backward(const void* q, const void* k, const void* gamma_q, const void* gamma_k, const float* rstd_q,
+                          const float* rstd_k, const void* dq_out, const void* dk_out, const int64_t* start, const int64_t* lengths,
+                          int64_t batch, int64_t seq, int64_t n_q_heads, int64_t n_kv_heads, int64_t head_dim, float rope_base,
+                          int32_t rope_layout, void* dq, void* dk, void* dgamma_q, void* dgamma_k, int accumulate_dgamma,
+                          void* workspace, void* stream) {
+  TRY(qk_norm_shape_ok("qk_norm_rope_backward", batch, seq, n_q_heads, n_kv_heads, head_dim));
+  REQUIRE(rope_base > 0.f, "qk_norm_rope_backward: rope_base must be > 0");
+  REQUIRE(rope_layout == 0 || rope_layout == 1, "qk_norm_rope_backward: rope_layout must be 0 or 1");
+  REQUIRE_PTR(q); REQUIRE_PTR(k); REQUIRE_PTR(gamma_q); REQUIRE_PTR(gamma_k); REQUIRE_PTR(dq_out); REQUIRE_PTR(dk_out);
+  REQUIRE(rstd_q != nullptr && rstd_k != nullptr, "qk_norm_rope_backward: rstd_q or rstd_k is null");
+  REQUIRE_PTR(dq); REQUIRE_PTR(dk); REQUIRE_PTR(dgamma_q); REQUIRE_PTR(dgamma_k); REQUIRE_PTR(workspace);
+  TRY(check_device());
+  return launch_qk_norm_rope_bwd(QkNormCall{q, k, gamma_q, gamma_k, const_cast<float*>(rstd_q), const_cast<float*>(rstd_k), start, lengths,
+                                            batch, seq, n_q_heads, n_kv_heads, head_dim, rope_base, rope_layout},
+                                 dq_out, dk_out, dq, dk, dgamma_q, dgamma_k, accumulate_dgamma ? 1 : 0, workspace, (hipStream_t)stream);
+}
+
+static int linear_shape_ok(const char* who, int64_t batch, int64_t seq, int64_t Hq, int64_t Hkv, int64_t dh) {
+  REQUIRE(batch > 0 && seq > 0 && Hq > 0 && Hkv > 0, "%s: non-positive dimension", who);
+  REQUIRE(dh == 32 || dh == 64 || dh == 128, "%s: head_dim must be 32, 64 or 128", who);
+  REQUIRE(Hq % Hkv == 0, "%s: n_q_heads must be a multiple of n_kv_heads", who);
+  REQUIRE(batch < ((int64_t)1 << 24) && seq < ((int64_t)1 << 30) && Hq < 65536 && batch * Hkv < ((int64_t)1 << 24),
+          "%s: batch, seq or head count too large", who);
+  return 0;
+}
+
+size_t linear_attention_workspace_bytes(int64_t batch, int64_t seq, int64_t n_q_heads, int64_t n_kv_heads, int64_t head_dim) {
+  if (linear_shape_ok("linear_attention_workspace_bytes", batch, seq, n_q_heads, n_kv_heads, head_dim)) return 0;
+  return linear_attention_fwd_workspace(batch, seq, n_q_heads, n_kv_heads, head_dim);
+}
+
+int linear_attention_forward(const void* q, const void* k, const void* v, const float* log_decay, const int64_t* lengths,
+                             const float* state_in, int64_t batch, int64_t seq, int64_t n_q_heads, int64_t n_kv_heads, int64_t head_dim,
+                             float scale, void* o, float* state_out, void* workspace, void* stream) {
+  TRY(linear_shape_ok("linear_attention_forward", batch, seq, n_q_heads, n_kv_heads, head_dim));
+  REQUIRE_PTR(q); REQUIRE_PTR(k); REQUIRE_PTR(v); REQUIRE_PTR(o); REQUIRE_PTR(workspace);
+  REQUIRE(log_decay != nullptr, "linear_attention_forward: log_decay is null");
+  REQUIRE(aligned16(state_in) && aligned16(state_out), "linear_attention_forward: a state is not 16-byte aligned");
+  TRY(check_device());
+  return launch_linear_attention_fwd(LinearCall{q, k, v, log_decay, lengths, batch, seq, n_q_heads, n_kv_heads, head_dim, scale}, state_in,
+                                     o, state_out, workspace, (hipStream_t)stream);
+}
+
+size_t linear_attention_backward_workspace_bytes(int64_t batch, int64_t seq, int64_t n_q_heads, int64_t n_kv_heads, int64_t head_dim) {
+  if (linear_shape_ok("linear_attention_backward_workspace_bytes", batch, seq, n_q_heads, n_kv_heads, head_dim)) return 0;
+  return linear_attention_bwd_workspace(batch, seq, n_q_heads, n_kv_heads, head_dim);
+}
+
+int linear_attention_backward(const void* q, const void* k, const void* v, const float* log_decay, const int64_t* lengths,
+                              const float* state_in, const void* d_o, const float* d_state_out, int64_t batch, int64_t seq,
+                              int64_t n_q_heads, int64_t n_kv_heads, int64_t head_dim, float scale, void* dq, void* dk, void* dv,
+                              float* d_state_in, void* workspace, void* stream) {
+  TRY(linear_shape_ok("linear_attention_backward", batch, seq, n_q_heads, n_kv_heads, head_dim));
+  REQUIRE_PTR(q); REQUIRE_PTR(k); REQUIRE_PTR(v); REQUIRE_PTR(d_o); REQUIRE_PTR(dq); REQUIRE_PTR(dk); REQUIRE_PTR(dv); REQUIRE_PTR(workspace);
+  REQUIRE(log_decay != nullptr, "linear_attention_backward: log_decay is null");
+  REQUIRE(aligned16(state_in) && aligned16(d_state_out) && aligned16(d_state_in), "linear_attention_backward: a state is not 16-byte aligned");
+  TRY(check_device());
+  return launch_linear_attention_bwd(LinearCall{q, k, v, log_decay, lengths, batch, seq, n_q_heads, n_kv_heads, head_dim, scale}, state_in,
+                                     d_o, d_state_out, dq, dk, dv, d_state_in, workspace, (hipStream_t)stream);
+}
+
+int linear_attention_step(const void* q, const void* k, const void* v, const float* log_decay, const int64_t* lengths, float* state,
+                          int64_t batch, int64_t n_q_heads, int64_t n_kv_heads, int64_t head_dim, float scale, void* o, void* stream) {
+  TRY(linear_shape_ok("linear_attention_step", batch, 1, n_q_heads, n_kv_heads, head_dim));
+  REQUIRE_PTR(q); REQUIRE_PTR(k); REQUIRE_PTR(v); REQUIRE_PTR(state); REQUIRE_PTR(o);
+  REQUIRE(log_decay != nullptr, "linear_attention_step: log_decay is null");
+  TRY(check_device());
+  return launch_linear_attention_step(LinearCall{q, k, v, log_decay, lengths, batch, 1, n_q_heads, n_kv_heads, head_dim, scale}, state, o,
+                                      (hipStream_t)stream);
+}
+
 static int opt_args_ok(const char* who, int32_t n, const int64_t* numel) {
   REQUIRE(n >= 1 && n <= kOptMaxTensors, "%s: 1..%d tensors per call, got %d", who, kOptMaxTensors, (int)n);
   REQUIRE(numel != nullptr, "%s: numel is null", who);

@@ -131,6 +131,37 @@ int launch_attention_bwd_rope(const void* q, const void* k, const void* v, const
                               void* dq, void* dk, void* dv, void* workspace, const float* rope_cos,
                               const float* rope_sin, int rope_layout, bool stats_done, hipStream_t st);
 
+// ---- qk_norm.hip
+// start, lengths (device, [batch]) may be null; rstd_q, rstd_k: [tokens][heads], both null in a forward that keeps no statistics
+struct QkNormCall {
+  const void *q, *k, *gamma_q, *gamma_k;
+  float *rstd_q, *rstd_k;
+  const int64_t *start, *lengths;
+  int64_t batch, seq, Hq, Hkv, dh;
+  float base;
+  int layout;
+};
+int launch_qk_norm_rope_fwd(const QkNormCall& c, float eps, void* q_out, void* k_out, hipStream_t st);
+size_t qk_norm_rope_bwd_workspace(int64_t tokens, int64_t Hq, int64_t Hkv, int64_t dh);
+int launch_qk_norm_rope_bwd(const QkNormCall& c, const void* dq_out, const void* dk_out, void* dq, void* dk, void* dgamma_q,
+                            void* dgamma_k, int accumulate, void* workspace, hipStream_t st);
+
+// ---- linear_attention.hip
+// q [B*S, Hq, dh], k, v [B*S, Hkv, dh]; log_decay [Hkv], lengths [B] (may be null); states [B, Hkv, dh, dh] fp32 (may be null)
+struct LinearCall {
+  const void *q, *k, *v;
+  const float* log_decay;
+  const int64_t* lengths;
+  int64_t B, S, Hq, Hkv, dh;
+  float scale;
+};
+size_t linear_attention_fwd_workspace(int64_t B, int64_t S, int64_t Hq, int64_t Hkv, int64_t dh);
+int launch_linear_attention_fwd(const LinearCall& c, const float* s_in, void* o, float* s_out, void* workspace, hipStream_t st);
+size_t linear_attention_bwd_workspace(int64_t B, int64_t S, int64_t Hq, int64_t Hkv, int64_t dh);
+int launch_linear_attention_bwd(const LinearCall& c, const float* s_in, const void* d_o, const float* ds_out, void* dq, void* dk, void* dv,
+                                float* ds_in, void* workspace, hipStream_t st);
+int launch_linear_attention_step(const LinearCall& c, float* state, void* o, hipStream_t st);
+
 // ---- ce.hip
 size_t ce_workspace(int64_t T, int64_t V);
 int launch_ce(const void* logits, const int64_t* targets, int64_t T, int64_t V, float grad_scale,
