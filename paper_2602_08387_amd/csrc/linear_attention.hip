@@ -1,130 +1,815 @@
-// Linear attention with a decay for each KV head: S_t = lambda S_{t-1} + k_t v_t^T, o_t = scale S_t^T q_t, and its gradient.
+// Linear attention with a decay for each KV head, and its gradient.  For one batch row and KV head, state S [dh, dh]:
+//
+//   S_t = lambda S_(t-1) + k_t v_t^T,   o_t = scale S_t^T q_t                                       (forward)
+//   dq_t = scale S_t do_t;   R_t = lambda R_(t+1) + scale sum_h q_t^h do_t^hT,  dk_t = R_t v_t,  dv_t = R_t^T k_t
+//
+// Over chunks of 64 tokens these are matrix products.  With i, j a token's place in its chunk and S the state before the chunk,
+//   o_i = scale (sum over j <= i of lambda^(i-j) (q_i . k_j) v_j + lambda^(i+1) S^T q_i),   S' = lambda^64 S + sum_j (lambda^(63-j) k_j) v_j^T
+// The gradient of q is the same with (do, v, k) in the place of (q, k, v) and the state transposed; those of k and v walk the chunks from
+// the last to the first with the state's gradient E, that of the state a chunk ends with:
+//   dv_j = scale sum over i >= j, h of lambda^(i-j) (q_i . k_j) do_i + lambda^(63-j) E^T k_j,   dk_j = ... (do_i . v_j) q_i + lambda^(63-j) E v_j
+//   E' = lambda^64 E + scale sum_i (lambda^(i+1) q_i) do_i^T
+// A chain of 64-token steps is long, so a sequence is cut into segments (linear_plan) that run side by side: a first kernel forms
+// what each segment adds to the state, a second adds these up from segment to segment, and the third does the chunks of a segment, starting
+// from the state it begins (ends) with.
+//
+// Precision.  States are fp32, in the accumulators and in memory.  The decayed keys (queries) whose products with the values (do) they sum are
+// split into three bf16 terms, so these products are exact up to fp32 (two terms where a state serves only results rounded to bf16), and
+// so are weighted scores, into two: sums of few heads or keys cancel, and a score rounded to bf16 then shows (gradients 4e-2 off in single elements).  A
+// state is rounded where it is multiplied with queries, to fp16, scaled by a power of two (1.5e-4 rms, where the result's own rounding to bf16 is
+// 1.7e-3; rounded to bf16 it would add as much again); the queries, scaled too, are exact in fp16.  Decays of many tokens are evaluated as
+// powers (exp2 of a multiple of the logarithm), the factor between chunks as the sum of two fp32, so that no rounding of lambda is repeated.
+//
+// Layout.  All products are v_mfma_f32_16x16x32_bf16, D[row][col] += A[row][k] B[k][col]: lane (g = lane / 16, r = lane % 16) holds row r of A and
+// column r of B, 8 of 32 k each, and rows 4 g .. 4 g + 3 of column r of D.  Scores are formed as S^T[j][i] = K Q^T, so that a lane
+// owns one query and its scores come out as the B operand of O^T[d][i] += V^T P^T: k-slot (g, e) is token 4 g + e of the first 16 for e < 4, and of
+// the second 16 otherwise, and the transposing reads of V take the same tokens.  Rows of O^T (and of the state's columns) are taken in the order
+// d = 32 (n / 2) + 8 (r / 4) + 4 (n % 2) + r % 4 for row r of block n, which puts 8 neighbours into one lane: 16-byte stores.
 #include "common.h"
 #include "kernels.h"
 
 namespace dl {
 
+constexpr int kChunk = 64;
+constexpr int kLinWaves = 8;   // waves of a workgroup: a state of 128 x 128 is 32 registers in each, and 16 of them fit a compute unit
+
 // The logarithm of a decay, minus infinity (no memory at all) made finite: times no token it is to give 0, not NaN.
 __device__ __forceinline__ double decay_log(float g) { return g < -1e30f ? -1e30 : (double)g; }
-// The decay of one token as the sum of two fp32: rounded to one, a state of n tokens' memory would be off by up to 6e-8 n.
+// A decay as the sum of two fp32: rounded to one, the state after n of them would be off by up to 6e-8 n.
 struct Decay { float hi, lo; };
-__device__ __forceinline__ Decay decay_of(float g) {
-  const double d = exp(decay_log(g));
+__device__ __forceinline__ Decay decay_of(float g, int tokens) {
+  const double d = exp(decay_log(g) * tokens);
   const float hi = (float)d;
   return Decay{hi, (float)(d - (double)hi)};
 }
 // lambda s + x
 __device__ __forceinline__ float decayed(const Decay& l, float s, float x) { return __builtin_fmaf(s, l.hi, __builtin_fmaf(s, l.lo, x)); }
+// lambda^n for 0 <= n, log2 = log2(lambda)
+__device__ __forceinline__ float power(float log2, int n) { return __builtin_amdgcn_exp2f(log2 * (float)n); }
 
-// One token after the other.  Workgroup: 16 columns of the state of one (batch row, KV head); thread: one of them in D / 16 rows.
-//   forward   S = lambda S + a b^T;                out_h = mult S^T x_h for the group's heads h
-//   REVERSE   R = lambda R + mult sum_h x_h y_h^T, from the last token to the first; out = R^T a
-// with b and y of the workgroup's 16 columns.  s_in is transposed if `flip`.
-struct RecurrentArgs {
-  const bf16_t *a, *b, *x, *y;
-  bf16_t* out;
-  const float *log_decay, *s_in;
-  float* s_out;
-  const int64_t* lengths;
-  int seq, Hq, Hkv, flip;
-  float mult;
-};
-template <int D, bool REVERSE>
-__global__ __launch_bounds__(256) void linear_recurrent_kernel(const RecurrentArgs p) {
-  constexpr int R = D / 16;
-  __shared__ float red[4][16];
-  const int pair = blockIdx.x, b = pair / p.Hkv, j = pair % p.Hkv, G = p.Hq / p.Hkv, col = (int)blockIdx.y * 16;
-  const int c = threadIdx.x & 15, rg = threadIdx.x >> 4, wave = threadIdx.x >> 6;
-  const Decay lam = decay_of(p.log_decay[j]);
-  int64_t len = p.lengths ? p.lengths[b] : p.seq;
-  len = len < 0 ? 0 : len > p.seq ? p.seq : len;
-  float s[R];
-#pragma unroll
-  for (int i = 0; i < R; ++i) {
-    const int row = i * 16 + rg;
-    s[i] = !p.s_in ? 0.f : p.s_in[(int64_t)pair * D * D + (p.flip ? (col + c) * D + row : row * D + col + c)];
+__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+
+// rows * 64 .. of one head: `rows` rows of D at stride ld; a row at or past `rows` reads as zeros and is not written
+template <int D>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const bf16_t* first, int64_t ld, int rows) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(first), 0, rows > 0 ? (int)(((rows - 1) * ld + D) * 2) : 0, 0x00020000);
+}
+__device__ __forceinline__ bf16x8 load8(__amdgpu_buffer_rsrc_t rs, uint32_t at) {
+  return __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)at, 0, 0));
+}
+__device__ __forceinline__ void store8(__amdgpu_buffer_rsrc_t rs, uint32_t at, const bf16x8& v) {
+  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), rs, (int)at, 0, 0);
+}
+
+// [rows][D] bf16 in LDS, 16-byte piece c of row r at piece c ^ swz(r), chosen so that 16 rows of one piece, and 4 rows of 64 bytes, fall into
+// different banks.
+template <int D>
+struct Rows {
+  static constexpr int BYTES = D * 2, PIECES = D / 8;
+  static __device__ __forceinline__ int swz(int r) {
+    if constexpr (PIECES == 16) return ((r & 3) << 2) | ((r >> 2) & 3);
+    else if constexpr (PIECES == 8) return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+    else return (r >> 2) & 3;
   }
-  auto reduce = [&](float v) {
-    v += __shfl_xor(v, 16, 64);
-    v += __shfl_xor(v, 32, 64);
-    __syncthreads();
-    if ((threadIdx.x & 63) < 16) red[wave][c] = v;
-    __syncthreads();
-    return (red[0][c] + red[1][c]) + (red[2][c] + red[3][c]);
-  };
-  for (int n = 0; n < p.seq; ++n) {
-    const int t = REVERSE ? p.seq - 1 - n : n;
-    const int64_t kv = (((int64_t)b * p.seq + t) * p.Hkv + j) * D, q = (((int64_t)b * p.seq + t) * p.Hq + (int64_t)j * G) * D;
-    if (t >= len) {
-      if (rg == 0) {
-        if (REVERSE) p.out[kv + col + c] = (bf16_t)0.f;
-        else for (int h = 0; h < G; ++h) p.out[q + (int64_t)h * D + col + c] = (bf16_t)0.f;
-      }
-      continue;
+  static __device__ __forceinline__ int at(int r, int piece) { return r * BYTES + ((piece ^ swz(r)) << 4); }
+  // operand of 16 rows from row0, k over step ks of the row
+  static __device__ __forceinline__ bf16x8 along(const char* t, int row0, int ks, int lane) {
+    return *reinterpret_cast<const bf16x8*>(t + at(row0 + (lane & 15), ks * 4 + (lane >> 4)));
+  }
+  // four values of 16 columns: rows row .. row + 3, the lane's column by the caller's piece and half of a piece
+  static __device__ __forceinline__ bf16x4 across(const char* t, int row, int piece, int half) {
+    return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(t + at(row, piece) + half * 8));
+  }
+  // operand of the 16 columns 16 n .. of the tile, k over the 32 rows from row0 (slots as at the top of the file)
+  static __device__ __forceinline__ bf16x8 columns(const char* t, int n, int row0, int lane) {
+    const int r = row0 + ((lane >> 4) << 2) + ((lane & 15) >> 2), piece = 2 * n + ((lane & 3) >> 1), half = lane & 1;
+    bf16x8 v;
+    v.lo = across(t, r, piece, half);
+    v.hi = across(t, r + 16, piece, half);
+    return v;
+  }
+  // the same of block n of the columns in stored order
+  static __device__ __forceinline__ bf16x8 columns_stored(const char* t, int n, int row0, int lane) {
+    const int r = row0 + ((lane >> 4) << 2) + ((lane & 15) >> 2), piece = (n >> 1) * 4 + (lane & 3), half = n & 1;
+    bf16x8 v;
+    v.lo = across(t, r, piece, half);
+    v.hi = across(t, r + 16, piece, half);
+    return v;
+  }
+};
+
+// A 64-row tile on its way from memory to LDS, through registers: 16 bytes a thread and piece.
+template <int D>
+struct Staged {
+  static constexpr int TOTAL = kChunk * Rows<D>::PIECES, THREADS = 64 * kLinWaves, N = (TOTAL + THREADS - 1) / THREADS;
+  bf16x8 v[N];
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t rs, int64_t ld) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int idx = i * THREADS + (int)threadIdx.x;
+      if (TOTAL % THREADS == 0 || idx < TOTAL) v[i] = load8(rs, (uint32_t)(idx / Rows<D>::PIECES * (int)ld * 2 + idx % Rows<D>::PIECES * 16));
     }
-    if constexpr (!REVERSE) {
-      const float bv = (float)p.b[kv + col + c];
+  }
+  __device__ __forceinline__ void store(char* t) const {
 #pragma unroll
-      for (int i = 0; i < R; ++i) s[i] = decayed(lam, s[i], (float)p.a[kv + i * 16 + rg] * bv);
-      for (int h = 0; h < G; ++h) {
-        float v = 0.f;
+    for (int i = 0; i < N; ++i) {
+      const int idx = i * THREADS + (int)threadIdx.x;
+      if (TOTAL % THREADS == 0 || idx < TOTAL) *reinterpret_cast<bf16x8*>(t + Rows<D>::at(idx / Rows<D>::PIECES, idx % Rows<D>::PIECES)) = v[i];
+    }
+  }
+};
+
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ f32x4 mfma16_f16(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+// Powers of two that take numbers up to some bound into the upper half of fp16's range (below 2^15, so that what is 2^29 times smaller than
+// the bound keeps its eleven bits), and back.
+struct Scale {
+  float up, down;
+  // exponent: of the bound, as an fp32 has it
+  __device__ __forceinline__ explicit Scale(int exponent) {
+    const int e = max(exponent, 14);
+    up = __int_as_float((268 - e) << 23);
+    down = e <= 14 ? __int_as_float(0) : __int_as_float((e - 14) << 23);
+  }
+};
+
+// An operand of KS steps (a lane's 8 values of 32 each, four lanes a row), in fp16: the rows scaled, exactly, to their largest value.
+template <int KS>
+struct ScaledRow {
+  f16x8 v[KS];
+  float down;
+  __device__ __forceinline__ explicit ScaledRow(const bf16x8 (&x)[KS]) {
+    uint32_t most = 0;
 #pragma unroll
-        for (int i = 0; i < R; ++i) v += s[i] * (float)p.x[q + (int64_t)h * D + i * 16 + rg];
-        v = reduce(v);
-        if (rg == 0) p.out[q + (int64_t)h * D + col + c] = (bf16_t)(v * p.mult);
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t two = __builtin_bit_cast(u32x4, x[k])[i];
+        most = max(most, max(two & 0x7fff0000u, (two << 16) & 0x7fff0000u));
       }
-    } else {
-      if (t < len - 1)
+    most = max(most, (uint32_t)__shfl_xor((int)most, 16, 64));
+    most = max(most, (uint32_t)__shfl_xor((int)most, 32, 64));
+    const Scale s((int)(most >> 23));
+    down = s.down;
 #pragma unroll
-        for (int i = 0; i < R; ++i) s[i] = decayed(lam, s[i], 0.f);
-      for (int h = 0; h < G; ++h) {
-        const float y = (float)p.y[q + (int64_t)h * D + col + c] * p.mult;
+    for (int k = 0; k < KS; ++k)
 #pragma unroll
-        for (int i = 0; i < R; ++i) s[i] += (float)p.x[q + (int64_t)h * D + i * 16 + rg] * y;
+      for (int e = 0; e < 8; ++e) v[k][e] = (_Float16)((float)x[k][e] * s.up);
+  }
+};
+
+__device__ __forceinline__ float uniform(float x) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x))); }
+
+// Weights of a chunk's tokens on their way into the state after the chunk (TO_END: lambda^(rows-1-t)) or into the gradient of the state
+// before it (mult lambda^(t+1)).  Of 64 tokens token 16 i + 4 g + k has weight lane[k] f[i].
+struct Weights {
+  float lane[4], f[4], log2;
+  int first;   // 4 g
+  template <bool TO_END>
+  __device__ __forceinline__ void init(float log2_, float mult, int lane_id) {
+    log2 = log2_;
+    first = (lane_id >> 4) << 2;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      lane[i] = mult * power(log2, TO_END ? 15 - first - i : first + i + 1);
+      f[i] = uniform(power(log2, TO_END ? 48 - 16 * i : 16 * i));
+    }
+  }
+};
+
+// A state [D along keys][D along values] over the waves: wave -> RB x CB blocks of 16 x 16 (of 32 x 32 elements four waves hold one each).  In
+// memory between the kernels it lies as the accumulators do: [wave][block][lane] f32x4.
+template <int D>
+struct State {
+  static constexpr int RB = D == 128 ? 2 : 1, CB = D == 32 ? 1 : D / 32, N = RB * CB, WAVES = D == 32 ? 4 : kLinWaves;
+  f32x4 a[RB][CB];
+  static __device__ __forceinline__ int row_block(int wave) { return (wave >> 1) * RB; }
+  static __device__ __forceinline__ int col_block(int wave) { return (wave & 1) * CB; }
+  // first of the four rows, and the column, of a lane in block (rb, cb) of the state
+  static __device__ __forceinline__ int row(int rb, int lane) { return rb * 16 + ((lane >> 4) << 2); }
+  static __device__ __forceinline__ int col(int cb, int lane) { return (cb >> 1) * 32 + (((lane & 15) >> 2) << 3) + ((cb & 1) << 2) + (lane & 3); }
+  static __device__ __forceinline__ bool holds(int wave) { return WAVES == kLinWaves || wave < WAVES; }
+
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+#pragma unroll
+      for (int j = 0; j < CB; ++j) a[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  __device__ __forceinline__ void decay(const Decay& l) {
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+#pragma unroll
+      for (int j = 0; j < CB; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) a[i][j][e] = decayed(l, a[i][j][e], 0.f);
+  }
+  // element of a [D][D] matrix, transposed if flip
+  static __device__ __forceinline__ int element(int row, int col, int flip) { return flip ? col * D + row : row * D + col; }
+  __device__ __forceinline__ void load_matrix(const float* s, int flip, int wave, int lane) {
+    if (!holds(wave)) return;
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+#pragma unroll
+      for (int j = 0; j < CB; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) a[i][j][e] = s[element(row(row_block(wave) + i, lane) + e, col(col_block(wave) + j, lane), flip)];
+  }
+  __device__ __forceinline__ void store_matrix(float* s, int wave, int lane) const {
+    if (!holds(wave)) return;
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+#pragma unroll
+      for (int j = 0; j < CB; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[element(row(row_block(wave) + i, lane) + e, col(col_block(wave) + j, lane), 0)] = a[i][j][e];
+  }
+  __device__ __forceinline__ void load(const float* s, int wave, int lane) {
+    if (!holds(wave)) return;
+#pragma unroll
+    for (int i = 0; i < N; ++i) a[i / CB][i % CB] = reinterpret_cast<const f32x4*>(s)[(wave * N + i) * 64 + lane];
+  }
+  __device__ __forceinline__ void store(float* s, int wave, int lane) const {
+    if (!holds(wave)) return;
+#pragma unroll
+    for (int i = 0; i < N; ++i) reinterpret_cast<f32x4*>(s)[(wave * N + i) * 64 + lane] = a[i / CB][i % CB];
+  }
+  // the largest of the wave's elements, those that are no numbers left out
+  __device__ __forceinline__ float largest(int wave) const {
+    float m = 0.f;
+    if (holds(wave)) {
+#pragma unroll
+      for (int i = 0; i < RB; ++i)
+#pragma unroll
+        for (int j = 0; j < CB; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) m = fmaxf(m, fabsf(a[i][j][e]));
+      if (__builtin_amdgcn_ballot_w64(m > 3e38f) != 0) {
+        m = 0.f;
+#pragma unroll
+        for (int i = 0; i < RB; ++i)
+#pragma unroll
+          for (int j = 0; j < CB; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) m = fabsf(a[i][j][e]) < INFINITY ? fmaxf(m, fabsf(a[i][j][e])) : m;
       }
-      float v = 0.f;
+    }
+    return wave_max(m);
+  }
+  // to LDS in fp16 [columns in stored order][rows]: an operand along either
+  __device__ __forceinline__ void to_lds(char* t, float up, int wave, int lane) const {
+    if (!holds(wave)) return;
 #pragma unroll
-      for (int i = 0; i < R; ++i) v += s[i] * (float)p.a[kv + i * 16 + rg];
-      v = reduce(v);
-      if (rg == 0) p.out[kv + col + c] = (bf16_t)v;
+    for (int i = 0; i < RB; ++i)
+#pragma unroll
+      for (int j = 0; j < CB; ++j) {
+        f16x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = (_Float16)(a[i][j][e] * up);
+        const int r = row(row_block(wave) + i, lane), p = (col_block(wave) + j) * 16 + (lane & 15);
+        *reinterpret_cast<f16x4*>(t + Rows<D>::at(p, r >> 3) + ((r & 7) << 1)) = v;
+      }
+  }
+  // += sum over the tile's 64 tokens of (w x)^T y, x and y in LDS; w x as the sum of SPLIT bf16.  rows: the tokens there are (the rest
+  // of the tile is zeros), which the weights to the end depend on.
+  template <int SPLIT, bool TO_END>
+  __device__ __forceinline__ void add(const char* x, const char* y, const Weights& w, int rows, int wave, int lane) {
+    if (!holds(wave)) return;
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      bf16x8 part[RB][SPLIT];
+#pragma unroll
+      for (int i = 0; i < RB; ++i) {
+        float f[8];
+        unpack8(Rows<D>::columns(x, row_block(wave) + i, p * 32, lane), f);
+        if (!TO_END || rows == kChunk) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) f[e] *= w.lane[e & 3] * w.f[2 * p + (e >> 2)];
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) f[e] *= power(w.log2, max(rows - 1 - (p * 32 + (e >> 2) * 16 + w.first + (e & 3)), 0));
+        }
+#pragma unroll
+        for (int k = 0; k < SPLIT; ++k) {
+          part[i][k] = pack8(f);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) f[e] -= (float)part[i][k][e];
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < CB; ++j) {
+        const bf16x8 v = Rows<D>::columns_stored(y, col_block(wave) + j, p * 32, lane);
+#pragma unroll
+        for (int k = SPLIT - 1; k >= 0; --k)
+#pragma unroll
+          for (int i = 0; i < RB; ++i) a[i][j] = mfma16(part[i][k], v, a[i][j]);
+      }
+    }
+  }
+};
+
+// The scale of a state whose waves left their largest elements in LDS.
+__device__ __forceinline__ Scale state_scale(const float* largest) {
+  float m = 0.f;
+#pragma unroll
+  for (int i = 0; i < kLinWaves; ++i) m = fmaxf(m, largest[i]);
+  return Scale(__builtin_amdgcn_readfirstlane(__float_as_int(m) >> 23));
+}
+
+// Weighted scores of 32 tokens as an operand: the sum of two bf16.
+struct Scores {
+  bf16x8 hi, lo;
+  __device__ __forceinline__ explicit Scores(const f32x4 (&sc)[2]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      hi[e] = (bf16_t)sc[e >> 2][e & 3];
+      lo[e] = (bf16_t)(sc[e >> 2][e & 3] - (float)hi[e]);
+    }
+  }
+  __device__ __forceinline__ f32x4 times(bf16x8 a, f32x4 c) const { return mfma16(a, hi, mfma16(a, lo, c)); }
+};
+
+struct LinearArgs {
+  const bf16_t *q, *k, *v, *d_o;
+  bf16_t *o, *dk, *dv;
+  const float* log_decay;
+  const int64_t* lengths;
+  float* seg;              // [pair][segment] states between the kernels
+  const float* s_in;
+  float* s_out;
+  int S, Hq, Hkv, flip;    // flip: s_in is read transposed
+  int seg_chunks, nseg;
+  float scale;
+};
+
+// tokens of batch row b
+__device__ __forceinline__ int row_length(const LinearArgs& p, int b) {
+  const int64_t n = p.lengths ? p.lengths[b] : p.S;
+  return (int)(n < 0 ? 0 : n > p.S ? p.S : n);
+}
+__device__ __forceinline__ float log2_decay(float g) { return (float)(decay_log(g) * 1.4426950408889634); }
+// ------------------------------------------------------------------------------------------
+// What a segment of m tokens adds to the state that passes through it: sum_t lambda^(m-1-t) k_t v_t^T, from k and v;
+// REVERSE: sum over t and the group's heads of scale lambda^(t+1) q_t do_t^T, from q and d_o.
+// ------------------------------------------------------------------------------------------
+template <int D, bool REVERSE>
+__global__ __launch_bounds__(64 * kLinWaves, 4) void linear_segment_kernel(const LinearArgs p) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  char *xt = smem, *yt = smem + kChunk * D * 2;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int pair = blockIdx.x / p.nseg, sg = blockIdx.x % p.nseg, b = pair / p.Hkv, j = pair % p.Hkv;
+  const int len = row_length(p, b), t0 = sg * p.seg_chunks * kChunk;
+  State<D> s;
+  s.clear();
+  float* out = p.seg + (int64_t)blockIdx.x * D * D;
+  const int m = min(len - t0, p.seg_chunks * kChunk);
+  if (m <= 0) {
+    s.store(out, wave, lane);
+    return;
+  }
+  const int G = REVERSE ? p.Hq / p.Hkv : 1, chunks = (m + kChunk - 1) / kChunk;
+  const int64_t ld = (int64_t)(REVERSE ? p.Hq : p.Hkv) * D;
+  const bf16_t *x = REVERSE ? p.q : p.k, *y = REVERSE ? p.d_o : p.v;
+  const int64_t first = ((int64_t)b * p.S + t0) * ld + (int64_t)j * G * D;
+  const float log2 = log2_decay(p.log_decay[j]);
+  const Decay whole = decay_of(p.log_decay[j], kChunk);
+  // chunks in the order in which the state passes through them
+  Staged<D> xs, ys;
+  auto fetch = [&](int it) {
+    const int c = REVERSE ? chunks - 1 - it / G : it, rows = min(m - c * kChunk, kChunk);
+    const int64_t at = first + (int64_t)c * kChunk * ld + (int64_t)(REVERSE ? it % G : 0) * D;
+    xs.load(rows_rsrc<D>(x + at, ld, rows), ld);
+    ys.load(rows_rsrc<D>(y + at, ld, rows), ld);
+  };
+  fetch(0);
+  Weights w;
+  w.init<!REVERSE>(log2, REVERSE ? p.scale : 1.f, lane);
+  for (int it = 0; it < chunks * G; ++it) {
+    __syncthreads();
+    xs.store(xt);
+    ys.store(yt);
+    __syncthreads();
+    if (it + 1 < chunks * G) fetch(it + 1);
+    const int rows = REVERSE ? kChunk : min(m - it * kChunk, kChunk);
+    if (it > 0 && it % G == 0) s.decay(rows == kChunk ? whole : decay_of(p.log_decay[j], rows));
+    s.template add<3, !REVERSE>(xt, yt, w, rows, wave, lane);
+  }
+  s.store(out, wave, lane);
+}
+
+// ------------------------------------------------------------------------------------------
+// From segment to segment: what each adds is replaced by the state it begins with; REVERSE: by the gradient of the state it ends
+// with.  A thread holds four elements of a state in fp64 (a decay of many tokens has no second fp32), eight segments ahead in flight.
+// ------------------------------------------------------------------------------------------
+template <int D, bool REVERSE>
+__global__ __launch_bounds__(256) void linear_scan_kernel(const LinearArgs p) {
+  using St = State<D>;
+  constexpr int PARTS = D * D / 1024, AHEAD = 8;
+  const int pair = blockIdx.x / PARTS, f = blockIdx.x % PARTS * 256 + threadIdx.x, b = pair / p.Hkv, j = pair % p.Hkv;
+  const int lane = f & 63, blk = (f >> 6) % St::N, wave = (f >> 6) / St::N;
+  const int row = St::row(St::row_block(wave) + blk / St::CB, lane), col = St::col(St::col_block(wave) + blk % St::CB, lane);
+  const int len = row_length(p, b), seg_tokens = p.seg_chunks * kChunk;
+  const double log = decay_log(p.log_decay[j]), whole = exp(log * seg_tokens);
+  f32x4* at = reinterpret_cast<f32x4*>(p.seg + (int64_t)pair * p.nseg * D * D) + f;
+  double s[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) s[e] = p.s_in ? (double)p.s_in[(int64_t)pair * D * D + St::element(row + e, col, p.flip)] : 0.0;
+  for (int n0 = 0; n0 < p.nseg; n0 += AHEAD) {
+    f32x4 u[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const int n = n0 + i;
+      if (n < p.nseg) u[i] = at[(int64_t)(REVERSE ? p.nseg - 1 - n : n) * (D * D / 4)];
+    }
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      if (n0 + i >= p.nseg) break;
+      const int n = REVERSE ? p.nseg - 1 - n0 - i : n0 + i, m = min(max(len - n * seg_tokens, 0), seg_tokens);
+      at[(int64_t)n * (D * D / 4)] = f32x4{(float)s[0], (float)s[1], (float)s[2], (float)s[3]};
+      if (m == 0) continue;
+      const double l = m == seg_tokens ? whole : exp(log * m);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[e] = l * s[e] + (double)u[i][e];
     }
   }
   if (p.s_out)
 #pragma unroll
-    for (int i = 0; i < R; ++i) p.s_out[(int64_t)pair * D * D + (i * 16 + rg) * D + col + c] = REVERSE && len > 0 ? decayed(lam, s[i], 0.f) : s[i];
+    for (int e = 0; e < 4; ++e) p.s_out[(int64_t)pair * D * D + St::element(row + e, col, 0)] = (float)s[e];
 }
 
-template <bool REVERSE>
-static int launch_recurrent(const RecurrentArgs& a, int64_t pairs, int64_t dh, hipStream_t st) {
-  const dim3 grid((unsigned)pairs, (unsigned)(dh / 16)), block(256);
-  if (dh == 128) hipLaunchKernelGGL((linear_recurrent_kernel<128, REVERSE>), grid, block, 0, st, a);
-  else if (dh == 64) hipLaunchKernelGGL((linear_recurrent_kernel<64, REVERSE>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((linear_recurrent_kernel<32, REVERSE>), grid, block, 0, st, a);
+// ------------------------------------------------------------------------------------------
+// o of a segment (dq of one, from d_o, v, k): its chunks from the first to the last, the state in the accumulators and, as an operand, in
+// LDS.  Four waves take 16 queries of a head each, the other four those of the next head; an odd last head is shared, half of the columns
+// for either.  SPLIT: 3 where the state goes on to the caller, 2 where it serves this kernel's products alone.
+// ------------------------------------------------------------------------------------------
+// NB blocks of 16 columns from n0 for the queries of one lane's row; returns them unscaled
+template <int D, int NB>
+__device__ __forceinline__ void out_tile(f32x4 (&o)[NB], const bf16x8 (&qf)[D / 32], const char* kt, const char* vt, const char* st, bool some,
+                                         float down, int tile, int n0, float log2, int lane) {
+  constexpr int KS = D / 32;
+  const int r = lane & 15, g = lane >> 4;
+#pragma unroll
+  for (int n = 0; n < NB; ++n) o[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (some) {
+    const ScaledRow<KS> qs(qf);
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+        o[n] = mfma16_f16(__builtin_bit_cast(f16x8, Rows<D>::along(st, (n0 + n) * 16, k, lane)), qs.v[k], o[n]);
+    const float after = power(log2, tile * 16 + r + 1) * down * qs.down;
+#pragma unroll
+    for (int n = 0; n < NB; ++n) o[n] *= after;
+  }
+#pragma unroll
+  for (int pr = 0; pr < 2; ++pr) {
+    if (2 * pr > tile) break;
+    f32x4 sc[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int blk = 2 * pr + i, d = (tile - blk) * 16 + r - g * 4;   // query's place less the key's
+      sc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (blk > tile) continue;
+#pragma unroll
+      for (int k = 0; k < KS; ++k) sc[i] = mfma16(Rows<D>::along(kt, blk * 16, k, lane), qf[k], sc[i]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sc[i][e] = e <= d ? sc[i][e] * power(log2, d - e) : 0.f;
+    }
+    const Scores pf(sc);
+#pragma unroll
+    for (int n = 0; n < NB; ++n) o[n] = pf.times(Rows<D>::columns_stored(vt, n0 + n, pr * 32, lane), o[n]);
+  }
+}
+
+template <int D, int SPLIT>
+__global__ __launch_bounds__(64 * kLinWaves, 4) void linear_out_kernel(const LinearArgs p, int pairs, int parts, int staged) {
+  constexpr int NB = D / 16, KS = D / 32;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  char *kt = smem, *vt = smem + kChunk * D * 2, *st = smem + 2 * kChunk * D * 2;
+  float* largest = reinterpret_cast<float*>(st + D * D * 2);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+  const int id = blockIdx.x % (pairs * p.nseg), part = blockIdx.x / (pairs * p.nseg);
+  const int pair = id / p.nseg, sg = id % p.nseg, b = pair / p.Hkv, j = pair % p.Hkv, G = p.Hq / p.Hkv;
+  const int per = (G + parts - 1) / parts, h0 = part * per, h1 = min(G, h0 + per);
+  const int len = row_length(p, b), t0 = sg * p.seg_chunks * kChunk;
+  const int rows_all = min(p.S - t0, p.seg_chunks * kChunk), m = max(min(len - t0, rows_all), 0), chunks = (m + kChunk - 1) / kChunk;
+  const int64_t ldq = (int64_t)p.Hq * D, ldk = (int64_t)p.Hkv * D, tok0 = (int64_t)b * p.S + t0;
+  const int64_t kv0 = tok0 * ldk + (int64_t)j * D, q0 = tok0 * ldq + (int64_t)j * G * D;
+  float* s_out = staged || part ? nullptr : p.s_out;
+
+  Staged<D> ks, vs;
+  auto fetch = [&](int c) {
+    const int64_t at = kv0 + (int64_t)c * kChunk * ldk;
+    ks.load(rows_rsrc<D>(p.k + at, ldk, min(m - c * kChunk, kChunk)), ldk);
+    vs.load(rows_rsrc<D>(p.v + at, ldk, min(m - c * kChunk, kChunk)), ldk);
+  };
+  if (chunks > 0) fetch(0);
+  State<D> s;
+  if (staged) s.load(p.seg + (int64_t)id * D * D, wave, lane);
+  else if (p.s_in) s.load_matrix(p.s_in + (int64_t)pair * D * D, p.flip, wave, lane);
+  else s.clear();
+  bool some = p.s_in != nullptr || sg > 0;   // a state that is not zero
+  float down = 0.f;
+  if (some) largest[wave] = s.largest(wave);
+  const float log2 = uniform(log2_decay(p.log_decay[j]));
+  const Decay whole = decay_of(p.log_decay[j], kChunk);
+  Weights w;
+  w.init<true>(log2, 1.f, lane);
+
+  for (int c = 0; c < chunks; ++c) {
+    const int rows = min(m - c * kChunk, kChunk), rows_out = min(rows_all - c * kChunk, kChunk);
+    const bool more = c + 1 < chunks;
+    __syncthreads();
+    if (some) {
+      const Scale sc = state_scale(largest);
+      down = sc.down;
+      s.to_lds(st, sc.up, wave, lane);
+    }
+    ks.store(kt);
+    vs.store(vt);
+    __syncthreads();
+    if (more) fetch(c + 1);
+    const int64_t qc = q0 + (int64_t)c * kChunk * ldq;
+    for (int h = h0; h < h1; h += 2) {
+      const bool both = h + 1 < h1;
+      if (!both && D == 32 && wave >= 4) break;   // 16 columns are not worth sharing
+      const int head = both ? h + (wave >> 2) : h, tile = (wave + (h >> 1)) & 3, t = tile * 16 + r;
+      const uint32_t at = (uint32_t)(t * (int)ldq * 2);
+      const __amdgpu_buffer_rsrc_t rq = rows_rsrc<D>(p.q + qc + (int64_t)head * D, ldq, rows);
+      const __amdgpu_buffer_rsrc_t ro = rows_rsrc<D>(p.o + qc + (int64_t)head * D, ldq, rows_out);
+      bf16x8 qf[KS];
+#pragma unroll
+      for (int k = 0; k < KS; ++k) qf[k] = load8(rq, at + k * 64 + g * 16);
+      auto finish = [&](auto& o, int n0, int blocks) {
+#pragma unroll
+        for (int n = 0; n < blocks; n += 2) {
+          bf16x8 v;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = (bf16_t)(t < rows ? o[n + (e >> 2)][e & 3] * p.scale : 0.f);
+          store8(ro, at + (n0 + n) * 32 + g * 16, v);
+        }
+      };
+      if (both || D == 32) {
+        f32x4 o[NB];
+        out_tile<D, NB>(o, qf, kt, vt, st, some, down, tile, 0, log2, lane);
+        finish(o, 0, NB);
+      } else if constexpr (D > 32) {
+        const int n0 = wave >= 4 ? NB / 2 : 0;
+        f32x4 o[NB / 2];
+        out_tile<D, NB / 2>(o, qf, kt, vt, st, some, down, tile, n0, log2, lane);
+        finish(o, n0, NB / 2);
+      }
+    }
+    if (more || s_out) {
+      s.decay(rows == kChunk ? whole : decay_of(p.log_decay[j], rows));
+      s.template add<SPLIT, true>(kt, vt, w, rows, wave, lane);
+      some = true;
+      if (more) largest[wave] = s.largest(wave);
+    }
+  }
+  const bf16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
+  for (int c = chunks; c * kChunk < rows_all; ++c)
+    for (int h = h0 + (wave >> 2); h < h1; h += 2) {
+      const __amdgpu_buffer_rsrc_t ro = rows_rsrc<D>(p.o + q0 + (int64_t)c * kChunk * ldq + (int64_t)h * D, ldq, min(rows_all - c * kChunk, kChunk));
+#pragma unroll
+      for (int n = 0; n < NB; n += 2) store8(ro, (uint32_t)(((wave & 3) * 16 + r) * (int)ldq * 2) + n * 32 + g * 16, zero);
+    }
+  if (s_out) s.store_matrix(s_out + (int64_t)pair * D * D, wave, lane);
+}
+
+// ------------------------------------------------------------------------------------------
+// dk and dv of a segment: its chunks from the last to the first, the gradient E of the state that a chunk ends with in the accumulators
+// and, as an operand along either side, in LDS.  The group's heads pass by, their q and do in LDS; four waves form dv of 16 keys each, the
+// other four dk, which is the same with q and do, k and v in each other's place and E transposed.
+// ------------------------------------------------------------------------------------------
+template <int D, int SPLIT>
+__global__ __launch_bounds__(64 * kLinWaves, 4) void linear_keys_kernel(const LinearArgs p, int staged) {
+  constexpr int NB = D / 16, KS = D / 32;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  char *qt = smem, *dt = smem + kChunk * D * 2, *et = smem + 2 * kChunk * D * 2;
+  float* largest = reinterpret_cast<float*>(et + D * D * 2);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+  const int pair = blockIdx.x / p.nseg, sg = blockIdx.x % p.nseg, b = pair / p.Hkv, j = pair % p.Hkv, G = p.Hq / p.Hkv;
+  const int len = row_length(p, b), t0 = sg * p.seg_chunks * kChunk;
+  const int rows_all = min(p.S - t0, p.seg_chunks * kChunk), m = max(min(len - t0, rows_all), 0), chunks = (m + kChunk - 1) / kChunk;
+  const int64_t ldq = (int64_t)p.Hq * D, ldk = (int64_t)p.Hkv * D, tok0 = (int64_t)b * p.S + t0;
+  const int64_t kv0 = tok0 * ldk + (int64_t)j * D, q0 = tok0 * ldq + (int64_t)j * G * D;
+  const bool dk_role = wave >= 4;
+  const int tile = wave & 3, key = tile * 16 + r;
+  const uint32_t at = (uint32_t)(key * (int)ldk * 2) + g * 16;
+  const bf16_t* own = (dk_role ? p.v : p.k) + kv0;
+  bf16_t* out = (dk_role ? p.dk : p.dv) + kv0;
+  const char *score_rows = dk_role ? dt : qt, *sum_rows = dk_role ? qt : dt;
+
+  Staged<D> qs, ds;
+  auto fetch = [&](int it) {
+    const int c = chunks - 1 - it / G, rows = min(m - c * kChunk, kChunk);
+    const int64_t from = q0 + (int64_t)c * kChunk * ldq + (int64_t)(it % G) * D;
+    qs.load(rows_rsrc<D>(p.q + from, ldq, rows), ldq);
+    ds.load(rows_rsrc<D>(p.d_o + from, ldq, rows), ldq);
+  };
+  if (chunks > 0) fetch(0);
+  State<D> s;
+  if (staged) s.load(p.seg + (int64_t)blockIdx.x * D * D, wave, lane);
+  else if (p.s_in) s.load_matrix(p.s_in + (int64_t)pair * D * D, 0, wave, lane);
+  else s.clear();
+  // not zero: a gradient comes in, or the row goes on behind this segment
+  bool some = p.s_in != nullptr || len > t0 + p.seg_chunks * kChunk;
+  float down = 0.f;
+  if (some) largest[wave] = s.largest(wave);
+  const float log2 = uniform(log2_decay(p.log_decay[j]));
+  const Decay whole = decay_of(p.log_decay[j], kChunk);
+  Weights w;
+  w.init<false>(log2, p.scale, lane);
+  f32x4 acc[NB];
+  bf16x8 kf[KS];
+  for (int it = 0; it < chunks * G; ++it) {
+    const int c = chunks - 1 - it / G, h = it % G, rows = min(m - c * kChunk, kChunk);
+    const int64_t kc = (int64_t)c * kChunk * ldk;
+    if (h == 0) {
+      const __amdgpu_buffer_rsrc_t rk = rows_rsrc<D>(own + kc, ldk, rows);
+#pragma unroll
+      for (int k = 0; k < KS; ++k) kf[k] = load8(rk, at + k * 64);
+    }
+    __syncthreads();
+    if (h == 0 && some) {
+      const Scale sc = state_scale(largest);
+      down = sc.down;
+      s.to_lds(et, sc.up, wave, lane);
+    }
+    qs.store(qt);
+    ds.store(dt);
+    __syncthreads();
+    if (it + 1 < chunks * G) fetch(it + 1);
+    if (h == 0) {
+#pragma unroll
+      for (int n = 0; n < NB; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (some) {
+        const ScaledRow<KS> ks(kf);
+        if (!dk_role) {
+#pragma unroll
+          for (int k = 0; k < KS; ++k)
+#pragma unroll
+            for (int n = 0; n < NB; ++n) acc[n] = mfma16_f16(__builtin_bit_cast(f16x8, Rows<D>::along(et, n * 16, k, lane)), ks.v[k], acc[n]);
+        } else {
+          // E's columns along keys in stored order; its rows as they lie are along values in the order of the operand
+#pragma unroll
+          for (int k = 0; k < KS; ++k)
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+              acc[n] = mfma16_f16(__builtin_bit_cast(f16x8, Rows<D>::columns_stored(et, n, k * 32, lane)), ks.v[k], acc[n]);
+        }
+        const float left = power(log2, max(rows - 1 - key, 0)) * down * ks.down;
+#pragma unroll
+        for (int n = 0; n < NB; ++n) acc[n] *= left;
+      }
+    }
+#pragma unroll
+    for (int pr = 0; pr < 2; ++pr) {
+      if (2 * pr + 1 < tile) continue;
+      f32x4 sc[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int blk = 2 * pr + i, d = (blk - tile) * 16 + g * 4 - r;   // first query's place less the key's
+        sc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (blk < tile) continue;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) sc[i] = mfma16(Rows<D>::along(score_rows, blk * 16, k, lane), kf[k], sc[i]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sc[i][e] = d + e >= 0 ? sc[i][e] * (p.scale * power(log2, d + e)) : 0.f;
+      }
+      const Scores pf(sc);
+#pragma unroll
+      for (int n = 0; n < NB; ++n) acc[n] = pf.times(Rows<D>::columns_stored(sum_rows, n, pr * 32, lane), acc[n]);
+    }
+    if (c > 0 || (!staged && p.s_out)) {
+      if (h == 0) s.decay(rows == kChunk ? whole : decay_of(p.log_decay[j], rows));
+      s.template add<SPLIT, false>(qt, dt, w, rows, wave, lane);
+      some = true;
+      if (h == G - 1 && c > 0) largest[wave] = s.largest(wave);
+    }
+    if (h == G - 1) {
+      const __amdgpu_buffer_rsrc_t ro = rows_rsrc<D>(out + kc, ldk, min(rows_all - c * kChunk, kChunk));
+#pragma unroll
+      for (int n = 0; n < NB; n += 2) {
+        bf16x8 v;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = (bf16_t)(key < rows ? acc[n + (e >> 2)][e & 3] : 0.f);
+        store8(ro, at + n * 32, v);
+      }
+    }
+  }
+  const bf16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
+  for (int c = chunks; c * kChunk < rows_all; ++c) {
+    const __amdgpu_buffer_rsrc_t ro = rows_rsrc<D>(out + (int64_t)c * kChunk * ldk, ldk, min(rows_all - c * kChunk, kChunk));
+#pragma unroll
+    for (int n = 0; n < NB; n += 2) store8(ro, at + n * 32, zero);
+  }
+  if (!staged && p.s_out) s.store_matrix(p.s_out + (int64_t)pair * D * D, wave, lane);
+}
+
+// ------------------------------------------------------------------------------------------
+// Host side
+// ------------------------------------------------------------------------------------------
+constexpr int kLinearBlocks = 512;   // workgroups that fill the chip: two on each compute unit
+
+// Segments of a sequence, a whole number of chunks each, and the workgroups that share a segment's query heads: as many segments as
+// make kLinearBlocks workgroups, of two chunks at the least.
+struct LinearPlan { int chunks, seg_chunks, nseg; };
+static LinearPlan linear_plan(int64_t pairs, int64_t S) {
+  LinearPlan p;
+  p.chunks = (int)((S + kChunk - 1) / kChunk);
+  int64_t n = (kLinearBlocks + pairs - 1) / pairs;
+  if (n > p.chunks / 2) n = p.chunks / 2;
+  if (n < 1) n = 1;
+  p.seg_chunks = (int)((p.chunks + n - 1) / n);
+  p.nseg = (p.chunks + p.seg_chunks - 1) / p.seg_chunks;
+  return p;
+}
+// room for the states of all segments: below twice kLinearBlocks of them, and a size that does not fall as the call grows
+static size_t segment_bytes(int64_t pairs, int64_t S, int64_t dh) {
+  const int64_t chunks = (S + kChunk - 1) / kChunk;
+  const int64_t n = pairs < 2 * kLinearBlocks && pairs * chunks < 2 * kLinearBlocks ? pairs * chunks : 2 * kLinearBlocks;
+  return (size_t)(n * dh * dh) * sizeof(float);
+}
+size_t linear_attention_fwd_workspace(int64_t B, int64_t S, int64_t Hq, int64_t Hkv, int64_t dh) { return segment_bytes(B * Hkv, S, dh); }
+size_t linear_attention_bwd_workspace(int64_t B, int64_t S, int64_t Hq, int64_t Hkv, int64_t dh) { return segment_bytes(B * Hkv, S, dh); }
+
+template <int D, bool REVERSE>
+static int run_states(const LinearArgs& a, int64_t pairs, hipStream_t st) {
+  hipLaunchKernelGGL((linear_segment_kernel<D, REVERSE>), dim3((unsigned)(pairs * a.nseg)), dim3(64 * kLinWaves), 2 * kChunk * D * 2, st, a);
+  if (int rc = check_launch("linear attention (segments)")) return rc;
+  hipLaunchKernelGGL((linear_scan_kernel<D, REVERSE>), dim3((unsigned)(pairs * (D * D / 1024))), dim3(256), 0, st, a);
+  return check_launch("linear attention (scan)");
+}
+
+// o from (q, k, v), or dq from (d_o, v, k) with the state transposed
+template <int D>
+static int run_out(const LinearArgs& a, int64_t pairs, hipStream_t st) {
+  constexpr size_t lds = (2 * kChunk + D) * D * 2 + kLinWaves * sizeof(float);
+  static std::atomic<unsigned long long> done2, done3;
+  const int G = a.Hq / a.Hkv;
+  int parts = (int)((kLinearBlocks + pairs * a.nseg - 1) / (pairs * a.nseg));
+  parts = parts < G ? parts : G;
+  const int staged = a.nseg > 1 || (parts > 1 && a.s_out);
+  if (staged)
+    if (int rc = run_states<D, false>(a, pairs, st)) return rc;
+  const dim3 grid((unsigned)(pairs * a.nseg * parts));
+  if (a.nseg > 1) {
+    if (int rc = reserve_lds(linear_out_kernel<D, 2>, lds, done2, "linear attention")) return rc;
+    hipLaunchKernelGGL((linear_out_kernel<D, 2>), grid, dim3(64 * kLinWaves), lds, st, a, (int)pairs, parts, staged);
+  } else {
+    if (int rc = reserve_lds(linear_out_kernel<D, 3>, lds, done3, "linear attention")) return rc;
+    hipLaunchKernelGGL((linear_out_kernel<D, 3>), grid, dim3(64 * kLinWaves), lds, st, a, (int)pairs, parts, staged);
+  }
   return check_launch("linear attention");
 }
 
-size_t linear_attention_fwd_workspace(int64_t B, int64_t S, int64_t Hq, int64_t Hkv, int64_t dh) { return 256; }
-size_t linear_attention_bwd_workspace(int64_t B, int64_t S, int64_t Hq, int64_t Hkv, int64_t dh) { return 256; }
+template <int D>
+static int run_keys(const LinearArgs& a, int64_t pairs, hipStream_t st) {
+  constexpr size_t lds = (2 * kChunk + D) * D * 2 + kLinWaves * sizeof(float);
+  static std::atomic<unsigned long long> done2, done3;
+  const dim3 grid((unsigned)(pairs * a.nseg));
+  if (a.nseg > 1) {
+    if (int rc = run_states<D, true>(a, pairs, st)) return rc;
+    if (int rc = reserve_lds(linear_keys_kernel<D, 2>, lds, done2, "linear attention")) return rc;
+    hipLaunchKernelGGL((linear_keys_kernel<D, 2>), grid, dim3(64 * kLinWaves), lds, st, a, 1);
+  } else {
+    if (int rc = reserve_lds(linear_keys_kernel<D, 3>, lds, done3, "linear attention")) return rc;
+    hipLaunchKernelGGL((linear_keys_kernel<D, 3>), grid, dim3(64 * kLinWaves), lds, st, a, 0);
+  }
+  return check_launch("linear attention (keys)");
+}
+
+static LinearArgs linear_args(const LinearCall& c, void* workspace) {
+  const LinearPlan plan = linear_plan(c.B * c.Hkv, c.S);
+  LinearArgs a{};
+  a.q = (const bf16_t*)c.q; a.k = (const bf16_t*)c.k; a.v = (const bf16_t*)c.v;
+  a.log_decay = c.log_decay; a.lengths = c.lengths; a.seg = (float*)workspace;
+  a.S = (int)c.S; a.Hq = (int)c.Hq; a.Hkv = (int)c.Hkv;
+  a.seg_chunks = plan.seg_chunks; a.nseg = plan.nseg; a.scale = c.scale;
+  return a;
+}
 
 int launch_linear_attention_fwd(const LinearCall& c, const float* s_in, void* o, float* s_out, void* workspace, hipStream_t st) {
-  RecurrentArgs a{};
-  a.a = (const bf16_t*)c.k; a.b = (const bf16_t*)c.v; a.x = (const bf16_t*)c.q; a.out = (bf16_t*)o;
-  a.log_decay = c.log_decay; a.s_in = s_in; a.s_out = s_out; a.lengths = c.lengths;
-  a.seq = (int)c.S; a.Hq = (int)c.Hq; a.Hkv = (int)c.Hkv; a.mult = c.scale;
-  return launch_recurrent<false>(a, c.B * c.Hkv, c.dh, st);
+  LinearArgs a = linear_args(c, workspace);
+  a.o = (bf16_t*)o; a.s_in = s_in; a.s_out = s_out;
+  const int64_t pairs = c.B * c.Hkv;
+  return c.dh == 128 ? run_out<128>(a, pairs, st) : c.dh == 64 ? run_out<64>(a, pairs, st) : run_out<32>(a, pairs, st);
 }
 
 int launch_linear_attention_bwd(const LinearCall& c, const float* s_in, const void* d_o, const float* ds_out, void* dq, void* dk, void* dv,
                                 float* ds_in, void* workspace, hipStream_t st) {
-  RecurrentArgs a{};
-  a.log_decay = c.log_decay; a.lengths = c.lengths;
-  a.seq = (int)c.S; a.Hq = (int)c.Hq; a.Hkv = (int)c.Hkv; a.mult = c.scale;
-  a.a = (const bf16_t*)c.v; a.b = (const bf16_t*)c.k; a.x = (const bf16_t*)d_o; a.out = (bf16_t*)dq; a.s_in = s_in; a.flip = 1;
-  if (int rc = launch_recurrent<false>(a, c.B * c.Hkv, c.dh, st)) return rc;
-  a.x = (const bf16_t*)d_o; a.y = (const bf16_t*)c.q; a.out = (bf16_t*)dk; a.s_in = ds_out;
-  if (int rc = launch_recurrent<true>(a, c.B * c.Hkv, c.dh, st)) return rc;
-  a.a = (const bf16_t*)c.k; a.x = (const bf16_t*)c.q; a.y = (const bf16_t*)d_o; a.out = (bf16_t*)dv; a.s_out = ds_in; a.flip = 0;
-  return launch_recurrent<true>(a, c.B * c.Hkv, c.dh, st);
+  const int64_t pairs = c.B * c.Hkv;
+  LinearArgs a = linear_args(c, workspace);
+  a.q = (const bf16_t*)d_o; a.k = (const bf16_t*)c.v; a.v = (const bf16_t*)c.k;
+  a.o = (bf16_t*)dq; a.s_in = s_in; a.flip = 1;
+  if (int rc = c.dh == 128 ? run_out<128>(a, pairs, st) : c.dh == 64 ? run_out<64>(a, pairs, st) : run_out<32>(a, pairs, st)) return rc;
+  a = linear_args(c, workspace);
+  a.d_o = (const bf16_t*)d_o; a.dk = (bf16_t*)dk; a.dv = (bf16_t*)dv; a.s_in = ds_out; a.s_out = ds_in;
+  return c.dh == 128 ? run_keys<128>(a, pairs, st) : c.dh == 64 ? run_keys<64>(a, pairs, st) : run_keys<32>(a, pairs, st);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -148,7 +833,7 @@ __global__ __launch_bounds__(256) void linear_step_kernel(const bf16_t* __restri
       for (int h = 0; h < G; ++h) *reinterpret_cast<bf16x4*>(op + (int64_t)h * D + c) = zero;
     return;
   }
-  const Decay lam = decay_of(log_decay[j]);
+  const Decay lam = decay_of(log_decay[j], 1);
   const bf16_t* kp = k + (int64_t)pair * D;
   const bf16x4 vv = *reinterpret_cast<const bf16x4*>(v + (int64_t)pair * D + c);
   float* sp = state + (int64_t)pair * D * D + c;
