@@ -49,6 +49,15 @@ __device__ __forceinline__ float power(float log2, int n) { return __builtin_amd
 
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
+// A value that the compiler works with from here on only: without this it keeps what it can derive from the lane's number and the decay
+// (LDS addresses, powers) for every phase of a loop in registers throughout, a hundred more than there are, and reloads them from scratch
+// memory in every iteration.
+template <typename T>
+__device__ __forceinline__ T here(T x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 // rows * 64 .. of one head: `rows` rows of D at stride ld; a row at or past `rows` reads as zeros and is not written
 template <int D>
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const bf16_t* first, int64_t ld, int rows) {
@@ -104,16 +113,18 @@ struct Staged {
   static constexpr int TOTAL = kChunk * Rows<D>::PIECES, THREADS = 64 * kLinWaves, N = (TOTAL + THREADS - 1) / THREADS;
   bf16x8 v[N];
   __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t rs, int64_t ld) {
+    const int thread = here((int)threadIdx.x);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int idx = i * THREADS + (int)threadIdx.x;
+      const int idx = i * THREADS + thread;
       if (TOTAL % THREADS == 0 || idx < TOTAL) v[i] = load8(rs, (uint32_t)(idx / Rows<D>::PIECES * (int)ld * 2 + idx % Rows<D>::PIECES * 16));
     }
   }
   __device__ __forceinline__ void store(char* t) const {
+    const int thread = here((int)threadIdx.x);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int idx = i * THREADS + (int)threadIdx.x;
+      const int idx = i * THREADS + thread;
       if (TOTAL % THREADS == 0 || idx < TOTAL) *reinterpret_cast<bf16x8*>(t + Rows<D>::at(idx / Rows<D>::PIECES, idx % Rows<D>::PIECES)) = v[i];
     }
   }
@@ -163,30 +174,28 @@ struct ScaledRow {
 __device__ __forceinline__ float uniform(float x) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x))); }
 
 // Weights of a chunk's tokens on their way into the state after the chunk (TO_END: lambda^(rows-1-t)) or into the gradient of the state
-// before it (mult lambda^(t+1)).  Of 64 tokens token 16 i + 4 g + k has weight lane[k] f[i].
+// before it (mult lambda^(t+1)): those of the lane's tokens 32 p + its slots, of a full chunk.
 struct Weights {
-  float lane[4], f[4], log2;
-  int first;   // 4 g
+  float w[2][8], log2;
   template <bool TO_END>
-  __device__ __forceinline__ void init(float log2_, float mult, int lane_id) {
+  __device__ __forceinline__ void init(float log2_, float mult, int lane) {
     log2 = log2_;
-    first = (lane_id >> 4) << 2;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      lane[i] = mult * power(log2, TO_END ? 15 - first - i : first + i + 1);
-      f[i] = uniform(power(log2, TO_END ? 48 - 16 * i : 16 * i));
-    }
+    for (int p = 0; p < 2; ++p)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[p][e] = mult * power(log2, TO_END ? 63 - token(p, e, lane) : token(p, e, lane) + 1);
   }
+  static __device__ __forceinline__ int token(int p, int e, int lane) { return p * 32 + (e >> 2) * 16 + ((lane >> 4) << 2) + (e & 3); }
 };
 
 // A state [D along keys][D along values] over the waves: wave -> RB x CB blocks of 16 x 16 (of 32 x 32 elements four waves hold one each).  In
 // memory between the kernels it lies as the accumulators do: [wave][block][lane] f32x4.
 template <int D>
 struct State {
-  static constexpr int RB = D == 128 ? 2 : 1, CB = D == 32 ? 1 : D / 32, N = RB * CB, WAVES = D == 32 ? 4 : kLinWaves;
+  static constexpr int RB = 1, CB = D == 128 ? 8 : D / 32, N = RB * CB, WAVES = D == 32 ? 4 : kLinWaves;
   f32x4 a[RB][CB];
-  static __device__ __forceinline__ int row_block(int wave) { return (wave >> 1) * RB; }
-  static __device__ __forceinline__ int col_block(int wave) { return (wave & 1) * CB; }
+  static __device__ __forceinline__ int row_block(int wave) { return D == 128 ? wave : wave >> 1; }
+  static __device__ __forceinline__ int col_block(int wave) { return D == 128 ? 0 : (wave & 1) * CB; }
   // first of the four rows, and the column, of a lane in block (rb, cb) of the state
   static __device__ __forceinline__ int row(int rb, int lane) { return rb * 16 + ((lane >> 4) << 2); }
   static __device__ __forceinline__ int col(int cb, int lane) { return (cb >> 1) * 32 + (((lane & 15) >> 2) << 3) + ((cb & 1) << 2) + (lane & 3); }
@@ -261,6 +270,7 @@ struct State {
   // to LDS in fp16 [columns in stored order][rows]: an operand along either
   __device__ __forceinline__ void to_lds(char* t, float up, int wave, int lane) const {
     if (!holds(wave)) return;
+    lane = here(lane);
 #pragma unroll
     for (int i = 0; i < RB; ++i)
 #pragma unroll
@@ -277,6 +287,7 @@ struct State {
   template <int SPLIT, bool TO_END>
   __device__ __forceinline__ void add(const char* x, const char* y, const Weights& w, int rows, int wave, int lane) {
     if (!holds(wave)) return;
+    lane = here(lane);
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
       bf16x8 part[RB][SPLIT];
@@ -286,10 +297,11 @@ struct State {
         unpack8(Rows<D>::columns(x, row_block(wave) + i, p * 32, lane), f);
         if (!TO_END || rows == kChunk) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) f[e] *= w.lane[e & 3] * w.f[2 * p + (e >> 2)];
+          for (int e = 0; e < 8; ++e) f[e] *= w.w[p][e];
         } else {
+          const float log2 = here(w.log2);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) f[e] *= power(w.log2, max(rows - 1 - (p * 32 + (e >> 2) * 16 + w.first + (e & 3)), 0));
+          for (int e = 0; e < 8; ++e) f[e] *= power(log2, max(rows - 1 - Weights::token(p, e, lane), 0));
         }
 #pragma unroll
         for (int k = 0; k < SPLIT; ++k) {
@@ -317,6 +329,36 @@ __device__ __forceinline__ Scale state_scale(const float* largest) {
   for (int i = 0; i < kLinWaves; ++i) m = fmaxf(m, largest[i]);
   return Scale(__builtin_amdgcn_readfirstlane(__float_as_int(m) >> 23));
 }
+
+// lambda^(place of the query - place of the key) for a 16 x 16 block of scores whose lane holds four keys (queries) of one query (key): of the
+// block on the diagonal (left: the lane's query less the first of its keys; the rest of it masked), and of the block next to it, from which the further ones
+// differ by a factor.
+struct Decays {
+  float same[4], next[4], f2, f3;
+  // step: -1 where the lane holds four keys, 1 where it holds four queries
+  __device__ __forceinline__ Decays(float log2, float mult, int left, int step) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int d = left + step * e;
+      same[e] = d >= 0 ? mult * power(log2, d) : 0.f;
+      next[e] = mult * power(log2, 16 + d);
+    }
+    f2 = uniform(power(log2, 16));
+    f3 = uniform(power(log2, 32));
+  }
+  // blocks: from the key's to the query's; keep(e) is false for what the diagonal block masks
+  template <typename F>
+  __device__ __forceinline__ void apply(f32x4& s, int blocks, F&& keep) const {
+    if (blocks == 0) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[e] = keep(e) ? s[e] * same[e] : 0.f;
+    } else {
+      const float f = blocks == 1 ? 1.f : blocks == 2 ? f2 : f3;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[e] *= next[e] * f;
+    }
+  }
+};
 
 // Weighted scores of 32 tokens as an operand: the sum of two bf16.
 struct Scores {
@@ -393,7 +435,7 @@ __global__ __launch_bounds__(64 * kLinWaves, 4) void linear_segment_kernel(const
     __syncthreads();
     if (it + 1 < chunks * G) fetch(it + 1);
     const int rows = REVERSE ? kChunk : min(m - it * kChunk, kChunk);
-    if (it > 0 && it % G == 0) s.decay(rows == kChunk ? whole : decay_of(p.log_decay[j], rows));
+    if (it > 0 && it % G == 0) s.decay(rows == kChunk ? whole : Decay{power(log2, rows), 0.f});
     s.template add<3, !REVERSE>(xt, yt, w, rows, wave, lane);
   }
   s.store(out, wave, lane);
@@ -447,8 +489,9 @@ __global__ __launch_bounds__(256) void linear_scan_kernel(const LinearArgs p) {
 // NB blocks of 16 columns from n0 for the queries of one lane's row; returns them unscaled
 template <int D, int NB>
 __device__ __forceinline__ void out_tile(f32x4 (&o)[NB], const bf16x8 (&qf)[D / 32], const char* kt, const char* vt, const char* st, bool some,
-                                         float down, int tile, int n0, float log2, int lane) {
+                                         float down, int tile, int n0, float log2, const Decays& ds, int lane) {
   constexpr int KS = D / 32;
+  lane = here(lane);
   const int r = lane & 15, g = lane >> 4;
 #pragma unroll
   for (int n = 0; n < NB; ++n) o[n] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -469,13 +512,12 @@ __device__ __forceinline__ void out_tile(f32x4 (&o)[NB], const bf16x8 (&qf)[D / 
     f32x4 sc[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const int blk = 2 * pr + i, d = (tile - blk) * 16 + r - g * 4;   // query's place less the key's
+      const int blk = 2 * pr + i;
       sc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
       if (blk > tile) continue;
 #pragma unroll
       for (int k = 0; k < KS; ++k) sc[i] = mfma16(Rows<D>::along(kt, blk * 16, k, lane), qf[k], sc[i]);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sc[i][e] = e <= d ? sc[i][e] * power(log2, d - e) : 0.f;
+      ds.apply(sc[i], tile - blk, [&](int e) { return g * 4 + e <= r; });
     }
     const Scores pf(sc);
 #pragma unroll
@@ -484,7 +526,7 @@ __device__ __forceinline__ void out_tile(f32x4 (&o)[NB], const bf16x8 (&qf)[D / 
 }
 
 template <int D, int SPLIT>
-__global__ __launch_bounds__(64 * kLinWaves, 4) void linear_out_kernel(const LinearArgs p, int pairs, int parts, int staged) {
+__global__ __launch_bounds__(64 * kLinWaves, D == 128 ? 2 : 4) void linear_out_kernel(const LinearArgs p, int pairs, int parts, int staged) {
   constexpr int NB = D / 16, KS = D / 32;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   char *kt = smem, *vt = smem + kChunk * D * 2, *st = smem + 2 * kChunk * D * 2;
@@ -517,6 +559,7 @@ __global__ __launch_bounds__(64 * kLinWaves, 4) void linear_out_kernel(const Lin
   const Decay whole = decay_of(p.log_decay[j], kChunk);
   Weights w;
   w.init<true>(log2, 1.f, lane);
+  const Decays decays(log2, 1.f, r - g * 4, -1);
 
   for (int c = 0; c < chunks; ++c) {
     const int rows = min(m - c * kChunk, kChunk), rows_out = min(rows_all - c * kChunk, kChunk);
@@ -553,17 +596,17 @@ __global__ __launch_bounds__(64 * kLinWaves, 4) void linear_out_kernel(const Lin
       };
       if (both || D == 32) {
         f32x4 o[NB];
-        out_tile<D, NB>(o, qf, kt, vt, st, some, down, tile, 0, log2, lane);
+        out_tile<D, NB>(o, qf, kt, vt, st, some, down, tile, 0, log2, decays, lane);
         finish(o, 0, NB);
       } else if constexpr (D > 32) {
         const int n0 = wave >= 4 ? NB / 2 : 0;
         f32x4 o[NB / 2];
-        out_tile<D, NB / 2>(o, qf, kt, vt, st, some, down, tile, n0, log2, lane);
+        out_tile<D, NB / 2>(o, qf, kt, vt, st, some, down, tile, n0, log2, decays, lane);
         finish(o, n0, NB / 2);
       }
     }
     if (more || s_out) {
-      s.decay(rows == kChunk ? whole : decay_of(p.log_decay[j], rows));
+      s.decay(rows == kChunk ? whole : Decay{power(log2, rows), 0.f});
       s.template add<SPLIT, true>(kt, vt, w, rows, wave, lane);
       some = true;
       if (more) largest[wave] = s.largest(wave);
@@ -585,7 +628,7 @@ __global__ __launch_bounds__(64 * kLinWaves, 4) void linear_out_kernel(const Lin
 // other four dk, which is the same with q and do, k and v in each other's place and E transposed.
 // ------------------------------------------------------------------------------------------
 template <int D, int SPLIT>
-__global__ __launch_bounds__(64 * kLinWaves, 4) void linear_keys_kernel(const LinearArgs p, int staged) {
+__global__ __launch_bounds__(64 * kLinWaves, D == 128 ? 2 : 4) void linear_keys_kernel(const LinearArgs p, int staged) {
   constexpr int NB = D / 16, KS = D / 32;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   char *qt = smem, *dt = smem + kChunk * D * 2, *et = smem + 2 * kChunk * D * 2;
@@ -623,6 +666,7 @@ __global__ __launch_bounds__(64 * kLinWaves, 4) void linear_keys_kernel(const Li
   const Decay whole = decay_of(p.log_decay[j], kChunk);
   Weights w;
   w.init<false>(log2, p.scale, lane);
+  const Decays decays(log2, p.scale, g * 4 - r, 1);
   f32x4 acc[NB];
   bf16x8 kf[KS];
   for (int it = 0; it < chunks * G; ++it) {
@@ -648,6 +692,7 @@ __global__ __launch_bounds__(64 * kLinWaves, 4) void linear_keys_kernel(const Li
       for (int n = 0; n < NB; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
       if (some) {
         const ScaledRow<KS> ks(kf);
+        const int lane = here(threadIdx.x & 63);
         if (!dk_role) {
 #pragma unroll
           for (int k = 0; k < KS; ++k)
@@ -661,7 +706,7 @@ __global__ __launch_bounds__(64 * kLinWaves, 4) void linear_keys_kernel(const Li
             for (int n = 0; n < NB; ++n)
               acc[n] = mfma16_f16(__builtin_bit_cast(f16x8, Rows<D>::columns_stored(et, n, k * 32, lane)), ks.v[k], acc[n]);
         }
-        const float left = power(log2, max(rows - 1 - key, 0)) * down * ks.down;
+        const float left = power(here(log2), max(rows - 1 - key, 0)) * down * ks.down;
 #pragma unroll
         for (int n = 0; n < NB; ++n) acc[n] *= left;
       }
@@ -669,23 +714,23 @@ __global__ __launch_bounds__(64 * kLinWaves, 4) void linear_keys_kernel(const Li
 #pragma unroll
     for (int pr = 0; pr < 2; ++pr) {
       if (2 * pr + 1 < tile) continue;
+      const int lane = here(threadIdx.x & 63), r = lane & 15, g = lane >> 4;
       f32x4 sc[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const int blk = 2 * pr + i, d = (blk - tile) * 16 + g * 4 - r;   // first query's place less the key's
+        const int blk = 2 * pr + i;
         sc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
         if (blk < tile) continue;
 #pragma unroll
         for (int k = 0; k < KS; ++k) sc[i] = mfma16(Rows<D>::along(score_rows, blk * 16, k, lane), kf[k], sc[i]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sc[i][e] = d + e >= 0 ? sc[i][e] * (p.scale * power(log2, d + e)) : 0.f;
+        decays.apply(sc[i], blk - tile, [&](int e) { return g * 4 + e >= r; });
       }
       const Scores pf(sc);
 #pragma unroll
       for (int n = 0; n < NB; ++n) acc[n] = pf.times(Rows<D>::columns_stored(sum_rows, n, pr * 32, lane), acc[n]);
     }
     if (c > 0 || (!staged && p.s_out)) {
-      if (h == 0) s.decay(rows == kChunk ? whole : decay_of(p.log_decay[j], rows));
+      if (h == 0) s.decay(rows == kChunk ? whole : Decay{power(log2, rows), 0.f});
       s.template add<SPLIT, false>(qt, dt, w, rows, wave, lane);
       some = true;
       if (h == G - 1 && c > 0) largest[wave] = s.largest(wave);
@@ -713,25 +758,26 @@ __global__ __launch_bounds__(64 * kLinWaves, 4) void linear_keys_kernel(const Li
 // ------------------------------------------------------------------------------------------
 // Host side
 // ------------------------------------------------------------------------------------------
-constexpr int kLinearBlocks = 512;   // workgroups that fill the chip: two on each compute unit
+// workgroups that fill the chip: one on each compute unit for states of 128 x 128, else two
+inline int linear_blocks(int64_t dh) { return dh == 128 ? 256 : 512; }
 
 // Segments of a sequence, a whole number of chunks each, and the workgroups that share a segment's query heads: as many segments as
-// make kLinearBlocks workgroups, of two chunks at the least.
+// make linear_blocks workgroups, of two chunks at the least.
 struct LinearPlan { int chunks, seg_chunks, nseg; };
-static LinearPlan linear_plan(int64_t pairs, int64_t S) {
+static LinearPlan linear_plan(int64_t pairs, int64_t S, int64_t dh) {
   LinearPlan p;
   p.chunks = (int)((S + kChunk - 1) / kChunk);
-  int64_t n = (kLinearBlocks + pairs - 1) / pairs;
+  int64_t n = (linear_blocks(dh) + pairs - 1) / pairs;
   if (n > p.chunks / 2) n = p.chunks / 2;
   if (n < 1) n = 1;
   p.seg_chunks = (int)((p.chunks + n - 1) / n);
   p.nseg = (p.chunks + p.seg_chunks - 1) / p.seg_chunks;
   return p;
 }
-// room for the states of all segments: below twice kLinearBlocks of them, and a size that does not fall as the call grows
+// room for the states of all segments: below twice linear_blocks of them, and a size that does not fall as the call grows
 static size_t segment_bytes(int64_t pairs, int64_t S, int64_t dh) {
-  const int64_t chunks = (S + kChunk - 1) / kChunk;
-  const int64_t n = pairs < 2 * kLinearBlocks && pairs * chunks < 2 * kLinearBlocks ? pairs * chunks : 2 * kLinearBlocks;
+  const int64_t chunks = (S + kChunk - 1) / kChunk, most = 2 * linear_blocks(dh);
+  const int64_t n = pairs < most && pairs * chunks < most ? pairs * chunks : most;
   return (size_t)(n * dh * dh) * sizeof(float);
 }
 size_t linear_attention_fwd_workspace(int64_t B, int64_t S, int64_t Hq, int64_t Hkv, int64_t dh) { return segment_bytes(B * Hkv, S, dh); }
@@ -751,7 +797,7 @@ static int run_out(const LinearArgs& a, int64_t pairs, hipStream_t st) {
   constexpr size_t lds = (2 * kChunk + D) * D * 2 + kLinWaves * sizeof(float);
   static std::atomic<unsigned long long> done2, done3;
   const int G = a.Hq / a.Hkv;
-  int parts = (int)((kLinearBlocks + pairs * a.nseg - 1) / (pairs * a.nseg));
+  int parts = (int)((linear_blocks(D) + pairs * a.nseg - 1) / (pairs * a.nseg));
   parts = parts < G ? parts : G;
   const int staged = a.nseg > 1 || (parts > 1 && a.s_out);
   if (staged)
@@ -784,7 +830,7 @@ static int run_keys(const LinearArgs& a, int64_t pairs, hipStream_t st) {
 }
 
 static LinearArgs linear_args(const LinearCall& c, void* workspace) {
-  const LinearPlan plan = linear_plan(c.B * c.Hkv, c.S);
+  const LinearPlan plan = linear_plan(c.B * c.Hkv, c.S, c.dh);
   LinearArgs a{};
   a.q = (const bf16_t*)c.q; a.k = (const bf16_t*)c.k; a.v = (const bf16_t*)c.v;
   a.log_decay = c.log_decay; a.lengths = c.lengths; a.seg = (float*)workspace;
