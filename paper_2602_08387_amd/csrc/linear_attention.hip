@@ -107,28 +107,24 @@ struct Rows {
   }
 };
 
-// A 64-row tile on its way from memory to LDS, through registers: 16 bytes a thread and piece.
+// A 64-row tile from memory to LDS without a detour through registers: each load of a wave fills 1 KB, lane after lane, so the pieces are
+// picked in memory in the order in which they lie in LDS.  Done when vmcnt is 0 and a barrier passed.
 template <int D>
-struct Staged {
-  static constexpr int TOTAL = kChunk * Rows<D>::PIECES, THREADS = 64 * kLinWaves, N = (TOTAL + THREADS - 1) / THREADS;
-  bf16x8 v[N];
-  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t rs, int64_t ld) {
-    const int thread = here((int)threadIdx.x);
+__device__ __forceinline__ void tile_to_lds(__amdgpu_buffer_rsrc_t rs, char* t, int64_t ld, int wave, int lane) {
+  constexpr int PIECES = Rows<D>::PIECES, RPI = 64 / PIECES, N = kChunk / RPI;
+  lane = here(lane);
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int idx = i * THREADS + thread;
-      if (TOTAL % THREADS == 0 || idx < TOTAL) v[i] = load8(rs, (uint32_t)(idx / Rows<D>::PIECES * (int)ld * 2 + idx % Rows<D>::PIECES * 16));
-    }
+  for (int i = 0; i < (N + kLinWaves - 1) / kLinWaves; ++i) {
+    const int j = i * kLinWaves + wave, r = j * RPI + lane / PIECES;
+    if (N % kLinWaves == 0 || j < N)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (LDS_PTR(void))(t + j * 1024), 16,
+                                               (uint32_t)(r * (int)ld * 2 + (((lane % PIECES) ^ Rows<D>::swz(r)) << 4)), 0, 0, 0);
   }
-  __device__ __forceinline__ void store(char* t) const {
-    const int thread = here((int)threadIdx.x);
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int idx = i * THREADS + thread;
-      if (TOTAL % THREADS == 0 || idx < TOTAL) *reinterpret_cast<bf16x8*>(t + Rows<D>::at(idx / Rows<D>::PIECES, idx % Rows<D>::PIECES)) = v[i];
-    }
-  }
-};
+}
+__device__ __forceinline__ void loads_done() {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+}
 
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
@@ -173,20 +169,14 @@ struct ScaledRow {
 
 __device__ __forceinline__ float uniform(float x) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x))); }
 
-// Weights of a chunk's tokens on their way into the state after the chunk (TO_END: lambda^(rows-1-t)) or into the gradient of the state
-// before it (mult lambda^(t+1)): those of the lane's tokens 32 p + its slots, of a full chunk.
-struct Weights {
-  float w[2][8], log2;
-  template <bool TO_END>
-  __device__ __forceinline__ void init(float log2_, float mult, int lane) {
-    log2 = log2_;
-#pragma unroll
-    for (int p = 0; p < 2; ++p)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) w[p][e] = mult * power(log2, TO_END ? 63 - token(p, e, lane) : token(p, e, lane) + 1);
-  }
-  static __device__ __forceinline__ int token(int p, int e, int lane) { return p * 32 + (e >> 2) * 16 + ((lane >> 4) << 2) + (e & 3); }
-};
+// Weights of a chunk's tokens, in LDS: on their way into the state after the chunk's `rows` tokens, lambda^(rows-1-t), and into the gradient of the
+// state before it, mult lambda^(t+1).  (Sixteen registers would hold a lane's, and are not there.)
+__device__ __forceinline__ void weights_to_end(float* w, float log2, int rows) {
+  if (threadIdx.x < kChunk) w[threadIdx.x] = power(log2, max(rows - 1 - (int)threadIdx.x, 0));
+}
+__device__ __forceinline__ void weights_from_start(float* w, float log2, float mult) {
+  if (threadIdx.x < kChunk) w[threadIdx.x] = mult * power(log2, (int)threadIdx.x + 1);
+}
 
 // A state [D along keys][D along values] over the waves: wave -> RB x CB blocks of 16 x 16 (of 32 x 32 elements four waves hold one each).  In
 // memory between the kernels it lies as the accumulators do: [wave][block][lane] f32x4.
@@ -282,27 +272,21 @@ struct State {
         *reinterpret_cast<f16x4*>(t + Rows<D>::at(p, r >> 3) + ((r & 7) << 1)) = v;
       }
   }
-  // += sum over the tile's 64 tokens of (w x)^T y, x and y in LDS; w x as the sum of SPLIT bf16.  rows: the tokens there are (the rest
-  // of the tile is zeros), which the weights to the end depend on.
-  template <int SPLIT, bool TO_END>
-  __device__ __forceinline__ void add(const char* x, const char* y, const Weights& w, int rows, int wave, int lane) {
+  // += sum over the tile's 64 tokens of (w x)^T y, all in LDS; w x as the sum of SPLIT bf16
+  template <int SPLIT>
+  __device__ __forceinline__ void add(const char* x, const char* y, const float* w, int wave, int lane) {
     if (!holds(wave)) return;
     lane = here(lane);
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
       bf16x8 part[RB][SPLIT];
+      const f32x4 w0 = *reinterpret_cast<const f32x4*>(w + p * 32 + ((lane >> 4) << 2)), w1 = *reinterpret_cast<const f32x4*>(w + p * 32 + 16 + ((lane >> 4) << 2));
 #pragma unroll
       for (int i = 0; i < RB; ++i) {
         float f[8];
         unpack8(Rows<D>::columns(x, row_block(wave) + i, p * 32, lane), f);
-        if (!TO_END || rows == kChunk) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) f[e] *= w.w[p][e];
-        } else {
-          const float log2 = here(w.log2);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) f[e] *= power(log2, max(rows - 1 - Weights::token(p, e, lane), 0));
-        }
+        for (int e = 0; e < 8; ++e) f[e] *= e < 4 ? w0[e] : w1[e - 4];
 #pragma unroll
         for (int k = 0; k < SPLIT; ++k) {
           part[i][k] = pack8(f);
@@ -400,6 +384,7 @@ template <int D, bool REVERSE>
 __global__ __launch_bounds__(64 * kLinWaves, 4) void linear_segment_kernel(const LinearArgs p) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   char *xt = smem, *yt = smem + kChunk * D * 2;
+  float* w = reinterpret_cast<float*>(smem + 2 * kChunk * D * 2);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int pair = blockIdx.x / p.nseg, sg = blockIdx.x % p.nseg, b = pair / p.Hkv, j = pair % p.Hkv;
   const int len = row_length(p, b), t0 = sg * p.seg_chunks * kChunk;
@@ -417,26 +402,18 @@ __global__ __launch_bounds__(64 * kLinWaves, 4) void linear_segment_kernel(const
   const int64_t first = ((int64_t)b * p.S + t0) * ld + (int64_t)j * G * D;
   const float log2 = log2_decay(p.log_decay[j]);
   const Decay whole = decay_of(p.log_decay[j], kChunk);
+  if (REVERSE) weights_from_start(w, log2, p.scale);
   // chunks in the order in which the state passes through them
-  Staged<D> xs, ys;
-  auto fetch = [&](int it) {
+  for (int it = 0; it < chunks * G; ++it) {
     const int c = REVERSE ? chunks - 1 - it / G : it, rows = min(m - c * kChunk, kChunk);
     const int64_t at = first + (int64_t)c * kChunk * ld + (int64_t)(REVERSE ? it % G : 0) * D;
-    xs.load(rows_rsrc<D>(x + at, ld, rows), ld);
-    ys.load(rows_rsrc<D>(y + at, ld, rows), ld);
-  };
-  fetch(0);
-  Weights w;
-  w.init<!REVERSE>(log2, REVERSE ? p.scale : 1.f, lane);
-  for (int it = 0; it < chunks * G; ++it) {
     __syncthreads();
-    xs.store(xt);
-    ys.store(yt);
-    __syncthreads();
-    if (it + 1 < chunks * G) fetch(it + 1);
-    const int rows = REVERSE ? kChunk : min(m - it * kChunk, kChunk);
-    if (it > 0 && it % G == 0) s.decay(rows == kChunk ? whole : Decay{power(log2, rows), 0.f});
-    s.template add<3, !REVERSE>(xt, yt, w, rows, wave, lane);
+    tile_to_lds<D>(rows_rsrc<D>(x + at, ld, rows), xt, ld, wave, lane);
+    tile_to_lds<D>(rows_rsrc<D>(y + at, ld, rows), yt, ld, wave, lane);
+    if (!REVERSE && (it == 0 || rows < kChunk)) weights_to_end(w, log2, rows);
+    loads_done();
+    if (it > 0 && it % G == 0) s.decay(REVERSE || rows == kChunk ? whole : Decay{power(log2, rows), 0.f});
+    s.template add<3>(xt, yt, w, wave, lane);
   }
   s.store(out, wave, lane);
 }
@@ -526,11 +503,11 @@ __device__ __forceinline__ void out_tile(f32x4 (&o)[NB], const bf16x8 (&qf)[D / 
 }
 
 template <int D, int SPLIT>
-__global__ __launch_bounds__(64 * kLinWaves, D == 128 ? 2 : 4) void linear_out_kernel(const LinearArgs p, int pairs, int parts, int staged) {
+__global__ __launch_bounds__(64 * kLinWaves, 4) void linear_out_kernel(const LinearArgs p, int pairs, int parts, int staged) {
   constexpr int NB = D / 16, KS = D / 32;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   char *kt = smem, *vt = smem + kChunk * D * 2, *st = smem + 2 * kChunk * D * 2;
-  float* largest = reinterpret_cast<float*>(st + D * D * 2);
+  float *largest = reinterpret_cast<float*>(st + D * D * 2), *w = largest + kLinWaves;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
   const int id = blockIdx.x % (pairs * p.nseg), part = blockIdx.x / (pairs * p.nseg);
   const int pair = id / p.nseg, sg = id % p.nseg, b = pair / p.Hkv, j = pair % p.Hkv, G = p.Hq / p.Hkv;
@@ -541,13 +518,6 @@ __global__ __launch_bounds__(64 * kLinWaves, D == 128 ? 2 : 4) void linear_out_k
   const int64_t kv0 = tok0 * ldk + (int64_t)j * D, q0 = tok0 * ldq + (int64_t)j * G * D;
   float* s_out = staged || part ? nullptr : p.s_out;
 
-  Staged<D> ks, vs;
-  auto fetch = [&](int c) {
-    const int64_t at = kv0 + (int64_t)c * kChunk * ldk;
-    ks.load(rows_rsrc<D>(p.k + at, ldk, min(m - c * kChunk, kChunk)), ldk);
-    vs.load(rows_rsrc<D>(p.v + at, ldk, min(m - c * kChunk, kChunk)), ldk);
-  };
-  if (chunks > 0) fetch(0);
   State<D> s;
   if (staged) s.load(p.seg + (int64_t)id * D * D, wave, lane);
   else if (p.s_in) s.load_matrix(p.s_in + (int64_t)pair * D * D, p.flip, wave, lane);
@@ -557,23 +527,22 @@ __global__ __launch_bounds__(64 * kLinWaves, D == 128 ? 2 : 4) void linear_out_k
   if (some) largest[wave] = s.largest(wave);
   const float log2 = uniform(log2_decay(p.log_decay[j]));
   const Decay whole = decay_of(p.log_decay[j], kChunk);
-  Weights w;
-  w.init<true>(log2, 1.f, lane);
   const Decays decays(log2, 1.f, r - g * 4, -1);
 
   for (int c = 0; c < chunks; ++c) {
     const int rows = min(m - c * kChunk, kChunk), rows_out = min(rows_all - c * kChunk, kChunk);
     const bool more = c + 1 < chunks;
+    const int64_t kc = kv0 + (int64_t)c * kChunk * ldk;
     __syncthreads();
+    tile_to_lds<D>(rows_rsrc<D>(p.k + kc, ldk, rows), kt, ldk, wave, lane);
+    tile_to_lds<D>(rows_rsrc<D>(p.v + kc, ldk, rows), vt, ldk, wave, lane);
+    if (c == 0 || rows < kChunk) weights_to_end(w, log2, rows);
     if (some) {
       const Scale sc = state_scale(largest);
       down = sc.down;
       s.to_lds(st, sc.up, wave, lane);
     }
-    ks.store(kt);
-    vs.store(vt);
-    __syncthreads();
-    if (more) fetch(c + 1);
+    loads_done();
     const int64_t qc = q0 + (int64_t)c * kChunk * ldq;
     for (int h = h0; h < h1; h += 2) {
       const bool both = h + 1 < h1;
@@ -607,7 +576,7 @@ __global__ __launch_bounds__(64 * kLinWaves, D == 128 ? 2 : 4) void linear_out_k
     }
     if (more || s_out) {
       s.decay(rows == kChunk ? whole : Decay{power(log2, rows), 0.f});
-      s.template add<SPLIT, true>(kt, vt, w, rows, wave, lane);
+      s.template add<SPLIT>(kt, vt, w, wave, lane);
       some = true;
       if (more) largest[wave] = s.largest(wave);
     }
@@ -628,11 +597,11 @@ __global__ __launch_bounds__(64 * kLinWaves, D == 128 ? 2 : 4) void linear_out_k
 // other four dk, which is the same with q and do, k and v in each other's place and E transposed.
 // ------------------------------------------------------------------------------------------
 template <int D, int SPLIT>
-__global__ __launch_bounds__(64 * kLinWaves, D == 128 ? 2 : 4) void linear_keys_kernel(const LinearArgs p, int staged) {
+__global__ __launch_bounds__(64 * kLinWaves, 4) void linear_keys_kernel(const LinearArgs p, int staged) {
   constexpr int NB = D / 16, KS = D / 32;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   char *qt = smem, *dt = smem + kChunk * D * 2, *et = smem + 2 * kChunk * D * 2;
-  float* largest = reinterpret_cast<float*>(et + D * D * 2);
+  float *largest = reinterpret_cast<float*>(et + D * D * 2), *w = largest + kLinWaves;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
   const int pair = blockIdx.x / p.nseg, sg = blockIdx.x % p.nseg, b = pair / p.Hkv, j = pair % p.Hkv, G = p.Hq / p.Hkv;
   const int len = row_length(p, b), t0 = sg * p.seg_chunks * kChunk;
@@ -646,14 +615,6 @@ __global__ __launch_bounds__(64 * kLinWaves, D == 128 ? 2 : 4) void linear_keys_
   bf16_t* out = (dk_role ? p.dk : p.dv) + kv0;
   const char *score_rows = dk_role ? dt : qt, *sum_rows = dk_role ? qt : dt;
 
-  Staged<D> qs, ds;
-  auto fetch = [&](int it) {
-    const int c = chunks - 1 - it / G, rows = min(m - c * kChunk, kChunk);
-    const int64_t from = q0 + (int64_t)c * kChunk * ldq + (int64_t)(it % G) * D;
-    qs.load(rows_rsrc<D>(p.q + from, ldq, rows), ldq);
-    ds.load(rows_rsrc<D>(p.d_o + from, ldq, rows), ldq);
-  };
-  if (chunks > 0) fetch(0);
   State<D> s;
   if (staged) s.load(p.seg + (int64_t)blockIdx.x * D * D, wave, lane);
   else if (p.s_in) s.load_matrix(p.s_in + (int64_t)pair * D * D, 0, wave, lane);
@@ -664,29 +625,28 @@ __global__ __launch_bounds__(64 * kLinWaves, D == 128 ? 2 : 4) void linear_keys_
   if (some) largest[wave] = s.largest(wave);
   const float log2 = uniform(log2_decay(p.log_decay[j]));
   const Decay whole = decay_of(p.log_decay[j], kChunk);
-  Weights w;
-  w.init<false>(log2, p.scale, lane);
+  weights_from_start(w, log2, p.scale);
   const Decays decays(log2, p.scale, g * 4 - r, 1);
   f32x4 acc[NB];
   bf16x8 kf[KS];
   for (int it = 0; it < chunks * G; ++it) {
     const int c = chunks - 1 - it / G, h = it % G, rows = min(m - c * kChunk, kChunk);
     const int64_t kc = (int64_t)c * kChunk * ldk;
+    const int64_t from = q0 + (int64_t)c * kChunk * ldq + (int64_t)h * D;
+    __syncthreads();
+    tile_to_lds<D>(rows_rsrc<D>(p.q + from, ldq, rows), qt, ldq, wave, lane);
+    tile_to_lds<D>(rows_rsrc<D>(p.d_o + from, ldq, rows), dt, ldq, wave, lane);
     if (h == 0) {
       const __amdgpu_buffer_rsrc_t rk = rows_rsrc<D>(own + kc, ldk, rows);
 #pragma unroll
       for (int k = 0; k < KS; ++k) kf[k] = load8(rk, at + k * 64);
     }
-    __syncthreads();
     if (h == 0 && some) {
       const Scale sc = state_scale(largest);
       down = sc.down;
       s.to_lds(et, sc.up, wave, lane);
     }
-    qs.store(qt);
-    ds.store(dt);
-    __syncthreads();
-    if (it + 1 < chunks * G) fetch(it + 1);
+    loads_done();
     if (h == 0) {
 #pragma unroll
       for (int n = 0; n < NB; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -731,7 +691,7 @@ __global__ __launch_bounds__(64 * kLinWaves, D == 128 ? 2 : 4) void linear_keys_
     }
     if (c > 0 || (!staged && p.s_out)) {
       if (h == 0) s.decay(rows == kChunk ? whole : Decay{power(log2, rows), 0.f});
-      s.template add<SPLIT, false>(qt, dt, w, rows, wave, lane);
+      s.template add<SPLIT>(qt, dt, w, wave, lane);
       some = true;
       if (h == G - 1 && c > 0) largest[wave] = s.largest(wave);
     }
@@ -758,8 +718,8 @@ __global__ __launch_bounds__(64 * kLinWaves, D == 128 ? 2 : 4) void linear_keys_
 // ------------------------------------------------------------------------------------------
 // Host side
 // ------------------------------------------------------------------------------------------
-// workgroups that fill the chip: one on each compute unit for states of 128 x 128, else two
-inline int linear_blocks(int64_t dh) { return dh == 128 ? 256 : 512; }
+// workgroups that fill the chip: two on each compute unit
+inline int linear_blocks(int64_t dh) { return 512; }
 
 // Segments of a sequence, a whole number of chunks each, and the workgroups that share a segment's query heads: as many segments as
 // make linear_blocks workgroups, of two chunks at the least.
@@ -785,7 +745,7 @@ size_t linear_attention_bwd_workspace(int64_t B, int64_t S, int64_t Hq, int64_t 
 
 template <int D, bool REVERSE>
 static int run_states(const LinearArgs& a, int64_t pairs, hipStream_t st) {
-  hipLaunchKernelGGL((linear_segment_kernel<D, REVERSE>), dim3((unsigned)(pairs * a.nseg)), dim3(64 * kLinWaves), 2 * kChunk * D * 2, st, a);
+  hipLaunchKernelGGL((linear_segment_kernel<D, REVERSE>), dim3((unsigned)(pairs * a.nseg)), dim3(64 * kLinWaves), 2 * kChunk * D * 2 + kChunk * sizeof(float), st, a);
   if (int rc = check_launch("linear attention (segments)")) return rc;
   hipLaunchKernelGGL((linear_scan_kernel<D, REVERSE>), dim3((unsigned)(pairs * (D * D / 1024))), dim3(256), 0, st, a);
   return check_launch("linear attention (scan)");
@@ -794,7 +754,7 @@ static int run_states(const LinearArgs& a, int64_t pairs, hipStream_t st) {
 // o from (q, k, v), or dq from (d_o, v, k) with the state transposed
 template <int D>
 static int run_out(const LinearArgs& a, int64_t pairs, hipStream_t st) {
-  constexpr size_t lds = (2 * kChunk + D) * D * 2 + kLinWaves * sizeof(float);
+  constexpr size_t lds = (2 * kChunk + D) * D * 2 + (kLinWaves + kChunk) * sizeof(float);
   static std::atomic<unsigned long long> done2, done3;
   const int G = a.Hq / a.Hkv;
   int parts = (int)((linear_blocks(D) + pairs * a.nseg - 1) / (pairs * a.nseg));
@@ -815,7 +775,7 @@ static int run_out(const LinearArgs& a, int64_t pairs, hipStream_t st) {
 
 template <int D>
 static int run_keys(const LinearArgs& a, int64_t pairs, hipStream_t st) {
-  constexpr size_t lds = (2 * kChunk + D) * D * 2 + kLinWaves * sizeof(float);
+  constexpr size_t lds = (2 * kChunk + D) * D * 2 + (kLinWaves + kChunk) * sizeof(float);
   static std::atomic<unsigned long long> done2, done3;
   const dim3 grid((unsigned)(pairs * a.nseg));
   if (a.nseg > 1) {
