@@ -121,6 +121,26 @@ __device__ __forceinline__ void tile_to_lds(__amdgpu_buffer_rsrc_t rs, char* t, 
                                                (uint32_t)(r * (int)ld * 2 + (((lane % PIECES) ^ Rows<D>::swz(r)) << 4)), 0, 0, 0);
   }
 }
+// The same through registers, for a kernel that has them: asked for a tile ahead, written to LDS when the one before is done with.
+template <int D>
+struct Staged {
+  static constexpr int TOTAL = kChunk * Rows<D>::PIECES, THREADS = 64 * kLinWaves, N = (TOTAL + THREADS - 1) / THREADS;
+  bf16x8 v[N];
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t rs, int64_t ld) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int idx = i * THREADS + (int)threadIdx.x;
+      if (TOTAL % THREADS == 0 || idx < TOTAL) v[i] = load8(rs, (uint32_t)(idx / Rows<D>::PIECES * (int)ld * 2 + idx % Rows<D>::PIECES * 16));
+    }
+  }
+  __device__ __forceinline__ void store(char* t) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int idx = i * THREADS + (int)threadIdx.x;
+      if (TOTAL % THREADS == 0 || idx < TOTAL) *reinterpret_cast<bf16x8*>(t + Rows<D>::at(idx / Rows<D>::PIECES, idx % Rows<D>::PIECES)) = v[i];
+    }
+  }
+};
 __device__ __forceinline__ void loads_done() {
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
@@ -170,12 +190,12 @@ struct ScaledRow {
 __device__ __forceinline__ float uniform(float x) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x))); }
 
 // Weights of a chunk's tokens, in LDS: on their way into the state after the chunk's `rows` tokens, lambda^(rows-1-t), and into the gradient of the
-// state before it, mult lambda^(t+1).  (Sixteen registers would hold a lane's, and are not there.)
+// state `before` tokens before the chunk, mult lambda^(before+t+1).  (Sixteen registers would hold a lane's, and are not there.)
 __device__ __forceinline__ void weights_to_end(float* w, float log2, int rows) {
   if (threadIdx.x < kChunk) w[threadIdx.x] = power(log2, max(rows - 1 - (int)threadIdx.x, 0));
 }
-__device__ __forceinline__ void weights_from_start(float* w, float log2, float mult) {
-  if (threadIdx.x < kChunk) w[threadIdx.x] = mult * power(log2, (int)threadIdx.x + 1);
+__device__ __forceinline__ void weights_from_start(float* w, float log2, float mult, int before) {
+  if (threadIdx.x < kChunk) w[threadIdx.x] = mult * power(log2, before + (int)threadIdx.x + 1);
 }
 
 // A state [D along keys][D along values] over the waves: wave -> RB x CB blocks of 16 x 16 (of 32 x 32 elements four waves hold one each).  In
@@ -362,7 +382,7 @@ struct LinearArgs {
   bf16_t *o, *dk, *dv;
   const float* log_decay;
   const int64_t* lengths;
-  float* seg;              // [pair][segment] states between the kernels
+  float* seg;              // [pair][segment] states (gradients) between the kernels; null: there is one segment, which takes s_in itself
   const float* s_in;
   float* s_out;
   int S, Hq, Hkv, flip;    // flip: s_in is read transposed
@@ -376,13 +396,13 @@ __device__ __forceinline__ int row_length(const LinearArgs& p, int b) {
   return (int)(n < 0 ? 0 : n > p.S ? p.S : n);
 }
 __device__ __forceinline__ float log2_decay(float g) { return (float)(decay_log(g) * 1.4426950408889634); }
+
 // ------------------------------------------------------------------------------------------
 // What a segment of m tokens adds to the state that passes through it: sum_t lambda^(m-1-t) k_t v_t^T, from k and v;
-// REVERSE: sum over t and the group's heads of scale lambda^(t+1) q_t do_t^T, from q and d_o.
+// GRADIENT: to the state's gradient, sum over t and the group's heads of scale lambda^(t+1) q_t do_t^T, from q and d_o.
 // ------------------------------------------------------------------------------------------
-template <int D, bool REVERSE>
-__global__ __launch_bounds__(64 * kLinWaves, 4) void linear_segment_kernel(const LinearArgs p) {
-  extern __shared__ __attribute__((aligned(1024))) char smem[];
+template <int D, bool GRADIENT>
+__device__ __forceinline__ void segment_sum(const LinearArgs& p, char* smem) {
   char *xt = smem, *yt = smem + kChunk * D * 2;
   float* w = reinterpret_cast<float*>(smem + 2 * kChunk * D * 2);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -396,34 +416,51 @@ __global__ __launch_bounds__(64 * kLinWaves, 4) void linear_segment_kernel(const
     s.store(out, wave, lane);
     return;
   }
-  const int G = REVERSE ? p.Hq / p.Hkv : 1, chunks = (m + kChunk - 1) / kChunk;
-  const int64_t ld = (int64_t)(REVERSE ? p.Hq : p.Hkv) * D;
-  const bf16_t *x = REVERSE ? p.q : p.k, *y = REVERSE ? p.d_o : p.v;
+  const int G = GRADIENT ? p.Hq / p.Hkv : 1, items = (m + kChunk - 1) / kChunk * G;
+  const int64_t ld = (int64_t)(GRADIENT ? p.Hq : p.Hkv) * D;
+  const bf16_t *x = GRADIENT ? p.q : p.k, *y = GRADIENT ? p.d_o : p.v;
   const int64_t first = ((int64_t)b * p.S + t0) * ld + (int64_t)j * G * D;
   const float log2 = log2_decay(p.log_decay[j]);
   const Decay whole = decay_of(p.log_decay[j], kChunk);
-  if (REVERSE) weights_from_start(w, log2, p.scale);
-  // chunks in the order in which the state passes through them
-  for (int it = 0; it < chunks * G; ++it) {
-    const int c = REVERSE ? chunks - 1 - it / G : it, rows = min(m - c * kChunk, kChunk);
-    const int64_t at = first + (int64_t)c * kChunk * ld + (int64_t)(REVERSE ? it % G : 0) * D;
+  Staged<D> xs, ys;
+  auto fetch = [&](int it) {
+    const int rows = min(m - it / G * kChunk, kChunk);
+    const int64_t at = first + (int64_t)(it / G) * kChunk * ld + (int64_t)(it % G) * D;
+    xs.load(rows_rsrc<D>(x + at, ld, rows), ld);
+    ys.load(rows_rsrc<D>(y + at, ld, rows), ld);
+  };
+  fetch(0);
+  for (int it = 0; it < items; ++it) {
+    const int c = it / G, rows = min(m - c * kChunk, kChunk);
     __syncthreads();
-    tile_to_lds<D>(rows_rsrc<D>(x + at, ld, rows), xt, ld, wave, lane);
-    tile_to_lds<D>(rows_rsrc<D>(y + at, ld, rows), yt, ld, wave, lane);
-    if (!REVERSE && (it == 0 || rows < kChunk)) weights_to_end(w, log2, rows);
-    loads_done();
-    if (it > 0 && it % G == 0) s.decay(REVERSE || rows == kChunk ? whole : Decay{power(log2, rows), 0.f});
+    xs.store(xt);
+    ys.store(yt);
+    if (GRADIENT) {
+      if (it % G == 0) weights_from_start(w, log2, p.scale, c * kChunk);
+    } else if (c == 0 || rows < kChunk) {
+      weights_to_end(w, log2, rows);
+    }
+    __syncthreads();
+    if (it + 1 < items) fetch(it + 1);
+    if (!GRADIENT && c > 0) s.decay(rows == kChunk ? whole : Decay{power(log2, rows), 0.f});
     s.template add<3>(xt, yt, w, wave, lane);
   }
   s.store(out, wave, lane);
 }
+// y 0: the states, of `a`; 1: their gradients, of `g`
+template <int D>
+__global__ __launch_bounds__(64 * kLinWaves, 4) void linear_segment_kernel(const LinearArgs a, const LinearArgs g) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  if (blockIdx.y == 0) segment_sum<D, false>(a, smem);
+  else segment_sum<D, true>(g, smem);
+}
 
 // ------------------------------------------------------------------------------------------
-// From segment to segment: what each adds is replaced by the state it begins with; REVERSE: by the gradient of the state it ends
+// From segment to segment: what each adds is replaced by the state it begins with; GRADIENT: by the gradient of the state it ends
 // with.  A thread holds four elements of a state in fp64 (a decay of many tokens has no second fp32), eight segments ahead in flight.
 // ------------------------------------------------------------------------------------------
-template <int D, bool REVERSE>
-__global__ __launch_bounds__(256) void linear_scan_kernel(const LinearArgs p) {
+template <int D, bool GRADIENT>
+__device__ __forceinline__ void segment_scan(const LinearArgs& p) {
   using St = State<D>;
   constexpr int PARTS = D * D / 1024, AHEAD = 8;
   const int pair = blockIdx.x / PARTS, f = blockIdx.x % PARTS * 256 + threadIdx.x, b = pair / p.Hkv, j = pair % p.Hkv;
@@ -440,12 +477,12 @@ __global__ __launch_bounds__(256) void linear_scan_kernel(const LinearArgs p) {
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) {
       const int n = n0 + i;
-      if (n < p.nseg) u[i] = at[(int64_t)(REVERSE ? p.nseg - 1 - n : n) * (D * D / 4)];
+      if (n < p.nseg) u[i] = at[(int64_t)(GRADIENT ? p.nseg - 1 - n : n) * (D * D / 4)];
     }
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) {
       if (n0 + i >= p.nseg) break;
-      const int n = REVERSE ? p.nseg - 1 - n0 - i : n0 + i, m = min(max(len - n * seg_tokens, 0), seg_tokens);
+      const int n = GRADIENT ? p.nseg - 1 - n0 - i : n0 + i, m = min(max(len - n * seg_tokens, 0), seg_tokens);
       at[(int64_t)n * (D * D / 4)] = f32x4{(float)s[0], (float)s[1], (float)s[2], (float)s[3]};
       if (m == 0) continue;
       const double l = m == seg_tokens ? whole : exp(log * m);
@@ -456,6 +493,11 @@ __global__ __launch_bounds__(256) void linear_scan_kernel(const LinearArgs p) {
   if (p.s_out)
 #pragma unroll
     for (int e = 0; e < 4; ++e) p.s_out[(int64_t)pair * D * D + St::element(row + e, col, 0)] = (float)s[e];
+}
+template <int D>
+__global__ __launch_bounds__(256) void linear_scan_kernel(const LinearArgs a, const LinearArgs g) {
+  if (blockIdx.y == 0) segment_scan<D, false>(a);
+  else segment_scan<D, true>(g);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -503,23 +545,21 @@ __device__ __forceinline__ void out_tile(f32x4 (&o)[NB], const bf16x8 (&qf)[D / 
 }
 
 template <int D, int SPLIT>
-__global__ __launch_bounds__(64 * kLinWaves, 4) void linear_out_kernel(const LinearArgs p, int pairs, int parts, int staged) {
+__device__ __forceinline__ void segment_out(const LinearArgs& p, int id, int part, int parts, char* smem) {
   constexpr int NB = D / 16, KS = D / 32;
-  extern __shared__ __attribute__((aligned(1024))) char smem[];
   char *kt = smem, *vt = smem + kChunk * D * 2, *st = smem + 2 * kChunk * D * 2;
   float *largest = reinterpret_cast<float*>(st + D * D * 2), *w = largest + kLinWaves;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
-  const int id = blockIdx.x % (pairs * p.nseg), part = blockIdx.x / (pairs * p.nseg);
   const int pair = id / p.nseg, sg = id % p.nseg, b = pair / p.Hkv, j = pair % p.Hkv, G = p.Hq / p.Hkv;
   const int per = (G + parts - 1) / parts, h0 = part * per, h1 = min(G, h0 + per);
   const int len = row_length(p, b), t0 = sg * p.seg_chunks * kChunk;
   const int rows_all = min(p.S - t0, p.seg_chunks * kChunk), m = max(min(len - t0, rows_all), 0), chunks = (m + kChunk - 1) / kChunk;
   const int64_t ldq = (int64_t)p.Hq * D, ldk = (int64_t)p.Hkv * D, tok0 = (int64_t)b * p.S + t0;
   const int64_t kv0 = tok0 * ldk + (int64_t)j * D, q0 = tok0 * ldq + (int64_t)j * G * D;
-  float* s_out = staged || part ? nullptr : p.s_out;
+  float* s_out = p.seg || part ? nullptr : p.s_out;
 
   State<D> s;
-  if (staged) s.load(p.seg + (int64_t)id * D * D, wave, lane);
+  if (p.seg) s.load(p.seg + (int64_t)id * D * D, wave, lane);
   else if (p.s_in) s.load_matrix(p.s_in + (int64_t)pair * D * D, p.flip, wave, lane);
   else s.clear();
   bool some = p.s_in != nullptr || sg > 0;   // a state that is not zero
@@ -591,19 +631,25 @@ __global__ __launch_bounds__(64 * kLinWaves, 4) void linear_out_kernel(const Lin
   if (s_out) s.store_matrix(s_out + (int64_t)pair * D * D, wave, lane);
 }
 
+// workgroup -> segment, and part of the group's heads
+template <int D, int SPLIT>
+__global__ __launch_bounds__(64 * kLinWaves, 4) void linear_out_kernel(const LinearArgs p, int segments, int parts) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  segment_out<D, SPLIT>(p, blockIdx.x % segments, blockIdx.x / segments, parts, smem);
+}
+
 // ------------------------------------------------------------------------------------------
 // dk and dv of a segment: its chunks from the last to the first, the gradient E of the state that a chunk ends with in the accumulators
 // and, as an operand along either side, in LDS.  The group's heads pass by, their q and do in LDS; four waves form dv of 16 keys each, the
 // other four dk, which is the same with q and do, k and v in each other's place and E transposed.
 // ------------------------------------------------------------------------------------------
 template <int D, int SPLIT>
-__global__ __launch_bounds__(64 * kLinWaves, 4) void linear_keys_kernel(const LinearArgs p, int staged) {
+__device__ __forceinline__ void segment_keys(const LinearArgs& p, int id, char* smem) {
   constexpr int NB = D / 16, KS = D / 32;
-  extern __shared__ __attribute__((aligned(1024))) char smem[];
   char *qt = smem, *dt = smem + kChunk * D * 2, *et = smem + 2 * kChunk * D * 2;
   float *largest = reinterpret_cast<float*>(et + D * D * 2), *w = largest + kLinWaves;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
-  const int pair = blockIdx.x / p.nseg, sg = blockIdx.x % p.nseg, b = pair / p.Hkv, j = pair % p.Hkv, G = p.Hq / p.Hkv;
+  const int pair = id / p.nseg, sg = id % p.nseg, b = pair / p.Hkv, j = pair % p.Hkv, G = p.Hq / p.Hkv;
   const int len = row_length(p, b), t0 = sg * p.seg_chunks * kChunk;
   const int rows_all = min(p.S - t0, p.seg_chunks * kChunk), m = max(min(len - t0, rows_all), 0), chunks = (m + kChunk - 1) / kChunk;
   const int64_t ldq = (int64_t)p.Hq * D, ldk = (int64_t)p.Hkv * D, tok0 = (int64_t)b * p.S + t0;
@@ -616,7 +662,7 @@ __global__ __launch_bounds__(64 * kLinWaves, 4) void linear_keys_kernel(const Li
   const char *score_rows = dk_role ? dt : qt, *sum_rows = dk_role ? qt : dt;
 
   State<D> s;
-  if (staged) s.load(p.seg + (int64_t)blockIdx.x * D * D, wave, lane);
+  if (p.seg) s.load(p.seg + (int64_t)id * D * D, wave, lane);
   else if (p.s_in) s.load_matrix(p.s_in + (int64_t)pair * D * D, 0, wave, lane);
   else s.clear();
   // not zero: a gradient comes in, or the row goes on behind this segment
@@ -625,7 +671,7 @@ __global__ __launch_bounds__(64 * kLinWaves, 4) void linear_keys_kernel(const Li
   if (some) largest[wave] = s.largest(wave);
   const float log2 = uniform(log2_decay(p.log_decay[j]));
   const Decay whole = decay_of(p.log_decay[j], kChunk);
-  weights_from_start(w, log2, p.scale);
+  weights_from_start(w, log2, p.scale, 0);
   const Decays decays(log2, p.scale, g * 4 - r, 1);
   f32x4 acc[NB];
   bf16x8 kf[KS];
@@ -689,7 +735,7 @@ __global__ __launch_bounds__(64 * kLinWaves, 4) void linear_keys_kernel(const Li
 #pragma unroll
       for (int n = 0; n < NB; ++n) acc[n] = pf.times(Rows<D>::columns_stored(sum_rows, n, pr * 32, lane), acc[n]);
     }
-    if (c > 0 || (!staged && p.s_out)) {
+    if (c > 0 || (!p.seg && p.s_out)) {
       if (h == 0) s.decay(rows == kChunk ? whole : Decay{power(log2, rows), 0.f});
       s.template add<SPLIT>(qt, dt, w, wave, lane);
       some = true;
@@ -712,110 +758,140 @@ __global__ __launch_bounds__(64 * kLinWaves, 4) void linear_keys_kernel(const Li
 #pragma unroll
     for (int n = 0; n < NB; n += 2) store8(ro, at + n * 32, zero);
   }
-  if (!staged && p.s_out) s.store_matrix(p.s_out + (int64_t)pair * D * D, wave, lane);
+  if (!p.seg && p.s_out) s.store_matrix(p.s_out + (int64_t)pair * D * D, wave, lane);
+}
+
+// The three gradients of a call in one launch, so that a segment's do, k and v come from memory once for both kinds of workgroups: dk and dv of `g`, dq of
+// `a`.  Both kinds alternate by eights (consecutive workgroups go to the eight XCDs in turn), unless dq's heads are dealt out.
+template <int D, int SPLIT>
+__global__ __launch_bounds__(64 * kLinWaves, 4) void linear_grad_kernel(const LinearArgs a, const LinearArgs g, int segments, int parts) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  int id = blockIdx.x;
+  bool keys = id < segments;
+  if (parts == 1 && id < (segments & ~7) * 2) {
+    keys = !(id & 8);
+    id = (id >> 4) * 8 + (id & 7);
+  } else if (parts == 1) {
+    id -= (segments & ~7);
+    keys = id < segments;
+    if (!keys) id -= segments & 7;
+  } else if (!keys) {
+    id -= segments;
+  }
+  if (keys) segment_keys<D, SPLIT>(g, id, smem);
+  else segment_out<D, SPLIT>(a, id % segments, id / segments, parts, smem);
 }
 
 // ------------------------------------------------------------------------------------------
 // Host side
 // ------------------------------------------------------------------------------------------
-// workgroups that fill the chip: two on each compute unit
-inline int linear_blocks(int64_t dh) { return 512; }
+constexpr int kLinearBlocks = 512;   // workgroups that fill the chip: two on each compute unit
 
-// Segments of a sequence, a whole number of chunks each, and the workgroups that share a segment's query heads: as many segments as
-// make linear_blocks workgroups, of two chunks at the least.
-struct LinearPlan { int chunks, seg_chunks, nseg; };
-static LinearPlan linear_plan(int64_t pairs, int64_t S, int64_t dh) {
+// Segments of a sequence, a whole number of chunks each: as many as make kLinearBlocks workgroups, of two chunks at the least.
+struct LinearPlan { int seg_chunks, nseg; };
+static LinearPlan linear_plan(int64_t pairs, int64_t S) {
   LinearPlan p;
-  p.chunks = (int)((S + kChunk - 1) / kChunk);
-  int64_t n = (linear_blocks(dh) + pairs - 1) / pairs;
-  if (n > p.chunks / 2) n = p.chunks / 2;
+  const int64_t chunks = (S + kChunk - 1) / kChunk;
+  int64_t n = (kLinearBlocks + pairs - 1) / pairs;
+  if (n > chunks / 2) n = chunks / 2;
   if (n < 1) n = 1;
-  p.seg_chunks = (int)((p.chunks + n - 1) / n);
-  p.nseg = (p.chunks + p.seg_chunks - 1) / p.seg_chunks;
+  p.seg_chunks = (int)((chunks + n - 1) / n);
+  p.nseg = (int)((chunks + p.seg_chunks - 1) / p.seg_chunks);
   return p;
 }
-// room for the states of all segments: below twice linear_blocks of them, and a size that does not fall as the call grows
+// parts into which the heads of a group are dealt where there are few segments
+static int linear_parts(int64_t segments, int64_t G) {
+  const int64_t n = (kLinearBlocks + segments - 1) / segments;
+  return (int)(n < G ? n : G);
+}
+// room for the states of all segments: below twice kLinearBlocks of them, and a size that does not fall as the call grows
 static size_t segment_bytes(int64_t pairs, int64_t S, int64_t dh) {
-  const int64_t chunks = (S + kChunk - 1) / kChunk, most = 2 * linear_blocks(dh);
+  const int64_t chunks = (S + kChunk - 1) / kChunk, most = 2 * kLinearBlocks;
   const int64_t n = pairs < most && pairs * chunks < most ? pairs * chunks : most;
   return (size_t)(n * dh * dh) * sizeof(float);
 }
 size_t linear_attention_fwd_workspace(int64_t B, int64_t S, int64_t Hq, int64_t Hkv, int64_t dh) { return segment_bytes(B * Hkv, S, dh); }
-size_t linear_attention_bwd_workspace(int64_t B, int64_t S, int64_t Hq, int64_t Hkv, int64_t dh) { return segment_bytes(B * Hkv, S, dh); }
+size_t linear_attention_bwd_workspace(int64_t B, int64_t S, int64_t Hq, int64_t Hkv, int64_t dh) { return 2 * segment_bytes(B * Hkv, S, dh); }
 
-template <int D, bool REVERSE>
-static int run_states(const LinearArgs& a, int64_t pairs, hipStream_t st) {
-  hipLaunchKernelGGL((linear_segment_kernel<D, REVERSE>), dim3((unsigned)(pairs * a.nseg)), dim3(64 * kLinWaves), 2 * kChunk * D * 2 + kChunk * sizeof(float), st, a);
-  if (int rc = check_launch("linear attention (segments)")) return rc;
-  hipLaunchKernelGGL((linear_scan_kernel<D, REVERSE>), dim3((unsigned)(pairs * (D * D / 1024))), dim3(256), 0, st, a);
-  return check_launch("linear attention (scan)");
-}
-
-// o from (q, k, v), or dq from (d_o, v, k) with the state transposed
-template <int D>
-static int run_out(const LinearArgs& a, int64_t pairs, hipStream_t st) {
-  constexpr size_t lds = (2 * kChunk + D) * D * 2 + (kLinWaves + kChunk) * sizeof(float);
-  static std::atomic<unsigned long long> done2, done3;
-  const int G = a.Hq / a.Hkv;
-  int parts = (int)((linear_blocks(D) + pairs * a.nseg - 1) / (pairs * a.nseg));
-  parts = parts < G ? parts : G;
-  const int staged = a.nseg > 1 || (parts > 1 && a.s_out);
-  if (staged)
-    if (int rc = run_states<D, false>(a, pairs, st)) return rc;
-  const dim3 grid((unsigned)(pairs * a.nseg * parts));
-  if (a.nseg > 1) {
-    if (int rc = reserve_lds(linear_out_kernel<D, 2>, lds, done2, "linear attention")) return rc;
-    hipLaunchKernelGGL((linear_out_kernel<D, 2>), grid, dim3(64 * kLinWaves), lds, st, a, (int)pairs, parts, staged);
-  } else {
-    if (int rc = reserve_lds(linear_out_kernel<D, 3>, lds, done3, "linear attention")) return rc;
-    hipLaunchKernelGGL((linear_out_kernel<D, 3>), grid, dim3(64 * kLinWaves), lds, st, a, (int)pairs, parts, staged);
-  }
-  return check_launch("linear attention");
-}
-
-template <int D>
-static int run_keys(const LinearArgs& a, int64_t pairs, hipStream_t st) {
-  constexpr size_t lds = (2 * kChunk + D) * D * 2 + (kLinWaves + kChunk) * sizeof(float);
-  static std::atomic<unsigned long long> done2, done3;
-  const dim3 grid((unsigned)(pairs * a.nseg));
-  if (a.nseg > 1) {
-    if (int rc = run_states<D, true>(a, pairs, st)) return rc;
-    if (int rc = reserve_lds(linear_keys_kernel<D, 2>, lds, done2, "linear attention")) return rc;
-    hipLaunchKernelGGL((linear_keys_kernel<D, 2>), grid, dim3(64 * kLinWaves), lds, st, a, 1);
-  } else {
-    if (int rc = reserve_lds(linear_keys_kernel<D, 3>, lds, done3, "linear attention")) return rc;
-    hipLaunchKernelGGL((linear_keys_kernel<D, 3>), grid, dim3(64 * kLinWaves), lds, st, a, 0);
-  }
-  return check_launch("linear attention (keys)");
-}
-
-static LinearArgs linear_args(const LinearCall& c, void* workspace) {
-  const LinearPlan plan = linear_plan(c.B * c.Hkv, c.S, c.dh);
+static LinearArgs linear_args(const LinearCall& c) {
+  const LinearPlan plan = linear_plan(c.B * c.Hkv, c.S);
   LinearArgs a{};
   a.q = (const bf16_t*)c.q; a.k = (const bf16_t*)c.k; a.v = (const bf16_t*)c.v;
-  a.log_decay = c.log_decay; a.lengths = c.lengths; a.seg = (float*)workspace;
+  a.log_decay = c.log_decay; a.lengths = c.lengths;
   a.S = (int)c.S; a.Hq = (int)c.Hq; a.Hkv = (int)c.Hkv;
   a.seg_chunks = plan.seg_chunks; a.nseg = plan.nseg; a.scale = c.scale;
   return a;
 }
 
+// the states (gradients) between segments, in a.seg (and g.seg, if g is given)
+template <int D>
+static int run_states(const LinearArgs& a, const LinearArgs* g, int64_t pairs, hipStream_t st) {
+  hipLaunchKernelGGL(linear_segment_kernel<D>, dim3((unsigned)(pairs * a.nseg), g ? 2 : 1), dim3(64 * kLinWaves),
+                     2 * kChunk * D * 2 + kChunk * sizeof(float), st, a, g ? *g : a);
+  if (int rc = check_launch("linear attention (segments)")) return rc;
+  hipLaunchKernelGGL(linear_scan_kernel<D>, dim3((unsigned)(pairs * (D * D / 1024)), g ? 2 : 1), dim3(256), 0, st, a, g ? *g : a);
+  return check_launch("linear attention (scan)");
+}
+
+template <int D> constexpr size_t kLinearLds = (2 * kChunk + D) * D * 2 + (kLinWaves + kChunk) * sizeof(float);
+
+template <int D, int SPLIT>
+static int launch_out(const LinearArgs& a, int64_t segments, int parts, hipStream_t st) {
+  static std::atomic<unsigned long long> done;
+  if (int rc = reserve_lds(linear_out_kernel<D, SPLIT>, kLinearLds<D>, done, "linear_attention_forward")) return rc;
+  hipLaunchKernelGGL((linear_out_kernel<D, SPLIT>), dim3((unsigned)(segments * parts)), dim3(64 * kLinWaves), kLinearLds<D>, st, a, (int)segments, parts);
+  return check_launch("linear_attention_forward");
+}
+template <int D>
+static int run_forward(LinearArgs a, int64_t pairs, float* workspace, hipStream_t st) {
+  const int64_t segments = pairs * a.nseg;
+  const int parts = linear_parts(segments, a.Hq / a.Hkv);
+  if (a.nseg > 1 || (parts > 1 && a.s_out)) {
+    a.seg = workspace;
+    if (int rc = run_states<D>(a, nullptr, pairs, st)) return rc;
+  }
+  return a.nseg > 1 ? launch_out<D, 2>(a, segments, parts, st) : launch_out<D, 3>(a, segments, parts, st);
+}
+
+template <int D, int SPLIT>
+static int launch_grad(const LinearArgs& a, const LinearArgs& g, int64_t segments, int parts, hipStream_t st) {
+  static std::atomic<unsigned long long> done;
+  if (int rc = reserve_lds(linear_grad_kernel<D, SPLIT>, kLinearLds<D>, done, "linear_attention_backward")) return rc;
+  hipLaunchKernelGGL((linear_grad_kernel<D, SPLIT>), dim3((unsigned)(segments * (1 + parts))), dim3(64 * kLinWaves), kLinearLds<D>, st, a, g,
+                     (int)segments, parts);
+  return check_launch("linear_attention_backward");
+}
+template <int D>
+static int run_backward(LinearArgs a, LinearArgs g, int64_t pairs, float* workspace, hipStream_t st) {
+  const int64_t segments = pairs * a.nseg;
+  const int parts = linear_parts(segments, a.Hq / a.Hkv);
+  if (a.nseg > 1) {
+    a.seg = workspace;
+    g.seg = workspace + segments * D * D;
+    if (int rc = run_states<D>(a, &g, pairs, st)) return rc;
+    return launch_grad<D, 2>(a, g, segments, parts, st);
+  }
+  return launch_grad<D, 3>(a, g, segments, parts, st);
+}
+
 int launch_linear_attention_fwd(const LinearCall& c, const float* s_in, void* o, float* s_out, void* workspace, hipStream_t st) {
-  LinearArgs a = linear_args(c, workspace);
+  LinearArgs a = linear_args(c);
   a.o = (bf16_t*)o; a.s_in = s_in; a.s_out = s_out;
   const int64_t pairs = c.B * c.Hkv;
-  return c.dh == 128 ? run_out<128>(a, pairs, st) : c.dh == 64 ? run_out<64>(a, pairs, st) : run_out<32>(a, pairs, st);
+  float* ws = (float*)workspace;
+  return c.dh == 128 ? run_forward<128>(a, pairs, ws, st) : c.dh == 64 ? run_forward<64>(a, pairs, ws, st) : run_forward<32>(a, pairs, ws, st);
 }
 
 int launch_linear_attention_bwd(const LinearCall& c, const float* s_in, const void* d_o, const float* ds_out, void* dq, void* dk, void* dv,
                                 float* ds_in, void* workspace, hipStream_t st) {
-  const int64_t pairs = c.B * c.Hkv;
-  LinearArgs a = linear_args(c, workspace);
+  // dq is the forward's o of (d_o, v, k) and the transposed state
+  LinearArgs a = linear_args(c), g = a;
   a.q = (const bf16_t*)d_o; a.k = (const bf16_t*)c.v; a.v = (const bf16_t*)c.k;
   a.o = (bf16_t*)dq; a.s_in = s_in; a.flip = 1;
-  if (int rc = c.dh == 128 ? run_out<128>(a, pairs, st) : c.dh == 64 ? run_out<64>(a, pairs, st) : run_out<32>(a, pairs, st)) return rc;
-  a = linear_args(c, workspace);
-  a.d_o = (const bf16_t*)d_o; a.dk = (bf16_t*)dk; a.dv = (bf16_t*)dv; a.s_in = ds_out; a.s_out = ds_in;
-  return c.dh == 128 ? run_keys<128>(a, pairs, st) : c.dh == 64 ? run_keys<64>(a, pairs, st) : run_keys<32>(a, pairs, st);
+  g.d_o = (const bf16_t*)d_o; g.dk = (bf16_t*)dk; g.dv = (bf16_t*)dv; g.s_in = ds_out; g.s_out = ds_in;
+  const int64_t pairs = c.B * c.Hkv;
+  float* ws = (float*)workspace;
+  return c.dh == 128 ? run_backward<128>(a, g, pairs, ws, st) : c.dh == 64 ? run_backward<64>(a, g, pairs, ws, st) : run_backward<32>(a, g, pairs, ws, st);
 }
 
 // ------------------------------------------------------------------------------------------
