@@ -23,8 +23,7 @@
 // Layout.  All products are v_mfma_f32_16x16x32_bf16, D[row][col] += A[row][k] B[k][col]: lane (g = lane / 16, r = lane % 16) holds row r of A and
 // column r of B, 8 of 32 k each, and rows 4 g .. 4 g + 3 of column r of D.  Scores are formed as S^T[j][i] = K Q^T, so that a lane
 // owns one query and its scores come out as the B operand of O^T[d][i] += V^T P^T: k-slot (g, e) is token 4 g + e of the first 16 for e < 4, and of
-// the second 16 otherwise, and the transposing reads of V take the same tokens.  Rows of O^T (and of the state's columns) are taken in the order
-// d = 32 (n / 2) + 8 (r / 4) + 4 (n % 2) + r % 4 for row r of block n, which puts 8 neighbours into one lane: 16-byte stores.
+// the second 16 otherwise, and the transposing reads of V take the same tokens.
 #include "common.h"
 #include "kernels.h"
 
@@ -70,42 +69,41 @@ __device__ __forceinline__ void store8(__amdgpu_buffer_rsrc_t rs, uint32_t at, c
   __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), rs, (int)at, 0, 0);
 }
 
-// [rows][D] bf16 in LDS, 16-byte piece c of row r at piece c ^ swz(r), chosen so that 16 rows of one piece, and 4 rows of 64 bytes, fall into
-// different banks.
+// [rows][D] of 16 bits in LDS, 16-byte piece c of row r at piece c ^ swz(r).  The LDS serves 256 bytes a clock; the pieces are dealt so that neither
+// 16 rows of one piece (reads along a row, 16 lanes at a time) nor 8 rows of 32 bytes (transposing reads, 32 lanes) meet in a bank.
 template <int D>
 struct Rows {
   static constexpr int BYTES = D * 2, PIECES = D / 8;
   static __device__ __forceinline__ int swz(int r) {
-    if constexpr (PIECES == 16) return ((r & 3) << 2) | ((r >> 2) & 3);
-    else if constexpr (PIECES == 8) return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
-    else return (r >> 2) & 3;
+    if constexpr (PIECES == 16) return ((r & 3) << 2) | (((r >> 2) & 1) << 1) | ((r >> 3) & 1);
+    else if constexpr (PIECES == 8) return (((r >> 1) & 3) << 1) | ((r >> 3) & 1);
+    else return (((r >> 2) & 1) << 1) | ((r >> 3) & 1);
   }
   static __device__ __forceinline__ int at(int r, int piece) { return r * BYTES + ((piece ^ swz(r)) << 4); }
-  // operand of 16 rows from row0, k over step ks of the row
-  static __device__ __forceinline__ bf16x8 along(const char* t, int row0, int ks, int lane) {
-    return *reinterpret_cast<const bf16x8*>(t + at(row0 + (lane & 15), ks * 4 + (lane >> 4)));
+  // Operands, by a lane's LDS address that is the same for all of a kind (of a tile at the start of LDS): everything else is an exclusive or with a
+  // constant, and constants added (the tile `t` and its row), which the read itself adds.
+  // along: 16 rows from row0, k over step ks of the row
+  static __device__ __forceinline__ uint32_t along_lane(uint32_t lds, int lane) { return lds + at(lane & 15, lane >> 4); }
+  static __device__ __forceinline__ bf16x8 along(uint32_t along_lane, int t, int row0, int ks) {
+    return *(LDS_PTR(const bf16x8))(uintptr_t)((along_lane ^ (uint32_t)(ks << 6)) + (uint32_t)(t + row0 * BYTES));
   }
-  // four values of 16 columns: rows row .. row + 3, the lane's column by the caller's piece and half of a piece
-  static __device__ __forceinline__ bf16x4 across(const char* t, int row, int piece, int half) {
-    return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(t + at(row, piece) + half * 8));
+  // columns: the 16 columns 16 n .. of the tile, k over the 32 rows from row0: slot (g, e) is row 4 g + e, or 12 + 4 g + e for e >= 4; with GAP 4 row 8 g + e
+  template <int GAP = 16>
+  static __device__ __forceinline__ uint32_t columns_lane(uint32_t lds, int lane) {
+    return lds + at((lane >> 4) * (GAP == 16 ? 4 : 8) + ((lane & 15) >> 2), (lane & 3) >> 1) + (lane & 1) * 8;
   }
-  // operand of the 16 columns 16 n .. of the tile, k over the 32 rows from row0 (slots as at the top of the file)
-  static __device__ __forceinline__ bf16x8 columns(const char* t, int n, int row0, int lane) {
-    const int r = row0 + ((lane >> 4) << 2) + ((lane & 15) >> 2), piece = 2 * n + ((lane & 3) >> 1), half = lane & 1;
+  template <int GAP = 16>
+  static __device__ __forceinline__ bf16x8 columns(uint32_t columns_lane, int t, int n, int row0) {
+    // a row further by 4 changes one bit of the swizzle, by 16 none
+    const uint32_t lo = columns_lane ^ (uint32_t)(n << 5), hi = GAP == 16 ? lo : columns_lane ^ (uint32_t)((n << 5) ^ (swz(4) << 4));
     bf16x8 v;
-    v.lo = across(t, r, piece, half);
-    v.hi = across(t, r + 16, piece, half);
-    return v;
-  }
-  // the same of block n of the columns in stored order
-  static __device__ __forceinline__ bf16x8 columns_stored(const char* t, int n, int row0, int lane) {
-    const int r = row0 + ((lane >> 4) << 2) + ((lane & 15) >> 2), piece = (n >> 1) * 4 + (lane & 3), half = n & 1;
-    bf16x8 v;
-    v.lo = across(t, r, piece, half);
-    v.hi = across(t, r + 16, piece, half);
+    v.lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)(lo + (uint32_t)(t + row0 * BYTES)));
+    v.hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)(hi + (uint32_t)(t + (row0 + GAP) * BYTES)));
     return v;
   }
 };
+// where a kernel's LDS begins
+__device__ __forceinline__ uint32_t lds_address(char* smem) { return (uint32_t)(uintptr_t)(LDS_PTR(char))smem; }
 
 // A 64-row tile from memory to LDS without a detour through registers: each load of a wave fills 1 KB, lane after lane, so the pieces are
 // picked in memory in the order in which they lie in LDS.  Done when vmcnt is 0 and a barrier passed.
@@ -151,41 +149,74 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 __device__ __forceinline__ f32x4 mfma16_f16(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
 // Powers of two that take numbers up to some bound into the upper half of fp16's range (below 2^15, so that what is 2^29 times smaller than
-// the bound keeps its eleven bits), and back.
+// the bound keeps its eleven bits), and back.  exponent: of the bound, as an fp32 has it.
 struct Scale {
   float up, down;
-  // exponent: of the bound, as an fp32 has it
   __device__ __forceinline__ explicit Scale(int exponent) {
-    const int e = max(exponent, 14);
+    const int e = max(exponent, 29);
     up = __int_as_float((268 - e) << 23);
-    down = e <= 14 ? __int_as_float(0) : __int_as_float((e - 14) << 23);
+    down = __int_as_float((e - 14) << 23);
   }
 };
 
-// An operand of KS steps (a lane's 8 values of 32 each, four lanes a row), in fp16: the rows scaled, exactly, to their largest value.
+// An operand of KS steps (a lane's 8 values of 32 each, four lanes a row), in fp16: the rows scaled, exactly, to their largest value.  Two values at a
+// time, in integers: of the 15 bits under a bf16's sign the exponent is moved and all are shifted into fp16's place.
 template <int KS>
 struct ScaledRow {
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
   f16x8 v[KS];
-  float down;
+  float down;   // infinite for a row that is not finite
   __device__ __forceinline__ explicit ScaledRow(const bf16x8 (&x)[KS]) {
-    uint32_t most = 0;
+    u16x2 top = {0, 0};
 #pragma unroll
     for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, __builtin_bit_cast(u32x4, x[k])[i] & 0x7fff7fffu));
+    uint32_t most = max((uint32_t)top.x, (uint32_t)top.y);
+    const auto a = __builtin_amdgcn_permlane16_swap(most, most, false, false);
+    most = max(a[0], a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(most, most, false, false);
+    most = max(b[0], b[1]);
+    const uint32_t e = max(most >> 7, 29u);
+    down = __int_as_float(e == 255 ? 0x7f800000 : (int)(e - 14) << 23);
+    const unsigned short less = (unsigned short)((e - 29) << 7);
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      const u32x4 u = __builtin_bit_cast(u32x4, x[k]);
+      u32x4 h;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const uint32_t two = __builtin_bit_cast(u32x4, x[k])[i];
-        most = max(most, max(two & 0x7fff0000u, (two << 16) & 0x7fff0000u));
+        const u16x2 m = __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, u[i] & 0x7fff7fffu), u16x2{less, less}) << (unsigned short)3;
+        h[i] = (u[i] & 0x80008000u) | __builtin_bit_cast(uint32_t, m);
       }
-    most = max(most, (uint32_t)__shfl_xor((int)most, 16, 64));
-    most = max(most, (uint32_t)__shfl_xor((int)most, 32, 64));
-    const Scale s((int)(most >> 23));
-    down = s.down;
-#pragma unroll
-    for (int k = 0; k < KS; ++k)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[k][e] = (_Float16)((float)x[k][e] * s.up);
+      v[k] = __builtin_bit_cast(f16x8, h);
+    }
   }
 };
+
+// Stores NB blocks of 16 values of a lane's row as bf16.  A lane holds values 16 n + 4 g .. + 3 of block n; lanes 16 apart exchange halves of two blocks,
+// and each stores 16 bytes of one of them.  all: no lane's row is to be zeros (keep false).
+template <int NB>
+__device__ __forceinline__ void store_row(__amdgpu_buffer_rsrc_t rs, uint32_t row_at, const f32x4 (&o)[NB], bool all, bool keep, int lane) {
+  const int g = lane >> 4;
+  row_at += (g & 1) * 32 + (g >> 1) * 16;
+#pragma unroll
+  for (int n = 0; n < NB; n += 2) {
+    u32x2 x[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      bf16x4 v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = (bf16_t)o[n + i][e];
+      x[i] = __builtin_bit_cast(u32x2, v);
+    }
+    const auto a = __builtin_amdgcn_permlane16_swap(x[0].x, x[1].x, false, false), b = __builtin_amdgcn_permlane16_swap(x[0].y, x[1].y, false, false);
+    u32x4 w = {a[0], b[0], a[1], b[1]};
+    if (!all)
+      if (!keep) w = u32x4{0, 0, 0, 0};
+    __builtin_amdgcn_raw_buffer_store_b128(w, rs, (int)(row_at + n * 32), 0, 0);
+  }
+}
 
 __device__ __forceinline__ float uniform(float x) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x))); }
 
@@ -208,7 +239,7 @@ struct State {
   static __device__ __forceinline__ int col_block(int wave) { return D == 128 ? 0 : (wave & 1) * CB; }
   // first of the four rows, and the column, of a lane in block (rb, cb) of the state
   static __device__ __forceinline__ int row(int rb, int lane) { return rb * 16 + ((lane >> 4) << 2); }
-  static __device__ __forceinline__ int col(int cb, int lane) { return (cb >> 1) * 32 + (((lane & 15) >> 2) << 3) + ((cb & 1) << 2) + (lane & 3); }
+  static __device__ __forceinline__ int col(int cb, int lane) { return cb * 16 + (lane & 15); }
   static __device__ __forceinline__ bool holds(int wave) { return WAVES == kLinWaves || wave < WAVES; }
 
   __device__ __forceinline__ void clear() {
@@ -217,13 +248,15 @@ struct State {
 #pragma unroll
       for (int j = 0; j < CB; ++j) a[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
+  // EXACT: with both terms of the decay
+  template <bool EXACT>
   __device__ __forceinline__ void decay(const Decay& l) {
 #pragma unroll
     for (int i = 0; i < RB; ++i)
 #pragma unroll
       for (int j = 0; j < CB; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) a[i][j][e] = decayed(l, a[i][j][e], 0.f);
+        for (int e = 0; e < 4; ++e) a[i][j][e] = EXACT ? decayed(l, a[i][j][e], 0.f) : a[i][j][e] * l.hi;
   }
   // element of a [D][D] matrix, transposed if flip
   static __device__ __forceinline__ int element(int row, int col, int flip) { return flip ? col * D + row : row * D + col; }
@@ -275,9 +308,16 @@ struct State {
             for (int e = 0; e < 4; ++e) m = fabsf(a[i][j][e]) < INFINITY ? fmaxf(m, fabsf(a[i][j][e])) : m;
       }
     }
-    return wave_max(m);
+    const auto a32 = __builtin_amdgcn_permlane32_swap(__float_as_int(m), __float_as_int(m), false, false);
+    m = fmaxf(__int_as_float(a32[0]), __int_as_float(a32[1]));
+    const auto a16 = __builtin_amdgcn_permlane16_swap(__float_as_int(m), __float_as_int(m), false, false);
+    m = fmaxf(__int_as_float(a16[0]), __int_as_float(a16[1]));
+    m = fmaxf(m, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(m), 0x128, 0xf, 0xf, true)));   // rotations within 16 lanes
+    m = fmaxf(m, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(m), 0x124, 0xf, 0xf, true)));
+    m = fmaxf(m, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(m), 0x122, 0xf, 0xf, true)));
+    return fmaxf(m, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(m), 0x121, 0xf, 0xf, true)));
   }
-  // to LDS in fp16 [columns in stored order][rows]: an operand along either
+  // to LDS in fp16 [columns][rows]: an operand along either
   __device__ __forceinline__ void to_lds(char* t, float up, int wave, int lane) const {
     if (!holds(wave)) return;
     lane = here(lane);
@@ -292,11 +332,12 @@ struct State {
         *reinterpret_cast<f16x4*>(t + Rows<D>::at(p, r >> 3) + ((r & 7) << 1)) = v;
       }
   }
-  // += sum over the tile's 64 tokens of (w x)^T y, all in LDS; w x as the sum of SPLIT bf16
+  // += sum over a tile's 64 tokens of (w x)^T y, all in LDS (x, y: where); w x as the sum of SPLIT bf16
   template <int SPLIT>
-  __device__ __forceinline__ void add(const char* x, const char* y, const float* w, int wave, int lane) {
+  __device__ __forceinline__ void add(int x, int y, const float* w, int wave, int lane, uint32_t columns_lane) {
     if (!holds(wave)) return;
     lane = here(lane);
+    const uint32_t cl = here(columns_lane ^ (uint32_t)(col_block(wave) << 5)), own = here(columns_lane ^ (uint32_t)(row_block(wave) << 5));
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
       bf16x8 part[RB][SPLIT];
@@ -304,7 +345,7 @@ struct State {
 #pragma unroll
       for (int i = 0; i < RB; ++i) {
         float f[8];
-        unpack8(Rows<D>::columns(x, row_block(wave) + i, p * 32, lane), f);
+        unpack8(Rows<D>::columns(own, x, i, p * 32), f);
 #pragma unroll
         for (int e = 0; e < 8; ++e) f[e] *= e < 4 ? w0[e] : w1[e - 4];
 #pragma unroll
@@ -316,7 +357,7 @@ struct State {
       }
 #pragma unroll
       for (int j = 0; j < CB; ++j) {
-        const bf16x8 v = Rows<D>::columns_stored(y, col_block(wave) + j, p * 32, lane);
+        const bf16x8 v = Rows<D>::columns(cl, y, j, p * 32);
 #pragma unroll
         for (int k = SPLIT - 1; k >= 0; --k)
 #pragma unroll
@@ -334,32 +375,27 @@ __device__ __forceinline__ Scale state_scale(const float* largest) {
   return Scale(__builtin_amdgcn_readfirstlane(__float_as_int(m) >> 23));
 }
 
-// lambda^(place of the query - place of the key) for a 16 x 16 block of scores whose lane holds four keys (queries) of one query (key): of the
-// block on the diagonal (left: the lane's query less the first of its keys; the rest of it masked), and of the block next to it, from which the further ones
-// differ by a factor.
+// mult lambda^(place of the query - place of the key) for a 16 x 16 block of scores whose lane holds four keys of one query (STEP -1) or four queries of
+// one key (STEP 1).  Uniform powers, and one of the lane's: a lane's own eight would be registers that are not there.
+template <int STEP>
 struct Decays {
-  float same[4], next[4], f2, f3;
-  // step: -1 where the lane holds four keys, 1 where it holds four queries
-  __device__ __forceinline__ Decays(float log2, float mult, int left, int step) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int d = left + step * e;
-      same[e] = d >= 0 ? mult * power(log2, d) : 0.f;
-      next[e] = mult * power(log2, 16 + d);
-    }
-    f2 = uniform(power(log2, 16));
-    f3 = uniform(power(log2, 32));
-  }
-  // blocks: from the key's to the query's; keep(e) is false for what the diagonal block masks
-  template <typename F>
-  __device__ __forceinline__ void apply(f32x4& s, int blocks, F&& keep) const {
+  float log2, mult, p1, p2, p3, p16, p32;
+  __device__ __forceinline__ Decays(float log2_, float mult_)
+      : log2(log2_), mult(mult_), p1(uniform(power(log2_, 1))), p2(uniform(power(log2_, 2))), p3(uniform(power(log2_, 3))),
+        p16(uniform(power(log2_, 16))), p32(uniform(power(log2_, 32))) {}
+  // blocks: from the key's to the query's, 0 .. 3; within the diagonal block what is not causal becomes 0
+  __device__ __forceinline__ void apply(f32x4& s, int blocks, int lane) const {
+    const int first = STEP * (((lane >> 4) << 2) - (lane & 15));   // of the lane's four differences within 16
     if (blocks == 0) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[e] = keep(e) ? s[e] * same[e] : 0.f;
+      for (int e = 0; e < 4; ++e) s[e] = first + STEP * e >= 0 ? s[e] * (mult * power(log2, first + STEP * e)) : 0.f;
     } else {
-      const float f = blocks == 1 ? 1.f : blocks == 2 ? f2 : f3;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) s[e] *= next[e] * f;
+      const float f = blocks == 1 ? 1.f : blocks == 2 ? p16 : p32;
+      const float base = mult * f * power(here(log2), 16 + first - (STEP < 0 ? 3 : 0));
+      s[STEP < 0 ? 3 : 0] *= base;
+      s[STEP < 0 ? 2 : 1] *= base * p1;
+      s[STEP < 0 ? 1 : 2] *= base * p2;
+      s[STEP < 0 ? 0 : 3] *= base * p3;
     }
   }
 };
@@ -403,7 +439,7 @@ __device__ __forceinline__ float log2_decay(float g) { return (float)(decay_log(
 // ------------------------------------------------------------------------------------------
 template <int D, bool GRADIENT>
 __device__ __forceinline__ void segment_sum(const LinearArgs& p, char* smem) {
-  char *xt = smem, *yt = smem + kChunk * D * 2;
+  constexpr int xt = 0, yt = kChunk * D * 2;
   float* w = reinterpret_cast<float*>(smem + 2 * kChunk * D * 2);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int pair = blockIdx.x / p.nseg, sg = blockIdx.x % p.nseg, b = pair / p.Hkv, j = pair % p.Hkv;
@@ -422,6 +458,7 @@ __device__ __forceinline__ void segment_sum(const LinearArgs& p, char* smem) {
   const int64_t first = ((int64_t)b * p.S + t0) * ld + (int64_t)j * G * D;
   const float log2 = log2_decay(p.log_decay[j]);
   const Decay whole = decay_of(p.log_decay[j], kChunk);
+  const uint32_t columns_lane = Rows<D>::columns_lane(lds_address(smem), lane);
   Staged<D> xs, ys;
   auto fetch = [&](int it) {
     const int rows = min(m - it / G * kChunk, kChunk);
@@ -433,8 +470,8 @@ __device__ __forceinline__ void segment_sum(const LinearArgs& p, char* smem) {
   for (int it = 0; it < items; ++it) {
     const int c = it / G, rows = min(m - c * kChunk, kChunk);
     __syncthreads();
-    xs.store(xt);
-    ys.store(yt);
+    xs.store(smem + xt);
+    ys.store(smem + yt);
     if (GRADIENT) {
       if (it % G == 0) weights_from_start(w, log2, p.scale, c * kChunk);
     } else if (c == 0 || rows < kChunk) {
@@ -442,8 +479,8 @@ __device__ __forceinline__ void segment_sum(const LinearArgs& p, char* smem) {
     }
     __syncthreads();
     if (it + 1 < items) fetch(it + 1);
-    if (!GRADIENT && c > 0) s.decay(rows == kChunk ? whole : Decay{power(log2, rows), 0.f});
-    s.template add<3>(xt, yt, w, wave, lane);
+    if (!GRADIENT && c > 0) s.template decay<true>(rows == kChunk ? whole : Decay{power(log2, rows), 0.f});
+    s.template add<3>(xt, yt, w, wave, lane, columns_lane);
   }
   s.store(out, wave, lane);
 }
@@ -505,13 +542,13 @@ __global__ __launch_bounds__(256) void linear_scan_kernel(const LinearArgs a, co
 // LDS.  Four waves take 16 queries of a head each, the other four those of the next head; an odd last head is shared, half of the columns
 // for either.  SPLIT: 3 where the state goes on to the caller, 2 where it serves this kernel's products alone.
 // ------------------------------------------------------------------------------------------
-// NB blocks of 16 columns from n0 for the queries of one lane's row; returns them unscaled
+// NB blocks of 16 columns from n0 of o for the query that the lane's row is
 template <int D, int NB>
-__device__ __forceinline__ void out_tile(f32x4 (&o)[NB], const bf16x8 (&qf)[D / 32], const char* kt, const char* vt, const char* st, bool some,
-                                         float down, int tile, int n0, float log2, const Decays& ds, int lane) {
-  constexpr int KS = D / 32;
-  lane = here(lane);
-  const int r = lane & 15, g = lane >> 4;
+__device__ __forceinline__ void out_tile(f32x4 (&o)[NB], const bf16x8 (&qf)[D / 32], bool some,
+                                         float down, int tile, int n0, float log2, float scale, const Decays<-1>& ds, int lane, uint32_t along_lane, uint32_t columns_lane) {
+  constexpr int KS = D / 32, kt = 0, vt = kChunk * D * 2, st = 2 * kChunk * D * 2;
+  const uint32_t al = here(along_lane), sl = here(along_lane + (uint32_t)(n0 * 16 * D * 2)), cl = here(columns_lane ^ (uint32_t)(n0 << 5));
+  const int r = lane & 15;
 #pragma unroll
   for (int n = 0; n < NB; ++n) o[n] = f32x4{0.f, 0.f, 0.f, 0.f};
   if (some) {
@@ -520,8 +557,8 @@ __device__ __forceinline__ void out_tile(f32x4 (&o)[NB], const bf16x8 (&qf)[D / 
     for (int k = 0; k < KS; ++k)
 #pragma unroll
       for (int n = 0; n < NB; ++n)
-        o[n] = mfma16_f16(__builtin_bit_cast(f16x8, Rows<D>::along(st, (n0 + n) * 16, k, lane)), qs.v[k], o[n]);
-    const float after = power(log2, tile * 16 + r + 1) * down * qs.down;
+        o[n] = mfma16_f16(__builtin_bit_cast(f16x8, Rows<D>::along(sl, st, n * 16, k)), qs.v[k], o[n]);
+    const float after = power(log2, tile * 16 + r + 1) * scale * down * qs.down;
 #pragma unroll
     for (int n = 0; n < NB; ++n) o[n] *= after;
   }
@@ -535,20 +572,20 @@ __device__ __forceinline__ void out_tile(f32x4 (&o)[NB], const bf16x8 (&qf)[D / 
       sc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
       if (blk > tile) continue;
 #pragma unroll
-      for (int k = 0; k < KS; ++k) sc[i] = mfma16(Rows<D>::along(kt, blk * 16, k, lane), qf[k], sc[i]);
-      ds.apply(sc[i], tile - blk, [&](int e) { return g * 4 + e <= r; });
+      for (int k = 0; k < KS; ++k) sc[i] = mfma16(Rows<D>::along(al, kt, blk * 16, k), qf[k], sc[i]);
+      ds.apply(sc[i], tile - blk, lane);
     }
     const Scores pf(sc);
 #pragma unroll
-    for (int n = 0; n < NB; ++n) o[n] = pf.times(Rows<D>::columns_stored(vt, n0 + n, pr * 32, lane), o[n]);
+    for (int n = 0; n < NB; ++n) o[n] = pf.times(Rows<D>::columns(cl, vt, n, pr * 32), o[n]);
   }
 }
 
 template <int D, int SPLIT>
 __device__ __forceinline__ void segment_out(const LinearArgs& p, int id, int part, int parts, char* smem) {
   constexpr int NB = D / 16, KS = D / 32;
-  char *kt = smem, *vt = smem + kChunk * D * 2, *st = smem + 2 * kChunk * D * 2;
-  float *largest = reinterpret_cast<float*>(st + D * D * 2), *w = largest + kLinWaves;
+  constexpr int kt = 0, vt = kChunk * D * 2, st = 2 * kChunk * D * 2;
+  float *largest = reinterpret_cast<float*>(smem + st + D * D * 2), *w = largest + kLinWaves;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
   const int pair = id / p.nseg, sg = id % p.nseg, b = pair / p.Hkv, j = pair % p.Hkv, G = p.Hq / p.Hkv;
   const int per = (G + parts - 1) / parts, h0 = part * per, h1 = min(G, h0 + per);
@@ -567,20 +604,21 @@ __device__ __forceinline__ void segment_out(const LinearArgs& p, int id, int par
   if (some) largest[wave] = s.largest(wave);
   const float log2 = uniform(log2_decay(p.log_decay[j]));
   const Decay whole = decay_of(p.log_decay[j], kChunk);
-  const Decays decays(log2, 1.f, r - g * 4, -1);
+  const Decays<-1> decays(log2, p.scale);
+  const uint32_t along_lane = Rows<D>::along_lane(lds_address(smem), lane), columns_lane = Rows<D>::columns_lane(lds_address(smem), lane);
 
   for (int c = 0; c < chunks; ++c) {
     const int rows = min(m - c * kChunk, kChunk), rows_out = min(rows_all - c * kChunk, kChunk);
     const bool more = c + 1 < chunks;
     const int64_t kc = kv0 + (int64_t)c * kChunk * ldk;
     __syncthreads();
-    tile_to_lds<D>(rows_rsrc<D>(p.k + kc, ldk, rows), kt, ldk, wave, lane);
-    tile_to_lds<D>(rows_rsrc<D>(p.v + kc, ldk, rows), vt, ldk, wave, lane);
+    tile_to_lds<D>(rows_rsrc<D>(p.k + kc, ldk, rows), smem + kt, ldk, wave, lane);
+    tile_to_lds<D>(rows_rsrc<D>(p.v + kc, ldk, rows), smem + vt, ldk, wave, lane);
     if (c == 0 || rows < kChunk) weights_to_end(w, log2, rows);
     if (some) {
       const Scale sc = state_scale(largest);
       down = sc.down;
-      s.to_lds(st, sc.up, wave, lane);
+      s.to_lds(smem + st, sc.up, wave, lane);
     }
     loads_done();
     const int64_t qc = q0 + (int64_t)c * kChunk * ldq;
@@ -594,29 +632,20 @@ __device__ __forceinline__ void segment_out(const LinearArgs& p, int id, int par
       bf16x8 qf[KS];
 #pragma unroll
       for (int k = 0; k < KS; ++k) qf[k] = load8(rq, at + k * 64 + g * 16);
-      auto finish = [&](auto& o, int n0, int blocks) {
-#pragma unroll
-        for (int n = 0; n < blocks; n += 2) {
-          bf16x8 v;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = (bf16_t)(t < rows ? o[n + (e >> 2)][e & 3] * p.scale : 0.f);
-          store8(ro, at + (n0 + n) * 32 + g * 16, v);
-        }
-      };
       if (both || D == 32) {
         f32x4 o[NB];
-        out_tile<D, NB>(o, qf, kt, vt, st, some, down, tile, 0, log2, decays, lane);
-        finish(o, 0, NB);
+        out_tile<D, NB>(o, qf, some, down, tile, 0, log2, p.scale, decays, lane, along_lane, columns_lane);
+        store_row<NB>(ro, at, o, rows == kChunk, t < rows, lane);
       } else if constexpr (D > 32) {
         const int n0 = wave >= 4 ? NB / 2 : 0;
         f32x4 o[NB / 2];
-        out_tile<D, NB / 2>(o, qf, kt, vt, st, some, down, tile, n0, log2, decays, lane);
-        finish(o, n0, NB / 2);
+        out_tile<D, NB / 2>(o, qf, some, down, tile, n0, log2, p.scale, decays, lane, along_lane, columns_lane);
+        store_row<NB / 2>(ro, at + n0 * 32, o, rows == kChunk, t < rows, lane);
       }
     }
     if (more || s_out) {
-      s.decay(rows == kChunk ? whole : Decay{power(log2, rows), 0.f});
-      s.template add<SPLIT>(kt, vt, w, wave, lane);
+      s.template decay<SPLIT == 3>(rows == kChunk ? whole : Decay{power(log2, rows), 0.f});
+      s.template add<SPLIT>(kt, vt, w, wave, lane, columns_lane);
       some = true;
       if (more) largest[wave] = s.largest(wave);
     }
@@ -646,8 +675,8 @@ __global__ __launch_bounds__(64 * kLinWaves, 4) void linear_out_kernel(const Lin
 template <int D, int SPLIT>
 __device__ __forceinline__ void segment_keys(const LinearArgs& p, int id, char* smem) {
   constexpr int NB = D / 16, KS = D / 32;
-  char *qt = smem, *dt = smem + kChunk * D * 2, *et = smem + 2 * kChunk * D * 2;
-  float *largest = reinterpret_cast<float*>(et + D * D * 2), *w = largest + kLinWaves;
+  constexpr int qt = 0, dt = kChunk * D * 2, et = 2 * kChunk * D * 2;
+  float *largest = reinterpret_cast<float*>(smem + et + D * D * 2), *w = largest + kLinWaves;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
   const int pair = id / p.nseg, sg = id % p.nseg, b = pair / p.Hkv, j = pair % p.Hkv, G = p.Hq / p.Hkv;
   const int len = row_length(p, b), t0 = sg * p.seg_chunks * kChunk;
@@ -656,10 +685,10 @@ __device__ __forceinline__ void segment_keys(const LinearArgs& p, int id, char* 
   const int64_t kv0 = tok0 * ldk + (int64_t)j * D, q0 = tok0 * ldq + (int64_t)j * G * D;
   const bool dk_role = wave >= 4;
   const int tile = wave & 3, key = tile * 16 + r;
-  const uint32_t at = (uint32_t)(key * (int)ldk * 2) + g * 16;
+  const uint32_t at = (uint32_t)(key * (int)ldk * 2);
   const bf16_t* own = (dk_role ? p.v : p.k) + kv0;
   bf16_t* out = (dk_role ? p.dk : p.dv) + kv0;
-  const char *score_rows = dk_role ? dt : qt, *sum_rows = dk_role ? qt : dt;
+  const uint32_t score_rows = dk_role ? dt : qt, sum_rows = dk_role ? qt : dt;
 
   State<D> s;
   if (p.seg) s.load(p.seg + (int64_t)id * D * D, wave, lane);
@@ -672,91 +701,88 @@ __device__ __forceinline__ void segment_keys(const LinearArgs& p, int id, char* 
   const float log2 = uniform(log2_decay(p.log_decay[j]));
   const Decay whole = decay_of(p.log_decay[j], kChunk);
   weights_from_start(w, log2, p.scale, 0);
-  const Decays decays(log2, p.scale, g * 4 - r, 1);
-  f32x4 acc[NB];
-  bf16x8 kf[KS];
-  for (int it = 0; it < chunks * G; ++it) {
-    const int c = chunks - 1 - it / G, h = it % G, rows = min(m - c * kChunk, kChunk);
+  const Decays<1> decays(log2, p.scale);
+  const uint32_t along_lane = Rows<D>::along_lane(lds_address(smem), lane), columns_lane = Rows<D>::columns_lane(lds_address(smem), lane);
+  for (int c = chunks - 1; c >= 0; --c) {
+    const int rows = min(m - c * kChunk, kChunk);
     const int64_t kc = (int64_t)c * kChunk * ldk;
-    const int64_t from = q0 + (int64_t)c * kChunk * ldq + (int64_t)h * D;
-    __syncthreads();
-    tile_to_lds<D>(rows_rsrc<D>(p.q + from, ldq, rows), qt, ldq, wave, lane);
-    tile_to_lds<D>(rows_rsrc<D>(p.d_o + from, ldq, rows), dt, ldq, wave, lane);
-    if (h == 0) {
-      const __amdgpu_buffer_rsrc_t rk = rows_rsrc<D>(own + kc, ldk, rows);
-#pragma unroll
-      for (int k = 0; k < KS; ++k) kf[k] = load8(rk, at + k * 64);
-    }
-    if (h == 0 && some) {
+    const bool more = c > 0 || (!p.seg && p.s_out);
+    const bool into = some;
+    auto bring = [&](int h) {   // the head's queries and do, once nobody works with what is there
+      const int64_t from = q0 + (int64_t)c * kChunk * ldq + (int64_t)h * D;
+      __syncthreads();
+      tile_to_lds<D>(rows_rsrc<D>(p.q + from, ldq, rows), smem + qt, ldq, wave, lane);
+      tile_to_lds<D>(rows_rsrc<D>(p.d_o + from, ldq, rows), smem + dt, ldq, wave, lane);
+    };
+    bring(0);
+    if (into) {
       const Scale sc = state_scale(largest);
       down = sc.down;
-      s.to_lds(et, sc.up, wave, lane);
+      s.to_lds(smem + et, sc.up, wave, lane);
     }
+    const __amdgpu_buffer_rsrc_t rk = rows_rsrc<D>(own + kc, ldk, rows);
+    bf16x8 kf[KS];
+#pragma unroll
+    for (int k = 0; k < KS; ++k) kf[k] = load8(rk, at + k * 64 + g * 16);
     loads_done();
-    if (h == 0) {
+    f32x4 acc[NB];
 #pragma unroll
-      for (int n = 0; n < NB; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (some) {
-        const ScaledRow<KS> ks(kf);
-        const int lane = here(threadIdx.x & 63);
-        if (!dk_role) {
+    for (int n = 0; n < NB; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (into) {
+      const ScaledRow<KS> ks(kf);
+      if (!dk_role) {
+        const uint32_t al = here(along_lane);
 #pragma unroll
-          for (int k = 0; k < KS; ++k)
+        for (int k = 0; k < KS; ++k)
 #pragma unroll
-            for (int n = 0; n < NB; ++n) acc[n] = mfma16_f16(__builtin_bit_cast(f16x8, Rows<D>::along(et, n * 16, k, lane)), ks.v[k], acc[n]);
-        } else {
-          // E's columns along keys in stored order; its rows as they lie are along values in the order of the operand
+          for (int n = 0; n < NB; ++n) acc[n] = mfma16_f16(__builtin_bit_cast(f16x8, Rows<D>::along(al, et, n * 16, k)), ks.v[k], acc[n]);
+      } else {
+        const uint32_t cl = Rows<D>::template columns_lane<4>(lds_address(smem), here(lane));
 #pragma unroll
-          for (int k = 0; k < KS; ++k)
+        for (int k = 0; k < KS; ++k)
 #pragma unroll
-            for (int n = 0; n < NB; ++n)
-              acc[n] = mfma16_f16(__builtin_bit_cast(f16x8, Rows<D>::columns_stored(et, n, k * 32, lane)), ks.v[k], acc[n]);
+          for (int n = 0; n < NB; ++n)
+            acc[n] = mfma16_f16(__builtin_bit_cast(f16x8, Rows<D>::template columns<4>(cl, et, n, k * 32)), ks.v[k], acc[n]);
+      }
+      const float left = power(here(log2), max(rows - 1 - key, 0)) * down * ks.down;
+#pragma unroll
+      for (int n = 0; n < NB; ++n) acc[n] *= left;
+    }
+    if (more) s.template decay<SPLIT == 3>(rows == kChunk ? whole : Decay{power(log2, rows), 0.f});
+    for (int h = 0; h < G; ++h) {
+      if (h > 0) {
+        bring(h);
+        loads_done();
+      }
+#pragma unroll
+      for (int pr = 0; pr < 2; ++pr) {
+        if (2 * pr + 1 < tile) continue;
+        const uint32_t al = here(along_lane + score_rows), cl = here(columns_lane + sum_rows);
+        f32x4 sc[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int blk = 2 * pr + i;
+          sc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+          if (blk < tile) continue;
+#pragma unroll
+          for (int k = 0; k < KS; ++k) sc[i] = mfma16(Rows<D>::along(al, 0, blk * 16, k), kf[k], sc[i]);
+          decays.apply(sc[i], blk - tile, lane);
         }
-        const float left = power(here(log2), max(rows - 1 - key, 0)) * down * ks.down;
+        const Scores pf(sc);
 #pragma unroll
-        for (int n = 0; n < NB; ++n) acc[n] *= left;
+        for (int n = 0; n < NB; ++n) acc[n] = pf.times(Rows<D>::columns(cl, 0, n, pr * 32), acc[n]);
       }
+      if (more) s.template add<SPLIT>(qt, dt, w, wave, lane, columns_lane);
     }
-#pragma unroll
-    for (int pr = 0; pr < 2; ++pr) {
-      if (2 * pr + 1 < tile) continue;
-      const int lane = here(threadIdx.x & 63), r = lane & 15, g = lane >> 4;
-      f32x4 sc[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int blk = 2 * pr + i;
-        sc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (blk < tile) continue;
-#pragma unroll
-        for (int k = 0; k < KS; ++k) sc[i] = mfma16(Rows<D>::along(score_rows, blk * 16, k, lane), kf[k], sc[i]);
-        decays.apply(sc[i], blk - tile, [&](int e) { return g * 4 + e >= r; });
-      }
-      const Scores pf(sc);
-#pragma unroll
-      for (int n = 0; n < NB; ++n) acc[n] = pf.times(Rows<D>::columns_stored(sum_rows, n, pr * 32, lane), acc[n]);
-    }
-    if (c > 0 || (!p.seg && p.s_out)) {
-      if (h == 0) s.decay(rows == kChunk ? whole : Decay{power(log2, rows), 0.f});
-      s.template add<SPLIT>(qt, dt, w, wave, lane);
-      some = true;
-      if (h == G - 1 && c > 0) largest[wave] = s.largest(wave);
-    }
-    if (h == G - 1) {
-      const __amdgpu_buffer_rsrc_t ro = rows_rsrc<D>(out + kc, ldk, min(rows_all - c * kChunk, kChunk));
-#pragma unroll
-      for (int n = 0; n < NB; n += 2) {
-        bf16x8 v;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = (bf16_t)(key < rows ? acc[n + (e >> 2)][e & 3] : 0.f);
-        store8(ro, at + n * 32, v);
-      }
-    }
+    some = some || more;
+    if (c > 0) largest[wave] = s.largest(wave);
+    store_row<NB>(rows_rsrc<D>(out + kc, ldk, min(rows_all - c * kChunk, kChunk)), at, acc, rows == kChunk, key < rows, lane);
   }
   const bf16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
   for (int c = chunks; c * kChunk < rows_all; ++c) {
     const __amdgpu_buffer_rsrc_t ro = rows_rsrc<D>(out + (int64_t)c * kChunk * ldk, ldk, min(rows_all - c * kChunk, kChunk));
 #pragma unroll
-    for (int n = 0; n < NB; n += 2) store8(ro, at + n * 32, zero);
+    for (int n = 0; n < NB; n += 2) store8(ro, at + n * 32 + g * 16, zero);
   }
   if (!p.seg && p.s_out) s.store_matrix(p.s_out + (int64_t)pair * D * D, wave, lane);
 }
