@@ -823,10 +823,10 @@ constexpr int kLinearBlocks = 512;   // workgroups that fill the chip: two on ea
 
 // Segments of a sequence, a whole number of chunks each: as many as make kLinearBlocks workgroups, of two chunks at the least.
 struct LinearPlan { int seg_chunks, nseg; };
-static LinearPlan linear_plan(int64_t pairs, int64_t S) {
+static LinearPlan linear_plan(int64_t pairs, int64_t S, int64_t blocks) {
   LinearPlan p;
   const int64_t chunks = (S + kChunk - 1) / kChunk;
-  int64_t n = (kLinearBlocks + pairs - 1) / pairs;
+  int64_t n = (blocks + pairs - 1) / pairs;
   if (n > chunks / 2) n = chunks / 2;
   if (n < 1) n = 1;
   p.seg_chunks = (int)((chunks + n - 1) / n);
@@ -834,8 +834,8 @@ static LinearPlan linear_plan(int64_t pairs, int64_t S) {
   return p;
 }
 // parts into which the heads of a group are dealt where there are few segments
-static int linear_parts(int64_t segments, int64_t G) {
-  const int64_t n = (kLinearBlocks + segments - 1) / segments;
+static int linear_parts(int64_t segments, int64_t G, int64_t blocks) {
+  const int64_t n = (blocks + segments - 1) / segments;
   return (int)(n < G ? n : G);
 }
 // room for the states of all segments: below twice kLinearBlocks of them, and a size that does not fall as the call grows
@@ -847,8 +847,8 @@ static size_t segment_bytes(int64_t pairs, int64_t S, int64_t dh) {
 size_t linear_attention_fwd_workspace(int64_t B, int64_t S, int64_t Hq, int64_t Hkv, int64_t dh) { return segment_bytes(B * Hkv, S, dh); }
 size_t linear_attention_bwd_workspace(int64_t B, int64_t S, int64_t Hq, int64_t Hkv, int64_t dh) { return 2 * segment_bytes(B * Hkv, S, dh); }
 
-static LinearArgs linear_args(const LinearCall& c) {
-  const LinearPlan plan = linear_plan(c.B * c.Hkv, c.S);
+static LinearArgs linear_args(const LinearCall& c, int64_t blocks) {
+  const LinearPlan plan = linear_plan(c.B * c.Hkv, c.S, blocks);
   LinearArgs a{};
   a.q = (const bf16_t*)c.q; a.k = (const bf16_t*)c.k; a.v = (const bf16_t*)c.v;
   a.log_decay = c.log_decay; a.lengths = c.lengths;
@@ -879,7 +879,7 @@ static int launch_out(const LinearArgs& a, int64_t segments, int parts, hipStrea
 template <int D>
 static int run_forward(LinearArgs a, int64_t pairs, float* workspace, hipStream_t st) {
   const int64_t segments = pairs * a.nseg;
-  const int parts = linear_parts(segments, a.Hq / a.Hkv);
+  const int parts = linear_parts(segments, a.Hq / a.Hkv, kLinearBlocks);
   if (a.nseg > 1 || (parts > 1 && a.s_out)) {
     a.seg = workspace;
     if (int rc = run_states<D>(a, nullptr, pairs, st)) return rc;
@@ -898,7 +898,7 @@ static int launch_grad(const LinearArgs& a, const LinearArgs& g, int64_t segment
 template <int D>
 static int run_backward(LinearArgs a, LinearArgs g, int64_t pairs, float* workspace, hipStream_t st) {
   const int64_t segments = pairs * a.nseg;
-  const int parts = linear_parts(segments, a.Hq / a.Hkv);
+  const int parts = linear_parts(segments, a.Hq / a.Hkv, kLinearBlocks / 2);
   if (a.nseg > 1) {
     a.seg = workspace;
     g.seg = workspace + segments * D * D;
@@ -909,7 +909,7 @@ static int run_backward(LinearArgs a, LinearArgs g, int64_t pairs, float* worksp
 }
 
 int launch_linear_attention_fwd(const LinearCall& c, const float* s_in, void* o, float* s_out, void* workspace, hipStream_t st) {
-  LinearArgs a = linear_args(c);
+  LinearArgs a = linear_args(c, kLinearBlocks);
   a.o = (bf16_t*)o; a.s_in = s_in; a.s_out = s_out;
   const int64_t pairs = c.B * c.Hkv;
   float* ws = (float*)workspace;
@@ -919,7 +919,7 @@ int launch_linear_attention_fwd(const LinearCall& c, const float* s_in, void* o,
 int launch_linear_attention_bwd(const LinearCall& c, const float* s_in, const void* d_o, const float* ds_out, void* dq, void* dk, void* dv,
                                 float* ds_in, void* workspace, hipStream_t st) {
   // dq is the forward's o of (d_o, v, k) and the transposed state
-  LinearArgs a = linear_args(c), g = a;
+  LinearArgs a = linear_args(c, kLinearBlocks / 2), g = a;
   a.q = (const bf16_t*)d_o; a.k = (const bf16_t*)c.v; a.v = (const bf16_t*)c.k;
   a.o = (bf16_t*)dq; a.s_in = s_in; a.flip = 1;
   g.d_o = (const bf16_t*)d_o; g.dk = (bf16_t*)dk; g.dv = (bf16_t*)dv; g.s_in = ds_out; g.s_out = ds_in;
