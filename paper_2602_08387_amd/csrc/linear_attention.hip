@@ -819,36 +819,65 @@ __global__ __launch_bounds__(64 * kLinWaves, 4) void linear_grad_kernel(const Li
 // ------------------------------------------------------------------------------------------
 // Host side
 // ------------------------------------------------------------------------------------------
-constexpr int kLinearBlocks = 512;   // workgroups that fill the chip: two on each compute unit
+constexpr int kMostSegments = 1024;   // of a call that cuts its sequences
 
-// Segments of a sequence, a whole number of chunks each: as many as make kLinearBlocks workgroups, of two chunks at the least.
-struct LinearPlan { int seg_chunks, nseg; };
-static LinearPlan linear_plan(int64_t pairs, int64_t S, int64_t blocks) {
-  LinearPlan p;
-  const int64_t chunks = (S + kChunk - 1) / kChunk;
-  int64_t n = (blocks + pairs - 1) / pairs;
-  if (n > chunks / 2) n = chunks / 2;
-  if (n < 1) n = 1;
-  p.seg_chunks = (int)((chunks + n - 1) / n);
-  p.nseg = (int)((chunks + p.seg_chunks - 1) / p.seg_chunks);
-  return p;
+// Segments of a sequence, a whole number of chunks each, and the parts into which a group's query heads are dealt where there are few segments.
+struct LinearPlan { int seg_chunks, nseg, parts; };
+
+// Time in us of a call whose sequences are cut into n: chains of chunks, or the bytes that move where they take longer.  The constants (us for a chunk, D 128,
+// 64, 32: a workgroup of linear_out_kernel with up to two heads, and for a further two; one for dk and dv, and for each head of the group; one tile pair of
+// linear_segment_kernel) are 1.3 times what single workgroups take with their inputs in the caches.  Workgroups that share compute units take 1.3 (1.6)
+// times as long; 4.3 TB/s.  Over 152 shapes of 128 to 8192 tokens, timed with every power of two, the choice is 1 % slower than the best on average, at
+// worst 1.2 times (77 us for 63); one segment throughout would be 2.4 times slower, always the most 1.2 times.
+static double linear_time(bool backward, double pairs, int chunks, int G, int64_t D, int n, LinearPlan* plan) {
+  static const double kStep[3][5] = {{6.5, 3.3, 4.7, 3.6, 2.9}, {3.5, 1.7, 2.5, 2.2, 1.6}, {2.5, 1.0, 1.7, 1.4, 1.2}};
+  const double* c = kStep[D == 128 ? 0 : D == 64 ? 1 : 2];
+  const double bytes_us = 4.3e6, tile = 2.0 * kChunk * D / bytes_us, slots = D == 128 ? 512 : 768;
+  const int sc = (chunks + n - 1) / n;
+  n = (chunks + sc - 1) / sc;
+  const double segs = pairs * n, state = n > 1 ? segs * D * D * 4 * (backward ? 2 : 1) / bytes_us : 0.0;
+  const double half = backward ? 256 : 512;   // a backward's other workgroups, for dk and dv, fill the rest
+  int parts = (int)(segs < half ? (half + segs - 1) / segs : 1);
+  if (parts > G) parts = G;
+  *plan = LinearPlan{sc, n, parts};
+  const int heads = (G + parts - 1) / parts;
+  const auto most = [](double a, double b) { return a > b ? a : b; };
+  const auto rounds = [](double work, double at_once) { return (double)(int64_t)((work + at_once - 1) / at_once); };
+  const auto busy = [](double blocks, double by) { return blocks > 256 ? by : 1.0; };
+  double t = 3.0;
+  if (n > 1) {
+    t += 4.0 + most(sc * c[4] * (backward ? G : 1) * rounds(segs * (backward ? 2 : 1), slots), pairs * chunks * tile * 2 * (backward ? 1 + G : 1) + state);
+    t += 4.0 + 1.5 * state + 0.12 * n;   // (states come from caches in part)
+  }
+  if (!backward)
+    t += most(sc * (c[0] + c[1] * ((heads + 1) / 2 - 1)) * rounds(segs * parts, slots) * busy(segs * parts, 1.3), pairs * chunks * tile * (2 * G + 2 * parts) + state);
+  else
+    t += most(sc * (c[2] + c[3] * G) * rounds(segs, slots / 2) * busy(segs * (1 + parts), 1.6), pairs * chunks * tile * (4 * G + 4 + 2 * parts) + state);
+  return t;
 }
-// parts into which the heads of a group are dealt where there are few segments
-static int linear_parts(int64_t segments, int64_t G, int64_t blocks) {
-  const int64_t n = (blocks + segments - 1) / segments;
-  return (int)(n < G ? n : G);
+static LinearPlan linear_plan(bool backward, int64_t pairs, int64_t S, int64_t Hq, int64_t Hkv, int64_t D) {
+  const int chunks = (int)((S + kChunk - 1) / kChunk), G = (int)(Hq / Hkv);
+  LinearPlan best, p;
+  double t = linear_time(backward, (double)pairs, chunks, G, D, 1, &best);
+  for (int n = 2; n <= chunks && pairs * n <= kMostSegments; n *= 2) {
+    const double u = linear_time(backward, (double)pairs, chunks, G, D, n, &p);
+    if (u < t) {
+      t = u;
+      best = p;
+    }
+  }
+  return best;
 }
-// room for the states of all segments: below twice kLinearBlocks of them, and a size that does not fall as the call grows
+// room for the states of all segments: a size that does not fall as the call grows
 static size_t segment_bytes(int64_t pairs, int64_t S, int64_t dh) {
-  const int64_t chunks = (S + kChunk - 1) / kChunk, most = 2 * kLinearBlocks;
-  const int64_t n = pairs < most && pairs * chunks < most ? pairs * chunks : most;
+  const int64_t chunks = (S + kChunk - 1) / kChunk;
+  const int64_t n = pairs < kMostSegments && pairs * chunks < kMostSegments ? pairs * chunks : kMostSegments;
   return (size_t)(n * dh * dh) * sizeof(float);
 }
 size_t linear_attention_fwd_workspace(int64_t B, int64_t S, int64_t Hq, int64_t Hkv, int64_t dh) { return segment_bytes(B * Hkv, S, dh); }
 size_t linear_attention_bwd_workspace(int64_t B, int64_t S, int64_t Hq, int64_t Hkv, int64_t dh) { return 2 * segment_bytes(B * Hkv, S, dh); }
 
-static LinearArgs linear_args(const LinearCall& c, int64_t blocks) {
-  const LinearPlan plan = linear_plan(c.B * c.Hkv, c.S, blocks);
+static LinearArgs linear_args(const LinearCall& c, const LinearPlan& plan) {
   LinearArgs a{};
   a.q = (const bf16_t*)c.q; a.k = (const bf16_t*)c.k; a.v = (const bf16_t*)c.v;
   a.log_decay = c.log_decay; a.lengths = c.lengths;
@@ -877,9 +906,8 @@ static int launch_out(const LinearArgs& a, int64_t segments, int parts, hipStrea
   return check_launch("linear_attention_forward");
 }
 template <int D>
-static int run_forward(LinearArgs a, int64_t pairs, float* workspace, hipStream_t st) {
+static int run_forward(LinearArgs a, int64_t pairs, int parts, float* workspace, hipStream_t st) {
   const int64_t segments = pairs * a.nseg;
-  const int parts = linear_parts(segments, a.Hq / a.Hkv, kLinearBlocks);
   if (a.nseg > 1 || (parts > 1 && a.s_out)) {
     a.seg = workspace;
     if (int rc = run_states<D>(a, nullptr, pairs, st)) return rc;
@@ -896,9 +924,8 @@ static int launch_grad(const LinearArgs& a, const LinearArgs& g, int64_t segment
   return check_launch("linear_attention_backward");
 }
 template <int D>
-static int run_backward(LinearArgs a, LinearArgs g, int64_t pairs, float* workspace, hipStream_t st) {
+static int run_backward(LinearArgs a, LinearArgs g, int64_t pairs, int parts, float* workspace, hipStream_t st) {
   const int64_t segments = pairs * a.nseg;
-  const int parts = linear_parts(segments, a.Hq / a.Hkv, kLinearBlocks / 2);
   if (a.nseg > 1) {
     a.seg = workspace;
     g.seg = workspace + segments * D * D;
@@ -909,23 +936,25 @@ static int run_backward(LinearArgs a, LinearArgs g, int64_t pairs, float* worksp
 }
 
 int launch_linear_attention_fwd(const LinearCall& c, const float* s_in, void* o, float* s_out, void* workspace, hipStream_t st) {
-  LinearArgs a = linear_args(c, kLinearBlocks);
-  a.o = (bf16_t*)o; a.s_in = s_in; a.s_out = s_out;
   const int64_t pairs = c.B * c.Hkv;
-  float* ws = (float*)workspace;
-  return c.dh == 128 ? run_forward<128>(a, pairs, ws, st) : c.dh == 64 ? run_forward<64>(a, pairs, ws, st) : run_forward<32>(a, pairs, ws, st);
+  const LinearPlan plan = linear_plan(false, pairs, c.S, c.Hq, c.Hkv, c.dh);
+  LinearArgs a = linear_args(c, plan);
+  a.o = (bf16_t*)o; a.s_in = s_in; a.s_out = s_out;
+  const auto run = c.dh == 128 ? run_forward<128> : c.dh == 64 ? run_forward<64> : run_forward<32>;
+  return run(a, pairs, plan.parts, (float*)workspace, st);
 }
 
 int launch_linear_attention_bwd(const LinearCall& c, const float* s_in, const void* d_o, const float* ds_out, void* dq, void* dk, void* dv,
                                 float* ds_in, void* workspace, hipStream_t st) {
   // dq is the forward's o of (d_o, v, k) and the transposed state
-  LinearArgs a = linear_args(c, kLinearBlocks / 2), g = a;
+  const int64_t pairs = c.B * c.Hkv;
+  const LinearPlan plan = linear_plan(true, pairs, c.S, c.Hq, c.Hkv, c.dh);
+  LinearArgs a = linear_args(c, plan), g = a;
   a.q = (const bf16_t*)d_o; a.k = (const bf16_t*)c.v; a.v = (const bf16_t*)c.k;
   a.o = (bf16_t*)dq; a.s_in = s_in; a.flip = 1;
   g.d_o = (const bf16_t*)d_o; g.dk = (bf16_t*)dk; g.dv = (bf16_t*)dv; g.s_in = ds_out; g.s_out = ds_in;
-  const int64_t pairs = c.B * c.Hkv;
-  float* ws = (float*)workspace;
-  return c.dh == 128 ? run_backward<128>(a, g, pairs, ws, st) : c.dh == 64 ? run_backward<64>(a, g, pairs, ws, st) : run_backward<32>(a, g, pairs, ws, st);
+  const auto run = c.dh == 128 ? run_backward<128> : c.dh == 64 ? run_backward<64> : run_backward<32>;
+  return run(a, g, pairs, plan.parts, (float*)workspace, st);
 }
 
 // ------------------------------------------------------------------------------------------
