@@ -300,7 +300,8 @@ int embed_backward(const void* dx0, const int64_t* ids, int64_t T, int64_t V, in
  *             padding: nothing there is read for any result, whatever it holds, and outputs and gradients there are written as 0.
  *   start     position of each row's first token (NULL: 0).  A row that is generated token by token has seq = 1 and start = the
  *             tokens before it.
- * batch and seq are any positive numbers; head_dim 32, 64 or 128; tensors may exceed 4 GiB.
+ * batch and seq are any positive numbers (batch * n_kv_heads of linear attention below 2^22); head_dim 32, 64 or 128; tensors may
+ * exceed 4 GiB.  The sizes of workspaces do not fall as batch or seq grows.
  * ------------------------------------------------------------------------------------------ */
 
 /* RMS norm of every query and key head, then the rotary embedding:
@@ -333,7 +334,8 @@ int qk_norm_rope_backward(const void* q, const void* k, const void* gamma_q, con
  * q, o [B*S, Hq, dh], k, v [B*S, Hkv, dh] bf16; log_decay [Hkv] f32 on the device, not above 0 (0: nothing is forgotten,
  * minus infinity: nothing is remembered), a constant of the model: it gets no gradient.  State in and out [B, Hkv, dh, dh] f32:
  * state_in NULL for zeros, state_out (the state after a row's last token) NULL if not wanted; state_out may alias state_in.
- * Sequences are worked on in chunks on the matrix units, the states between them are fp32.
+ * Sequences are worked on in chunks of 64 tokens on the matrix units, the states between them are fp32.  A value of a row that is not
+ * finite (padding aside) may show in the results of every token of its chunk, not only of those that the sums above name.
  * workspace: linear_attention_workspace_bytes(...).                                                          */
 size_t linear_attention_workspace_bytes(int64_t batch, int64_t seq, int64_t n_q_heads, int64_t n_kv_heads,
                                         int64_t head_dim);

@@ -658,8 +658,8 @@ static int linear_shape_ok(const char* who, int64_t batch, int64_t seq, int64_t 
   REQUIRE(batch > 0 && seq > 0 && Hq > 0 && Hkv > 0, "%s: non-positive dimension", who);
   REQUIRE(dh == 32 || dh == 64 || dh == 128, "%s: head_dim must be 32, 64 or 128", who);
   REQUIRE(Hq % Hkv == 0, "%s: n_q_heads must be a multiple of n_kv_heads", who);
-  REQUIRE(batch < ((int64_t)1 << 24) && seq < ((int64_t)1 << 30) && Hq < 65536 && batch * Hkv < ((int64_t)1 << 24),
-          "%s: batch, seq or head count too large", who);
+  REQUIRE(batch < ((int64_t)1 << 22) && seq < ((int64_t)1 << 30) && Hq < 65536 && batch * Hkv < ((int64_t)1 << 22),
+          "%s: batch, seq or head count too large", who);   // a launch holds fewer than 2^32 threads: 2 * 512 for a row's KV head
   return 0;
 }
 

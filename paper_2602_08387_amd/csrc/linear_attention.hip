@@ -839,8 +839,9 @@ static double linear_time(bool backward, double pairs, int chunks, int G, int64_
   const double half = backward ? 256 : 512;   // a backward's other workgroups, for dk and dv, fill the rest
   int parts = (int)(segs < half ? (half + segs - 1) / segs : 1);
   if (parts > G) parts = G;
-  *plan = LinearPlan{sc, n, parts};
   const int heads = (G + parts - 1) / parts;
+  parts = (G + heads - 1) / heads;   // none without a head
+  *plan = LinearPlan{sc, n, parts};
   const auto most = [](double a, double b) { return a > b ? a : b; };
   const auto rounds = [](double work, double at_once) { return (double)(int64_t)((work + at_once - 1) / at_once); };
   const auto busy = [](double blocks, double by) { return blocks > 256 ? by : 1.0; };

@@ -228,8 +228,11 @@ int launch_qk_norm_rope_fwd(const QkNormCall& c, float eps, void* q_out, void* k
   return check_launch("qk_norm_rope_forward");
 }
 
+// the most that a plan of so many tokens, or fewer, has: a size that does not fall as the call grows
 size_t qk_norm_rope_bwd_workspace(int64_t tokens, int64_t Hq, int64_t Hkv, int64_t dh) {
-  return (size_t)qk_plan(tokens, Hq, Hkv, dh).blocks * 2 * dh * sizeof(float);
+  const QkPlan p = qk_plan(1, Hq, Hkv, dh);
+  const int64_t waves = tokens * (p.groups[0] + p.groups[1]), blocks = (waves + kQkWaves - 1) / kQkWaves;
+  return (size_t)(blocks < kQkMostBlocks ? blocks : kQkMostBlocks) * 2 * dh * sizeof(float);
 }
 
 int launch_qk_norm_rope_bwd(const QkNormCall& c, const void* dq_out, const void* dk_out, void* dq, void* dk, void* dgamma_q,
