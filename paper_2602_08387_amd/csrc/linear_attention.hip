@@ -50,7 +50,8 @@ __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __
 
 // A value that the compiler works with from here on only: without this it keeps what it can derive from the lane's number and the decay
 // (LDS addresses, powers) for every phase of a loop in registers throughout, a hundred more than there are, and reloads them from scratch
-// memory in every iteration.
+// memory in every iteration.  (Such a register costs bandwidth too: the 8 that linear_out_kernel<128> once spilled in every chunk were half as
+// many bytes to HBM as o itself, 403 MB for 268 at 65536 tokens of 16 heads, and 202 us for 185.)
 template <typename T>
 __device__ __forceinline__ T here(T x) {
   asm volatile("" : "+v"(x));
@@ -388,6 +389,7 @@ struct Decays {
   __device__ __forceinline__ Decays(float log2_, float mult_)
       : log2(log2_), mult(mult_), p1(uniform(power(log2_, 1))), p2(uniform(power(log2_, 2))), p3(uniform(power(log2_, 3))),
         p16(uniform(power(log2_, 16))), p32(uniform(power(log2_, 32))) {}
+  // (With a state of 128 x 128 no register is left for what a lane derives from its number and keeps: the caller passes here(lane).)
   // blocks: from the key's to the query's, 0 .. 3; within the diagonal block what is not causal becomes 0
   __device__ __forceinline__ void apply(f32x4& s, int blocks, int lane) const {
     const int first = STEP * (((lane >> 4) << 2) - (lane & 15));   // of the lane's four differences within 16
@@ -404,6 +406,26 @@ struct Decays {
     }
   }
 };
+
+// o[n] += factor times the product of a(n, k) with the scaled row, for NB blocks, four in turn
+template <int KS, int NB, typename F>
+__device__ __forceinline__ void add_scaled(f32x4 (&o)[NB], const ScaledRow<KS>& x, float factor, F&& a) {
+  constexpr int AT_ONCE = NB < 4 ? NB : 4;
+#pragma unroll
+  for (int n0 = 0; n0 < NB; n0 += AT_ONCE) {
+    f32x4 t[AT_ONCE];
+#pragma unroll
+    for (int n = 0; n < AT_ONCE; ++n) t[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int n = 0; n < AT_ONCE; ++n) t[n] = mfma16_f16(__builtin_bit_cast(f16x8, a(n0 + n, k)), x.v[k], t[n]);
+#pragma unroll
+    for (int n = 0; n < AT_ONCE; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[n0 + n][e] = __builtin_fmaf(t[n][e], factor, o[n0 + n][e]);
+  }
+}
 
 // Weighted scores of 32 tokens as an operand: the sum of two bf16.
 struct Scores {
@@ -567,20 +589,8 @@ __device__ __forceinline__ void out_tile(f32x4 (&o)[NB], const bf16x8 (&qf)[D / 
                                          float down, int tile, int n0, float log2, float scale, const Decays<-1>& ds, int lane, uint32_t along_lane, uint32_t columns_lane) {
   constexpr int KS = D / 32, kt = 0, vt = kChunk * D * 2, st = 2 * kChunk * D * 2;
   const uint32_t al = here(along_lane), sl = here(along_lane + (uint32_t)(n0 * 16 * D * 2)), cl = here(columns_lane ^ (uint32_t)(n0 << 5));
-  const int r = lane & 15;
-#pragma unroll
+  #pragma unroll
   for (int n = 0; n < NB; ++n) o[n] = f32x4{0.f, 0.f, 0.f, 0.f};
-  if (some) {
-    const ScaledRow<KS> qs(qf);
-#pragma unroll
-    for (int k = 0; k < KS; ++k)
-#pragma unroll
-      for (int n = 0; n < NB; ++n)
-        o[n] = mfma16_f16(__builtin_bit_cast(f16x8, Rows<D>::along(sl, st, n * 16, k)), qs.v[k], o[n]);
-    const float after = power(log2, tile * 16 + r + 1) * scale * down * qs.down;
-#pragma unroll
-    for (int n = 0; n < NB; ++n) o[n] *= after;
-  }
 #pragma unroll
   for (int pr = 0; pr < 2; ++pr) {
     if (2 * pr > tile) break;
@@ -592,10 +602,15 @@ __device__ __forceinline__ void out_tile(f32x4 (&o)[NB], const bf16x8 (&qf)[D / 
       if (blk > tile) continue;
 #pragma unroll
       for (int k = 0; k < KS; ++k) sc[i] = mfma16(Rows<D>::along(al, kt, blk * 16, k), qf[k], sc[i]);
-      ds.apply(sc[i], tile - blk, lane);
+      ds.apply(sc[i], tile - blk, D == 128 ? here(lane) : lane);
     }
     const Scores pf(sc);
     pf.times(o, [&](int n) { return Rows<D>::columns(cl, vt, n, pr * 32); });
+  }
+  if (some) {   // last, when the queries as they are need no registers any more
+    const ScaledRow<KS> qs(qf);
+    const float after = power(log2, tile * 16 + (here(lane) & 15) + 1) * scale * down * qs.down;
+    add_scaled<KS>(o, qs, after, [&](int n, int k) { return Rows<D>::along(sl, st, n * 16, k); });
   }
 }
 
@@ -784,7 +799,7 @@ __device__ __forceinline__ void segment_keys(const LinearArgs& p, int id, char* 
           if (blk < tile) continue;
 #pragma unroll
           for (int k = 0; k < KS; ++k) sc[i] = mfma16(Rows<D>::along(al, 0, blk * 16, k), kf[k], sc[i]);
-          decays.apply(sc[i], blk - tile, lane);
+          decays.apply(sc[i], blk - tile, D == 128 ? here(lane) : lane);
         }
         const Scores pf(sc);
         pf.times(acc, [&](int n) { return Rows<D>::columns(cl, 0, n, pr * 32); });
