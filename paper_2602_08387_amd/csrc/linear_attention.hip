@@ -221,7 +221,7 @@ __device__ __forceinline__ void store_row(__amdgpu_buffer_rsrc_t rs, uint32_t ro
 
 __device__ __forceinline__ float uniform(float x) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x))); }
 
-// Weights of a chunk's tokens, in LDS: on their way into the state after the chunk's `rows` tokens, lambda^(rows-1-t), and into the gradient of the
+// Weights of a chunk's tokens, in LDS: on their way into the state after `rows` tokens from the chunk's first, lambda^(rows-1-t), and into the gradient of the
 // state `before` tokens before the chunk, mult lambda^(before+t+1).  (Sixteen registers would hold a lane's, and are not there.)
 __device__ __forceinline__ void weights_to_end(float* w, float log2, int rows) {
   if (threadIdx.x < kChunk) w[threadIdx.x] = power(log2, max(rows - 1 - (int)threadIdx.x, 0));
@@ -478,7 +478,7 @@ __device__ __forceinline__ float log2_decay(float g) { return (float)(decay_log(
 // What a segment of m tokens adds to the state that passes through it: sum_t lambda^(m-1-t) k_t v_t^T, from k and v;
 // GRADIENT: to the state's gradient, sum over t and the group's heads of scale lambda^(t+1) q_t do_t^T, from q and d_o.
 // ------------------------------------------------------------------------------------------
-template <int D, bool GRADIENT>
+template <int D, int SPLIT, bool GRADIENT>
 __device__ __forceinline__ void segment_sum(const LinearArgs& p, char* smem) {
   constexpr int xt = 0, yt = kChunk * D * 2;
   float* w = reinterpret_cast<float*>(smem + 2 * kChunk * D * 2);
@@ -498,7 +498,6 @@ __device__ __forceinline__ void segment_sum(const LinearArgs& p, char* smem) {
   const bf16_t *x = GRADIENT ? p.q : p.k, *y = GRADIENT ? p.d_o : p.v;
   const int64_t first = ((int64_t)b * p.S + t0) * ld + (int64_t)j * G * D;
   const float log2 = log2_decay(p.log_decay[j]);
-  const Decay whole = decay_of(p.log_decay[j], kChunk);
   const uint32_t columns_lane = Rows<D>::columns_lane(lds_address(smem), lane);
   Staged<D> xs, ys;
   auto fetch = [&](int it) {
@@ -509,28 +508,26 @@ __device__ __forceinline__ void segment_sum(const LinearArgs& p, char* smem) {
   };
   fetch(0);
   for (int it = 0; it < items; ++it) {
-    const int c = it / G, rows = min(m - c * kChunk, kChunk);
+    const int c = it / G;
     __syncthreads();
     xs.store(smem + xt);
     ys.store(smem + yt);
-    if (GRADIENT) {
-      if (it % G == 0) weights_from_start(w, log2, p.scale, c * kChunk);
-    } else if (c == 0 || rows < kChunk) {
-      weights_to_end(w, log2, rows);
-    }
+    if (!GRADIENT) weights_to_end(w, log2, m - c * kChunk);
+    else if (it % G == 0) weights_from_start(w, log2, p.scale, c * kChunk);
     __syncthreads();
     if (it + 1 < items) fetch(it + 1);
-    if (!GRADIENT && c > 0) s.template decay<true>(rows == kChunk ? whole : Decay{power(log2, rows), 0.f});
-    s.template add<3>(xt, yt, w, wave, lane, columns_lane);
+    s.template add<SPLIT>(xt, yt, w, wave, lane, columns_lane);
   }
   s.store(out, wave, lane);
 }
-// y 0: the states, of `a`; 1: their gradients, of `g`
-template <int D>
+// y 0: the states, of `a`; 1: their gradients, of `g`.  What may reach the caller (the forward's states, the backward's gradients) is summed with three
+// terms, whether the caller asked for it or not, so that no other result depends on that; the states of a backward serve dq alone.
+template <int D, bool BACKWARD>
 __global__ __launch_bounds__(64 * kLinWaves, 4) void linear_segment_kernel(const LinearArgs a, const LinearArgs g) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
-  if (blockIdx.y == 0) segment_sum<D, false>(a, smem);
-  else segment_sum<D, true>(g, smem);
+  if (!BACKWARD) segment_sum<D, 3, false>(a, smem);
+  else if (blockIdx.y == 0) segment_sum<D, 2, false>(a, smem);
+  else segment_sum<D, 3, true>(g, smem);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -905,8 +902,9 @@ static LinearArgs linear_args(const LinearCall& c, const LinearPlan& plan) {
 // the states (gradients) between segments, in a.seg (and g.seg, if g is given)
 template <int D>
 static int run_states(const LinearArgs& a, const LinearArgs* g, int64_t pairs, hipStream_t st) {
-  hipLaunchKernelGGL(linear_segment_kernel<D>, dim3((unsigned)(pairs * a.nseg), g ? 2 : 1), dim3(64 * kLinWaves),
-                     2 * kChunk * D * 2 + kChunk * sizeof(float), st, a, g ? *g : a);
+  const auto segments = g ? linear_segment_kernel<D, true> : linear_segment_kernel<D, false>;
+  hipLaunchKernelGGL(segments, dim3((unsigned)(pairs * a.nseg), g ? 2 : 1), dim3(64 * kLinWaves), 2 * kChunk * D * 2 + kChunk * sizeof(float), st,
+                     a, g ? *g : a);
   if (int rc = check_launch("linear attention (segments)")) return rc;
   hipLaunchKernelGGL(linear_scan_kernel<D>, dim3((unsigned)(pairs * (D * D / 1024)), g ? 2 : 1), dim3(256), 0, st, a, g ? *g : a);
   return check_launch("linear attention (scan)");
