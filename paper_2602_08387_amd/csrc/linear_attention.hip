@@ -840,7 +840,7 @@ struct LinearPlan { int seg_chunks, nseg, parts; };
 // 64, 32: a workgroup of linear_out_kernel with up to two heads, and for a further two; one for dk and dv, and for each head of the group; one tile pair of
 // linear_segment_kernel) are 1.3 times what single workgroups take with their inputs in the caches.  Workgroups that share compute units take 1.3 (1.6)
 // times as long; 4.3 TB/s.  Over 152 shapes of 128 to 8192 tokens, timed with every power of two, the choice is 1 % slower than the best on average, at
-// worst 1.2 times (77 us for 63); one segment throughout would be 2.4 times slower, always the most 1.2 times.
+// worst 1.25 times (75 us for 60); one segment throughout would be 3.8 times slower, always the most 1.2 times.
 static double linear_time(bool backward, double pairs, int chunks, int G, int64_t D, int n, LinearPlan* plan) {
   static const double kStep[3][5] = {{6.5, 3.3, 4.7, 3.6, 2.9}, {3.5, 1.7, 2.5, 2.2, 1.6}, {2.5, 1.0, 1.7, 1.4, 1.2}};
   const double* c = kStep[D == 128 ? 0 : D == 64 ? 1 : 2];
