@@ -980,17 +980,19 @@ int launch_linear_attention_bwd(const LinearCall& c, const float* s_in, const vo
 }
 
 // ------------------------------------------------------------------------------------------
-// One token for every batch row.  Bound by HBM: the state is read and written once, 8 bytes an element: 256 rows of 8 states of 128 x 128 in 49 us
-// (0.28 GB, 5.7 TB/s); of one row by the launch, 4.5 us.  Workgroup: COLS columns of
-// one state; a thread holds four columns of every RG-th row, so that the state stays in registers between its update and the products
-// with the group's queries.
+// One token for every batch row.  Bound by HBM: the state is read and written once, 8 bytes an element: 256 rows of 8 states of 128 x 128 in 46.5
+// us (0.28 GB, 6.0 TB/s); of one row by what waits for each other, 4.1 us.  Workgroup: COLS columns of one state; a thread holds four columns of
+// every RG-th row, so that the state stays in registers between its update and the products with the group's queries.  HEADS of these at once, read
+// before the state is: one after the other a group of four takes 4.6 and 49 us; but four where there is one, 6.6 us for 4.6 (40 rows of 12
+// heads of 64), and one of two 4.6 for 4.2.
 // ------------------------------------------------------------------------------------------
-template <int D, int COLS>
+template <int D, int COLS, int HEADS>
 __global__ __launch_bounds__(256) void linear_step_kernel(const bf16_t* __restrict__ q, const bf16_t* __restrict__ k, const bf16_t* __restrict__ v,
                                                           const float* __restrict__ log_decay, const int64_t* __restrict__ lengths,
                                                           float* __restrict__ state, int Hq, int Hkv, float scale, bf16_t* __restrict__ o) {
-  constexpr int CV = COLS / 4, RG = 256 / CV, R = (D + RG - 1) / RG;
-  __shared__ f32x4 red[4][CV];
+  constexpr int CV = COLS / 4, RG = 256 / CV, R = D / RG;
+  static_assert(D % RG == 0, "every thread holds R rows");
+  __shared__ f32x4 red[4][HEADS][CV];
   const int pair = blockIdx.x, b = pair / Hkv, j = pair % Hkv, G = Hq / Hkv, col = (int)blockIdx.y * COLS;
   const int cv = threadIdx.x % CV, rg = threadIdx.x / CV, wave = threadIdx.x >> 6, c = col + cv * 4;
   const bf16_t* qp = q + ((int64_t)b * Hq + (int64_t)j * G) * D;
@@ -1001,36 +1003,52 @@ __global__ __launch_bounds__(256) void linear_step_kernel(const bf16_t* __restri
       for (int h = 0; h < G; ++h) *reinterpret_cast<bf16x4*>(op + (int64_t)h * D + c) = zero;
     return;
   }
+  float qv[HEADS][R];
+  auto load_queries = [&](int h0) {
+#pragma unroll
+    for (int n = 0; n < HEADS; ++n)
+#pragma unroll
+      for (int i = 0; i < R; ++i) qv[n][i] = (float)qp[(int64_t)min(h0 + n, G - 1) * D + i * RG + rg];
+  };
+  load_queries(0);
   const Decay lam = decay_of(log_decay[j], 1);
   const bf16_t* kp = k + (int64_t)pair * D;
   const bf16x4 vv = *reinterpret_cast<const bf16x4*>(v + (int64_t)pair * D + c);
   float* sp = state + (int64_t)pair * D * D + c;
   f32x4 s[R];
 #pragma unroll
-  for (int i = 0; i < R; ++i)
-    if (D % RG == 0 || i * RG + rg < D) s[i] = *reinterpret_cast<const f32x4*>(sp + (i * RG + rg) * D);
+  for (int i = 0; i < R; ++i) s[i] = *reinterpret_cast<const f32x4*>(sp + (i * RG + rg) * D);
 #pragma unroll
-  for (int i = 0; i < R; ++i)
-    if (D % RG == 0 || i * RG + rg < D) {
-      const float kk = (float)kp[i * RG + rg];
+  for (int i = 0; i < R; ++i) {
+    const float kk = (float)kp[i * RG + rg];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[i][e] = decayed(lam, s[i][e], kk * (float)vv[e]);
-      *reinterpret_cast<f32x4*>(sp + (i * RG + rg) * D) = s[i];
+    for (int e = 0; e < 4; ++e) s[i][e] = decayed(lam, s[i][e], kk * (float)vv[e]);
+    *reinterpret_cast<f32x4*>(sp + (i * RG + rg) * D) = s[i];
+  }
+  for (int h0 = 0; h0 < G; h0 += HEADS) {
+    f32x4 acc[HEADS];
+#pragma unroll
+    for (int n = 0; n < HEADS; ++n) {
+      acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < R; ++i) acc[n] += s[i] * qv[n][i];
     }
-  for (int h = 0; h < G; ++h) {
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < R; ++i)
-      if (D % RG == 0 || i * RG + rg < D) acc += s[i] * (float)qp[(int64_t)h * D + i * RG + rg];
+    if (h0 + HEADS < G) load_queries(h0 + HEADS);
 #pragma unroll
     for (int off = CV; off < 64; off <<= 1)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], off, 64);
+      for (int n = 0; n < HEADS; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[n][e] += __shfl_xor(acc[n][e], off, 64);
+    if (h0 > 0) __syncthreads();
+    if ((threadIdx.x & 63) < CV)
+#pragma unroll
+      for (int n = 0; n < HEADS; ++n) red[wave][n][cv] = acc[n];
     __syncthreads();
-    if ((threadIdx.x & 63) < CV) red[wave][cv] = acc;
-    __syncthreads();
-    if (threadIdx.x < CV) {
-      const f32x4 t = ((red[0][cv] + red[1][cv]) + (red[2][cv] + red[3][cv])) * scale;
+    const int h = h0 + threadIdx.x / CV;
+    if (threadIdx.x < HEADS * CV && h < G) {
+      const int n = threadIdx.x / CV;
+      const f32x4 t = ((red[0][n][cv] + red[1][n][cv]) + (red[2][n][cv] + red[3][n][cv])) * scale;
       bf16x4 w;
 #pragma unroll
       for (int e = 0; e < 4; ++e) w[e] = (bf16_t)t[e];
@@ -1041,12 +1059,15 @@ __global__ __launch_bounds__(256) void linear_step_kernel(const bf16_t* __restri
 
 int launch_linear_attention_step(const LinearCall& c, float* state, void* o, hipStream_t st) {
   const int64_t pairs = c.B * c.Hkv;
-#define STEP(D, COLS)                                                                                                          \
-  hipLaunchKernelGGL((linear_step_kernel<D, COLS>), dim3((unsigned)pairs, D / COLS), dim3(256), 0, st, (const bf16_t*)c.q,      \
+  const int64_t G = c.Hq / c.Hkv;
+#define STEP(D, HEADS)                                                                                                          \
+  hipLaunchKernelGGL((linear_step_kernel<D, 32, HEADS>), dim3((unsigned)pairs, D / 32), dim3(256), 0, st, (const bf16_t*)c.q,   \
                      (const bf16_t*)c.k, (const bf16_t*)c.v, c.log_decay, c.lengths, state, (int)c.Hq, (int)c.Hkv, c.scale, (bf16_t*)o)
-  if (c.dh == 128) STEP(128, 32);
-  else if (c.dh == 64) STEP(64, 32);
-  else STEP(32, 32);
+#define STEP_HEADS(D) if (G > 2) STEP(D, 4); else if (G == 2) STEP(D, 2); else STEP(D, 1)
+  if (c.dh == 128) { STEP_HEADS(128); }
+  else if (c.dh == 64) { STEP_HEADS(64); }
+  else { STEP_HEADS(32); }
+#undef STEP_HEADS
 #undef STEP
   return check_launch("linear_attention_step");
 }
