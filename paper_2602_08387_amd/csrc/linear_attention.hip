@@ -383,31 +383,18 @@ __device__ __forceinline__ Scale state_scale(const float* largest) {
   return Scale(__builtin_amdgcn_readfirstlane(__float_as_int(m) >> 23));
 }
 
-// mult lambda^(place of the query - place of the key) for a 16 x 16 block of scores whose lane holds four keys of one query (STEP -1) or four queries of
-// one key (STEP 1).  Uniform powers, and one of the lane's: a lane's own eight would be registers that are not there.
+// A 16 x 16 block of scores, whose lane holds four keys of one query (STEP -1) or four queries of one key (STEP 1), times mult lambda^(place of the query -
+// place of the key); what is not causal becomes 0.  blocks: from the key's to the query's, -1 .. 3.  The same work for every block, without branches, so
+// that two of them, their reads and products, pass together: with branches around what is not causal, and one power of the lane's for the blocks off the
+// diagonal, dk, dv and dq of 4096 tokens of 32 heads of 64 on one KV head take 49.6 us for 44.7, the forward's last kernel 80 for 78 (16384 tokens
+// of 32 and 8 heads of 128); heads of 64 that share nothing 36.9 for 37.4.
+// (Beside a state of 128 x 128 no register is left for what a lane derives from its number and keeps: the caller passes here(lane).)
 template <int STEP>
-struct Decays {
-  float log2, mult, p1, p2, p3, p16, p32;
-  __device__ __forceinline__ Decays(float log2_, float mult_)
-      : log2(log2_), mult(mult_), p1(uniform(power(log2_, 1))), p2(uniform(power(log2_, 2))), p3(uniform(power(log2_, 3))),
-        p16(uniform(power(log2_, 16))), p32(uniform(power(log2_, 32))) {}
-  // (With a state of 128 x 128 no register is left for what a lane derives from its number and keeps: the caller passes here(lane).)
-  // blocks: from the key's to the query's, 0 .. 3; within the diagonal block what is not causal becomes 0
-  __device__ __forceinline__ void apply(f32x4& s, int blocks, int lane) const {
-    const int first = STEP * (((lane >> 4) << 2) - (lane & 15));   // of the lane's four differences within 16
-    if (blocks == 0) {
+__device__ __forceinline__ void weigh_scores(f32x4& s, float log2, float mult, int blocks, int lane) {
+  const int first = blocks * 16 + STEP * (((lane >> 4) << 2) - (lane & 15));   // the lane's four differences: this, and the next three in STEPs
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[e] = first + STEP * e >= 0 ? s[e] * (mult * power(log2, first + STEP * e)) : 0.f;
-    } else {
-      const float f = blocks == 1 ? 1.f : blocks == 2 ? p16 : p32;
-      const float base = mult * f * power(here(log2), 16 + first - (STEP < 0 ? 3 : 0));
-      s[STEP < 0 ? 3 : 0] *= base;
-      s[STEP < 0 ? 2 : 1] *= base * p1;
-      s[STEP < 0 ? 1 : 2] *= base * p2;
-      s[STEP < 0 ? 0 : 3] *= base * p3;
-    }
-  }
-};
+  for (int e = 0; e < 4; ++e) s[e] = first + STEP * e >= 0 ? s[e] * (mult * power(log2, first + STEP * e)) : 0.f;
+}
 
 // o[n] += factor times the product of a(n, k) with the scaled row, for NB blocks, four in turn
 template <int KS, int NB, typename F>
@@ -589,7 +576,7 @@ __global__ __launch_bounds__(256) void linear_scan_kernel(const LinearArgs a, co
 // NB blocks of 16 columns from n0 of o for the query that the lane's row is
 template <int D, int NB>
 __device__ __forceinline__ void out_tile(f32x4 (&o)[NB], const bf16x8 (&qf)[D / 32], bool some,
-                                         float down, int tile, int n0, float log2, float scale, const Decays<-1>& ds, int lane, uint32_t along_lane, uint32_t columns_lane) {
+                                         float down, int tile, int n0, float log2, float scale, int lane, uint32_t along_lane, uint32_t columns_lane) {
   constexpr int KS = D / 32, kt = 0, vt = kChunk * D * 2, st = 2 * kChunk * D * 2;
   const uint32_t al = here(along_lane), sl = here(along_lane + (uint32_t)(n0 * 16 * D * 2)), cl = here(columns_lane ^ (uint32_t)(n0 << 5));
   #pragma unroll
@@ -600,13 +587,12 @@ __device__ __forceinline__ void out_tile(f32x4 (&o)[NB], const bf16x8 (&qf)[D / 
     f32x4 sc[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const int blk = 2 * pr + i;
       sc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (blk > tile) continue;
 #pragma unroll
-      for (int k = 0; k < KS; ++k) sc[i] = mfma16(Rows<D>::along(al, kt, blk * 16, k), qf[k], sc[i]);
-      ds.apply(sc[i], tile - blk, D == 128 ? here(lane) : lane);
+      for (int k = 0; k < KS; ++k) sc[i] = mfma16(Rows<D>::along(al, kt, (2 * pr + i) * 16, k), qf[k], sc[i]);
     }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) weigh_scores<-1>(sc[i], log2, scale, tile - 2 * pr - i, D == 128 ? here(lane) : lane);
     const Scores pf(sc);
     pf.times(o, [&](int n) { return Rows<D>::columns(cl, vt, n, pr * 32); });
   }
@@ -640,7 +626,6 @@ __device__ __forceinline__ void segment_out(const LinearArgs& p, int id, int par
   if (some) largest[wave] = s.largest(wave);
   const float log2 = uniform(log2_decay(p.log_decay[j]));
   const Decay whole = decay_of(p.log_decay[j], kChunk);
-  const Decays<-1> decays(log2, p.scale);
   const uint32_t along_lane = Rows<D>::along_lane(lds_address(smem), lane), columns_lane = Rows<D>::columns_lane(lds_address(smem), lane);
 
   for (int c = 0; c < chunks; ++c) {
@@ -670,12 +655,12 @@ __device__ __forceinline__ void segment_out(const LinearArgs& p, int id, int par
       for (int k = 0; k < KS; ++k) qf[k] = load8(rq, at + k * 64 + g * 16);
       if (both || D == 32) {
         f32x4 o[NB];
-        out_tile<D, NB>(o, qf, some, down, tile, 0, log2, p.scale, decays, lane, along_lane, columns_lane);
+        out_tile<D, NB>(o, qf, some, down, tile, 0, log2, p.scale, lane, along_lane, columns_lane);
         store_row<NB>(ro, at, o, rows == kChunk, t < rows, lane);
       } else if constexpr (D > 32) {
         const int n0 = wave >= 4 ? NB / 2 : 0;
         f32x4 o[NB / 2];
-        out_tile<D, NB / 2>(o, qf, some, down, tile, n0, log2, p.scale, decays, lane, along_lane, columns_lane);
+        out_tile<D, NB / 2>(o, qf, some, down, tile, n0, log2, p.scale, lane, along_lane, columns_lane);
         store_row<NB / 2>(ro, at + n0 * 32, o, rows == kChunk, t < rows, lane);
       }
     }
@@ -737,7 +722,6 @@ __device__ __forceinline__ void segment_keys(const LinearArgs& p, int id, char* 
   const float log2 = uniform(log2_decay(p.log_decay[j]));
   const Decay whole = decay_of(p.log_decay[j], kChunk);
   weights_from_start(w, log2, p.scale, 0);
-  const Decays<1> decays(log2, p.scale);
   const uint32_t along_lane = Rows<D>::along_lane(lds_address(smem), lane), columns_lane = Rows<D>::columns_lane(lds_address(smem), lane);
   for (int c = chunks - 1; c >= 0; --c) {
     const int rows = min(m - c * kChunk, kChunk);
@@ -797,13 +781,12 @@ __device__ __forceinline__ void segment_keys(const LinearArgs& p, int id, char* 
         f32x4 sc[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const int blk = 2 * pr + i;
           sc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-          if (blk < tile) continue;
 #pragma unroll
-          for (int k = 0; k < KS; ++k) sc[i] = mfma16(Rows<D>::along(al, 0, blk * 16, k), kf[k], sc[i]);
-          decays.apply(sc[i], blk - tile, D == 128 ? here(lane) : lane);
+          for (int k = 0; k < KS; ++k) sc[i] = mfma16(Rows<D>::along(al, 0, (2 * pr + i) * 16, k), kf[k], sc[i]);
         }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) weigh_scores<1>(sc[i], log2, p.scale, 2 * pr + i - tile, D == 128 ? here(lane) : lane);
         const Scores pf(sc);
         pf.times(acc, [&](int n) { return Rows<D>::columns(cl, 0, n, pr * 32); });
       }
@@ -825,7 +808,7 @@ __device__ __forceinline__ void segment_keys(const LinearArgs& p, int id, char* 
 // The three gradients of a call in one launch: first the workgroups for dk and dv of `g`, which take longest, then those for dq of `a`.  192 us at 16384
 // tokens of 32 and 8 heads of 128 (0.79 GB, 4.1 TB/s).  (Both kinds alternating by eights, so that a segment's do, k and v would come from memory
 // once for both: 256 us when this order took 227.  A head's q and do asked for while the one before is worked on: no change, but for heads of
-// 64 of which very many share a KV head, 49 -> 39 us at 32 of one.)
+// 64 of which very many share a KV head, a fifth less at 32 of one.)
 template <int D, int SPLIT>
 __global__ __launch_bounds__(64 * kLinWaves, 4) void linear_grad_kernel(const LinearArgs a, const LinearArgs g, int segments, int parts) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
