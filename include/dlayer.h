@@ -334,8 +334,10 @@ int qk_norm_rope_backward(const void* q, const void* k, const void* gamma_q, con
  * q, o [B*S, Hq, dh], k, v [B*S, Hkv, dh] bf16; log_decay [Hkv] f32 on the device, not above 0 (0: nothing is forgotten,
  * minus infinity: nothing is remembered), a constant of the model: it gets no gradient.  State in and out [B, Hkv, dh, dh] f32:
  * state_in NULL for zeros, state_out (the state after a row's last token) NULL if not wanted; state_out may alias state_in.
- * Sequences are worked on in chunks of 64 tokens on the matrix units, the states between them are fp32.  A value of a row that is not
- * finite (padding aside) may show in the results of every token of its chunk, not only of those that the sums above name.
+ * Sequences are worked on in chunks of 64 tokens on the matrix units, the states between them are fp32; where queries meet them they are the
+ * sum of two fp16 (22 bits), scaled to the state's largest element, and weighted scores and keys are sums of bf16: all results are right up to their
+ * own rounding to bf16, those of inputs that have means too.  A value of a row that is not finite (padding aside) may show in the results of every
+ * token of its chunk, not only of those that the sums above name.
  * workspace: linear_attention_workspace_bytes(...).                                                          */
 size_t linear_attention_workspace_bytes(int64_t batch, int64_t seq, int64_t n_q_heads, int64_t n_kv_heads,
                                         int64_t head_dim);

@@ -15,12 +15,15 @@
 // pass over the data (16384 tokens of 32 and 8 heads of 128: 117 us, 0.54 GB; a pass over them 0.34 GB, 70 us.  Backward: 288 us, 1.23 GB;
 // 0.54 GB, 113 us); the bytes that move do so at 4.3 to 4.6 TB/s, where a copy reaches 4.76.
 //
-// Precision.  States are fp32, in the accumulators and in memory.  The decayed keys (queries) whose products with the values (do) they sum are
-// split into three bf16 terms, so these products are exact up to fp32 (two terms where a state serves only results rounded to bf16), and
-// so are weighted scores, into two: sums of few heads or keys cancel, and a score rounded to bf16 then shows (gradients 4e-2 off in single elements).  A
-// state is rounded where it is multiplied with queries, to fp16, scaled by a power of two (1.5e-4 rms, where the result's own rounding to bf16 is
-// 1.7e-3; rounded to bf16 it would add as much again); the queries, scaled too, are exact in fp16.  Decays of many tokens are evaluated as
-// powers (exp2 of a multiple of the logarithm), the factor between chunks as the sum of two fp32, so that no rounding of lambda is repeated.
+// Precision.  States are fp32, in the accumulators and in memory; as operands they are the sum of two fp16, scaled by a power of two: 22 bits, and queries,
+// scaled too, are exact in fp16.  Keys and values that have means make a state a large rank-one part and, in front of it, what tells tokens apart, which is all that
+// a query orthogonal to the keys' mean sees.  In one fp16 results would be off by 2e-4 without means, 8e-3 at means of one deviation and 4e-2 at four, where
+// their own rounding to bf16 is 1.7e-3; in two, by 4e-8, 2e-6 and 8e-6 (2-norms, emulated in fp64 for 4096 tokens of heads of 128).  The decayed keys
+// (queries) whose products with the values (do) a state sums are split into three bf16 terms, which is exact up to fp32.  Where a state serves only results
+// rounded to bf16, two terms do (2e-6, 3e-6 and 1e-5), and its decay from chunk to chunk is one fp32 (2e-7, 3e-6 and 2e-5).  Weighted scores are two terms (4e-7
+// whatever the means); sums of few heads or keys cancel, and a score rounded to bf16 then shows (gradients 4e-2 off in single elements).  Decays of many tokens
+// are evaluated as powers (exp2 of a multiple of the logarithm), the factor between chunks of a state that leaves as the sum of two fp32, so that no
+// rounding of lambda is repeated.
 //
 // Layout.  All products are v_mfma_f32_16x16x32_bf16, D[row][col] += A[row][k] B[k][col]: lane (g = lane / 16, r = lane % 16) holds row r of A and
 // column r of B, 8 of 32 k each, and rows 4 g .. 4 g + 3 of column r of D.  Scores are formed as S^T[j][i] = K Q^T, so that a lane
@@ -152,7 +155,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 __device__ __forceinline__ f32x4 mfma16_f16(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
 // Powers of two that take numbers up to some bound into the upper half of fp16's range (below 2^15, so that what is 2^29 times smaller than
-// the bound keeps its eleven bits), and back.  exponent: of the bound, as an fp32 has it.
+// the bound keeps its eleven bits, and eleven more in a second term), and back.  exponent: of the bound, as an fp32 has it.
 struct Scale {
   float up, down;
   __device__ __forceinline__ explicit Scale(int exponent) {
@@ -231,6 +234,13 @@ __device__ __forceinline__ void weights_to_end(float* w, float log2, int rows) {
 __device__ __forceinline__ void weights_from_start(float* w, float log2, float mult, int before) {
   if (threadIdx.x < kChunk) w[threadIdx.x] = mult * power(log2, before + (int)threadIdx.x + 1);
 }
+
+constexpr float kLowTerm = 1.f / 4096;   // unit of the second term of a state as an operand
+// Both terms lie in LDS.  Of a 128 x 128 state, two workgroups' would take 192 of a compute unit's 160 KB: there they take turns in one place.  (One workgroup a
+// compute unit, with registers to load the next tiles ahead: 117 us for 110 in the forward's last kernel, 16384 tokens of 32 and 8 heads of 128, 265
+// for 246 in the gradients'.)
+template <int D> constexpr bool kBothTerms = D < 128;
+template <int D> constexpr int kStateLds = (kBothTerms<D> ? 2 : 1) * D * D * 2;
 
 // A state [D along keys][D along values] over the waves: wave -> RB x CB blocks of 16 x 16 (of 32 x 32 elements four waves hold one each).  In
 // memory between the kernels it lies as the accumulators do: [wave][block][lane] f32x4.
@@ -320,19 +330,32 @@ struct State {
     m = fmaxf(m, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(m), 0x122, 0xf, 0xf, true)));
     return fmaxf(m, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(m), 0x121, 0xf, 0xf, true)));
   }
-  // to LDS in fp16 [columns][rows]: an operand along either
-  __device__ __forceinline__ void to_lds(char* t, float up, int wave, int lane) const {
+  // to LDS [columns][rows]: an operand along either.  The scaled state is the sum of two fp16: its rounding and, in units of kLowTerm, what that rounds off (at
+  // most 8; no number where the first is infinite, which the clamp keeps out of the product).  The second lies behind the first, or low says which is meant.
+  __device__ __forceinline__ void to_lds(char* t, float up, bool low, int wave, int lane) const {
     if (!holds(wave)) return;
     lane = here(lane);
+    up = here(up);   // no conversion ahead of the barrier in front of this
+    const float bound = low ? 8.f : INFINITY, unit = low ? 1.f / kLowTerm : 1.f;
 #pragma unroll
     for (int i = 0; i < RB; ++i)
 #pragma unroll
       for (int j = 0; j < CB; ++j) {
-        f16x4 v;
+        f16x4 v, rest;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = (_Float16)(a[i][j][e] * up);
+        for (int e = 0; e < 4; ++e) {
+          const float x = a[i][j][e] * up, h = (float)(_Float16)x;
+          if (kBothTerms<D>) {
+            v[e] = (_Float16)h;
+            rest[e] = (_Float16)(__builtin_amdgcn_fmed3f(x - h, -8.f, 8.f) * (1.f / kLowTerm));
+          } else {
+            v[e] = (_Float16)(__builtin_amdgcn_fmed3f(x - (low ? h : 0.f), -bound, bound) * unit);
+          }
+        }
         const int r = row(row_block(wave) + i, lane), p = (col_block(wave) + j) * 16 + (lane & 15);
-        *reinterpret_cast<f16x4*>(t + Rows<D>::at(p, r >> 3) + ((r & 7) << 1)) = v;
+        char* at = t + Rows<D>::at(p, r >> 3) + ((r & 7) << 1);
+        *reinterpret_cast<f16x4*>(at) = v;
+        if (kBothTerms<D>) *reinterpret_cast<f16x4*>(at + D * D * 2) = rest;
       }
   }
   // += sum over a tile's 64 tokens of (w x)^T y, all in LDS (x, y: where); w x as the sum of SPLIT bf16
@@ -573,10 +596,11 @@ __global__ __launch_bounds__(256) void linear_scan_kernel(const LinearArgs a, co
 // for either.  78 us at 16384 tokens of 32 and 8 heads of 128 (0.37 GB, 4.7 TB/s).
 // SPLIT: 3 where the state goes on to the caller, 2 where it serves this kernel's products alone.
 // ------------------------------------------------------------------------------------------
-// NB blocks of 16 columns from n0 of o for the query that the lane's row is
+// NB blocks of 16 columns from n0 of o for the query that the lane's row is.  some: there is a state, scaled by sc; low: of its terms the second is in LDS,
+// where there is but one, and the first afterwards
 template <int D, int NB>
-__device__ __forceinline__ void out_tile(f32x4 (&o)[NB], const bf16x8 (&qf)[D / 32], bool some,
-                                         float down, int tile, int n0, float log2, float scale, int lane, uint32_t along_lane, uint32_t columns_lane) {
+__device__ __forceinline__ void out_tile(f32x4 (&o)[NB], const bf16x8 (&qf)[D / 32], const State<D>& s, bool some, const Scale& sc, bool low, char* smem,
+                                         int tile, int n0, float log2, float scale, int wave, int lane, uint32_t along_lane, uint32_t columns_lane) {
   constexpr int KS = D / 32, kt = 0, vt = kChunk * D * 2, st = 2 * kChunk * D * 2;
   const uint32_t al = here(along_lane), sl = here(along_lane + (uint32_t)(n0 * 16 * D * 2)), cl = here(columns_lane ^ (uint32_t)(n0 << 5));
   #pragma unroll
@@ -584,22 +608,35 @@ __device__ __forceinline__ void out_tile(f32x4 (&o)[NB], const bf16x8 (&qf)[D / 
 #pragma unroll
   for (int pr = 0; pr < 2; ++pr) {
     if (2 * pr > tile) break;
-    f32x4 sc[2];
+    f32x4 p[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      sc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      p[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int k = 0; k < KS; ++k) sc[i] = mfma16(Rows<D>::along(al, kt, (2 * pr + i) * 16, k), qf[k], sc[i]);
+      for (int k = 0; k < KS; ++k) p[i] = mfma16(Rows<D>::along(al, kt, (2 * pr + i) * 16, k), qf[k], p[i]);
     }
 #pragma unroll
-    for (int i = 0; i < 2; ++i) weigh_scores<-1>(sc[i], log2, scale, tile - 2 * pr - i, D == 128 ? here(lane) : lane);
-    const Scores pf(sc);
+    for (int i = 0; i < 2; ++i) weigh_scores<-1>(p[i], log2, scale, tile - 2 * pr - i, D == 128 ? here(lane) : lane);
+    const Scores pf(p);
     pf.times(o, [&](int n) { return Rows<D>::columns(cl, vt, n, pr * 32); });
   }
   if (some) {   // last, when the queries as they are need no registers any more
     const ScaledRow<KS> qs(qf);
-    const float after = power(log2, tile * 16 + (here(lane) & 15) + 1) * scale * down * qs.down;
-    add_scaled<KS>(o, qs, after, [&](int n, int k) { return Rows<D>::along(sl, st, n * 16, k); });
+    const float after = power(log2, tile * 16 + (here(lane) & 15) + 1) * scale * sc.down * qs.down;
+    const auto add = [&](int t, float factor) {
+      const uint32_t at = here(sl);
+      add_scaled<KS>(o, qs, factor, [&](int n, int k) { return Rows<D>::along(at, t, n * 16, k); });
+    };
+    if constexpr (kBothTerms<D>) {
+      add(st + D * D * 2, after * kLowTerm);
+      add(st, after);
+    } else {
+      add(st, low ? after * kLowTerm : after);
+      __syncthreads();
+      s.to_lds(smem + st, sc.up, !low, wave, lane);
+      __syncthreads();
+      add(st, low ? after : after * kLowTerm);
+    }
   }
 }
 
@@ -607,7 +644,7 @@ template <int D, int SPLIT>
 __device__ __forceinline__ void segment_out(const LinearArgs& p, int id, int part, int parts, char* smem) {
   constexpr int NB = D / 16, KS = D / 32;
   constexpr int kt = 0, vt = kChunk * D * 2, st = 2 * kChunk * D * 2;
-  float *largest = reinterpret_cast<float*>(smem + st + D * D * 2), *w = largest + kLinWaves;
+  float *largest = reinterpret_cast<float*>(smem + st + kStateLds<D>), *w = largest + kLinWaves;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
   const int pair = id / p.nseg, sg = id % p.nseg, b = pair / p.Hkv, j = pair % p.Hkv, G = p.Hq / p.Hkv;
   const int per = (G + parts - 1) / parts, h0 = part * per, h1 = min(G, h0 + per);
@@ -622,7 +659,7 @@ __device__ __forceinline__ void segment_out(const LinearArgs& p, int id, int par
   else if (p.s_in) s.load_matrix(p.s_in + (int64_t)pair * D * D, p.flip, wave, lane);
   else s.clear();
   bool some = p.s_in != nullptr || sg > 0;   // a state that is not zero
-  float down = 0.f;
+  Scale sc(0);
   if (some) largest[wave] = s.largest(wave);
   const float log2 = uniform(log2_decay(p.log_decay[j]));
   const Decay whole = decay_of(p.log_decay[j], kChunk);
@@ -637,13 +674,13 @@ __device__ __forceinline__ void segment_out(const LinearArgs& p, int id, int par
     tile_to_lds<D>(rows_rsrc<D>(p.v + kc, ldk, rows), smem + vt, ldk, wave, lane);
     if (c == 0 || rows < kChunk) weights_to_end(w, log2, rows);
     if (some) {
-      const Scale sc = state_scale(largest);
-      down = sc.down;
-      s.to_lds(smem + st, sc.up, wave, lane);
+      sc = state_scale(largest);
+      s.to_lds(smem + st, sc.up, false, wave, lane);
     }
     loads_done();
+    bool low = false;
     const int64_t qc = q0 + (int64_t)c * kChunk * ldq;
-    for (int h = h0; h < h1; h += 2) {
+    for (int h = h0; h < h1; h += 2, low = !low) {
       const bool both = h + 1 < h1;
       if (!both && D == 32 && wave >= 4) break;   // 16 columns are not worth sharing
       const int head = both ? h + (wave >> 2) : h, tile = (wave + (h >> 1)) & 3, t = tile * 16 + r;
@@ -655,12 +692,12 @@ __device__ __forceinline__ void segment_out(const LinearArgs& p, int id, int par
       for (int k = 0; k < KS; ++k) qf[k] = load8(rq, at + k * 64 + g * 16);
       if (both || D == 32) {
         f32x4 o[NB];
-        out_tile<D, NB>(o, qf, some, down, tile, 0, log2, p.scale, lane, along_lane, columns_lane);
+        out_tile<D, NB>(o, qf, s, some, sc, low, smem, tile, 0, log2, p.scale, wave, lane, along_lane, columns_lane);
         store_row<NB>(ro, at, o, rows == kChunk, t < rows, lane);
       } else if constexpr (D > 32) {
         const int n0 = wave >= 4 ? NB / 2 : 0;
         f32x4 o[NB / 2];
-        out_tile<D, NB / 2>(o, qf, some, down, tile, n0, log2, p.scale, lane, along_lane, columns_lane);
+        out_tile<D, NB / 2>(o, qf, s, some, sc, low, smem, tile, n0, log2, p.scale, wave, lane, along_lane, columns_lane);
         store_row<NB / 2>(ro, at + n0 * 32, o, rows == kChunk, t < rows, lane);
       }
     }
@@ -696,8 +733,8 @@ __global__ __launch_bounds__(64 * kLinWaves, 4) void linear_out_kernel(const Lin
 template <int D, int SPLIT>
 __device__ __forceinline__ void segment_keys(const LinearArgs& p, int id, char* smem) {
   constexpr int NB = D / 16, KS = D / 32;
-  constexpr int qt = 0, dt = kChunk * D * 2, et = 2 * kChunk * D * 2;
-  float *largest = reinterpret_cast<float*>(smem + et + D * D * 2), *w = largest + kLinWaves;
+  constexpr int qt = 0, dt = kChunk * D * 2, et = 2 * kChunk * D * 2, lt = et + kStateLds<D> - D * D * 2;   // lt: the state's second term
+  float *largest = reinterpret_cast<float*>(smem + et + kStateLds<D>), *w = largest + kLinWaves;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
   const int pair = id / p.nseg, sg = id % p.nseg, b = pair / p.Hkv, j = pair % p.Hkv, G = p.Hq / p.Hkv;
   const int len = row_length(p, b), t0 = sg * p.seg_chunks * kChunk;
@@ -717,7 +754,7 @@ __device__ __forceinline__ void segment_keys(const LinearArgs& p, int id, char* 
   else s.clear();
   // not zero: a gradient comes in, or the row goes on behind this segment
   bool some = p.s_in != nullptr || len > t0 + p.seg_chunks * kChunk;
-  float down = 0.f;
+  Scale sc(0);
   if (some) largest[wave] = s.largest(wave);
   const float log2 = uniform(log2_decay(p.log_decay[j]));
   const Decay whole = decay_of(p.log_decay[j], kChunk);
@@ -736,9 +773,8 @@ __device__ __forceinline__ void segment_keys(const LinearArgs& p, int id, char* 
     };
     bring(0);
     if (into) {
-      const Scale sc = state_scale(largest);
-      down = sc.down;
-      s.to_lds(smem + et, sc.up, wave, lane);
+      sc = state_scale(largest);
+      s.to_lds(smem + et, sc.up, true, wave, lane);
     }
     const __amdgpu_buffer_rsrc_t rk = rows_rsrc<D>(own + kc, ldk, rows);
     bf16x8 kf[KS];
@@ -749,22 +785,42 @@ __device__ __forceinline__ void segment_keys(const LinearArgs& p, int id, char* 
 #pragma unroll
     for (int n = 0; n < NB; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
     if (into) {
-      const ScaledRow<KS> ks(kf);
-      if (!dk_role) {
-        const uint32_t al = here(along_lane);
+      float down;
+      const auto add = [&](int t) {
+        bf16x8 kh[KS];   // scaled for each term: beside a state of 128 x 128 there are no registers to keep this and kf, nor for the addresses of more columns
 #pragma unroll
-        for (int k = 0; k < KS; ++k)
+        for (int k = 0; k < KS; ++k) kh[k] = D == 128 ? __builtin_bit_cast(bf16x8, here(__builtin_bit_cast(u32x4, kf[k]))) : kf[k];
+        const ScaledRow<KS> ks(kh);
+        down = ks.down;
+        constexpr int AT_ONCE = D == 128 ? 2 : NB;
 #pragma unroll
-          for (int n = 0; n < NB; ++n) acc[n] = mfma16_f16(__builtin_bit_cast(f16x8, Rows<D>::along(al, et, n * 16, k)), ks.v[k], acc[n]);
-      } else {
-        const uint32_t cl = Rows<D>::template columns_lane<4>(lds_address(smem), here(lane));
+        for (int n0 = 0; n0 < NB; n0 += AT_ONCE) {
+          if (!dk_role) {
+            const uint32_t al = here(along_lane);
 #pragma unroll
-        for (int k = 0; k < KS; ++k)
+            for (int k = 0; k < KS; ++k)
 #pragma unroll
-          for (int n = 0; n < NB; ++n)
-            acc[n] = mfma16_f16(__builtin_bit_cast(f16x8, Rows<D>::template columns<4>(cl, et, n, k * 32)), ks.v[k], acc[n]);
+              for (int n = n0; n < n0 + AT_ONCE; ++n) acc[n] = mfma16_f16(__builtin_bit_cast(f16x8, Rows<D>::along(al, t, n * 16, k)), ks.v[k], acc[n]);
+          } else {
+            const uint32_t cl = Rows<D>::template columns_lane<4>(lds_address(smem), here(lane));
+#pragma unroll
+            for (int k = 0; k < KS; ++k)
+#pragma unroll
+              for (int n = n0; n < n0 + AT_ONCE; ++n)
+                acc[n] = mfma16_f16(__builtin_bit_cast(f16x8, Rows<D>::template columns<4>(cl, t, n, k * 32)), ks.v[k], acc[n]);
+          }
+        }
+      };
+      add(lt);
+#pragma unroll
+      for (int n = 0; n < NB; ++n) acc[n] *= kLowTerm;
+      if constexpr (!kBothTerms<D>) {
+        __syncthreads();
+        s.to_lds(smem + et, sc.up, false, wave, lane);
+        __syncthreads();
       }
-      const float left = power(here(log2), max(rows - 1 - key, 0)) * down * ks.down;
+      add(et);
+      const float left = power(here(log2), max(rows - 1 - key, 0)) * sc.down * down;
 #pragma unroll
       for (int n = 0; n < NB; ++n) acc[n] *= left;
     }
@@ -901,7 +957,7 @@ static int run_states(const LinearArgs& a, const LinearArgs* g, int64_t pairs, h
   return check_launch("linear attention (scan)");
 }
 
-template <int D> constexpr size_t kLinearLds = (2 * kChunk + D) * D * 2 + (kLinWaves + kChunk) * sizeof(float);
+template <int D> constexpr size_t kLinearLds = 2 * kChunk * D * 2 + kStateLds<D> + (kLinWaves + kChunk) * sizeof(float);
 
 template <int D, int SPLIT>
 static int launch_out(const LinearArgs& a, int64_t segments, int parts, hipStream_t st) {
