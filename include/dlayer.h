@@ -334,6 +334,7 @@ int qk_norm_rope_backward(const void* q, const void* k, const void* gamma_q, con
  * q, o [B*S, Hq, dh], k, v [B*S, Hkv, dh] bf16; log_decay [Hkv] f32 on the device, not above 0 (0: nothing is forgotten,
  * minus infinity: nothing is remembered), a constant of the model: it gets no gradient.  State in and out [B, Hkv, dh, dh] f32:
  * state_in NULL for zeros, state_out (the state after a row's last token) NULL if not wanted; state_out may alias state_in.
+ * o must not overlap q, k or v.
  * Sequences are worked on in chunks of 64 tokens on the matrix units, the states between them are fp32; where queries meet them they are the
  * sum of two fp16 (22 bits), scaled to the state's largest element, and weighted scores and keys are sums of bf16: all results are right up to their
  * own rounding to bf16, those of inputs that have means too.  A value of a row that is not finite (padding aside) may show in the results of every
@@ -349,7 +350,7 @@ int linear_attention_forward(const void* q, const void* k, const void* v, const 
  * with R_t = lambda R_(t+1) + scale sum_h q_t^h d_o_t^hT (sum over the query heads h of group j; the last token adds d_state_out),
  *   dq_t^h = scale S_t d_o_t^h,  dk_t = R_t v_t,  dv_t = R_t^T k_t,  d_state_in = lambda R_0
  * q, k, v, log_decay, lengths and state_in are those of the forward; nothing is saved between the two, the states are formed again.
- * d_state_in may be NULL, and may alias d_state_out.  The outputs must not overlap the bf16 inputs.
+ * d_state_in may be NULL, and may alias d_state_out; it must not overlap state_in.  dq, dk and dv must not overlap the bf16 inputs.
  * workspace: linear_attention_backward_workspace_bytes(...).                                                 */
 size_t linear_attention_backward_workspace_bytes(int64_t batch, int64_t seq, int64_t n_q_heads, int64_t n_kv_heads,
                                                  int64_t head_dim);
@@ -359,7 +360,8 @@ int linear_attention_backward(const void* q, const void* k, const void* v, const
                               void* dq, void* dk, void* dv, float* d_state_in, void* workspace, void* stream);
 
 /* linear_attention_forward for one more token of every row (seq 1), the state updated in place: q, o [B, Hq, dh], k, v [B, Hkv, dh],
- * state [B, Hkv, dh, dh] f32.  A row of length 0 takes no token: its o is 0 and its state stays as it is.    */
+ * state [B, Hkv, dh, dh] f32.  A row of length 0 takes no token: its o is 0 and its state stays as it is.
+ * o must not overlap q, k or v.                                                                              */
 int linear_attention_step(const void* q, const void* k, const void* v, const float* log_decay, const int64_t* lengths,
                           float* state, int64_t batch, int64_t n_q_heads, int64_t n_kv_heads, int64_t head_dim,
                           float scale, void* o, void* stream);

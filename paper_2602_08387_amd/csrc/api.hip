@@ -663,6 +663,21 @@ static int linear_shape_ok(const char* who, int64_t batch, int64_t seq, int64_t 
   return 0;
 }
 
+// Whether `bytes` from a and `more` from b have any in common; a null pointer has none.
+static bool overlap(const void* a, uint64_t bytes, const void* b, uint64_t more) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return a && b && (x < y ? y - x < bytes : x - y < more);
+}
+// Bytes of a bf16 tensor, or of the fp32 states; unsigned, since a product past 64 bits belongs to no tensor there is.
+static uint64_t heads_bytes(int64_t batch, int64_t seq, int64_t heads, int64_t dh) { return (uint64_t)batch * seq * heads * dh * 2; }
+static uint64_t states_bytes(int64_t batch, int64_t heads, int64_t dh) { return (uint64_t)batch * heads * dh * dh * 4; }
+// A call's workgroups read these inputs after others have written `out` (of_q, of_kv: bytes of a tensor of the query and of the KV heads).
+static bool over_inputs(const void* out, uint64_t bytes, const void* q, const void* d_o, uint64_t of_q, const void* k, const void* v, uint64_t of_kv) {
+  return overlap(out, bytes, q, of_q) || overlap(out, bytes, d_o, of_q) || overlap(out, bytes, k, of_kv) || overlap(out, bytes, v, of_kv);
+}
+// In place, or apart: a state is read as it is written, element by element.
+static bool shifted(const void* a, const void* b, uint64_t bytes) { return a != b && overlap(a, bytes, b, bytes); }
+
 size_t linear_attention_workspace_bytes(int64_t batch, int64_t seq, int64_t n_q_heads, int64_t n_kv_heads, int64_t head_dim) {
   if (linear_shape_ok("linear_attention_workspace_bytes", batch, seq, n_q_heads, n_kv_heads, head_dim)) return 0;
   return linear_attention_fwd_workspace(batch, seq, n_q_heads, n_kv_heads, head_dim);
@@ -675,6 +690,9 @@ int linear_attention_forward(const void* q, const void* k, const void* v, const 
   REQUIRE_PTR(q); REQUIRE_PTR(k); REQUIRE_PTR(v); REQUIRE_PTR(o); REQUIRE_PTR(workspace);
   REQUIRE(log_decay != nullptr, "linear_attention_forward: log_decay is null");
   REQUIRE(aligned16(state_in) && aligned16(state_out), "linear_attention_forward: a state is not 16-byte aligned");
+  const uint64_t of_q = heads_bytes(batch, seq, n_q_heads, head_dim), of_kv = heads_bytes(batch, seq, n_kv_heads, head_dim);
+  REQUIRE(!over_inputs(o, of_q, q, nullptr, of_q, k, v, of_kv), "linear_attention_forward: o must not overlap q, k or v");
+  REQUIRE(!shifted(state_out, state_in, states_bytes(batch, n_kv_heads, head_dim)), "linear_attention_forward: state_out must be state_in or not overlap it");
   TRY(check_device());
   return launch_linear_attention_fwd(LinearCall{q, k, v, log_decay, lengths, batch, seq, n_q_heads, n_kv_heads, head_dim, scale}, state_in,
                                      o, state_out, workspace, (hipStream_t)stream);
@@ -693,6 +711,12 @@ int linear_attention_backward(const void* q, const void* k, const void* v, const
   REQUIRE_PTR(q); REQUIRE_PTR(k); REQUIRE_PTR(v); REQUIRE_PTR(d_o); REQUIRE_PTR(dq); REQUIRE_PTR(dk); REQUIRE_PTR(dv); REQUIRE_PTR(workspace);
   REQUIRE(log_decay != nullptr, "linear_attention_backward: log_decay is null");
   REQUIRE(aligned16(state_in) && aligned16(d_state_out) && aligned16(d_state_in), "linear_attention_backward: a state is not 16-byte aligned");
+  const uint64_t of_q = heads_bytes(batch, seq, n_q_heads, head_dim), of_kv = heads_bytes(batch, seq, n_kv_heads, head_dim);
+  const uint64_t of_state = states_bytes(batch, n_kv_heads, head_dim);
+  REQUIRE(!over_inputs(dq, of_q, q, d_o, of_q, k, v, of_kv) && !over_inputs(dk, of_kv, q, d_o, of_q, k, v, of_kv) &&
+          !over_inputs(dv, of_kv, q, d_o, of_q, k, v, of_kv), "linear_attention_backward: dq, dk and dv must not overlap q, k, v or d_o");
+  REQUIRE(!overlap(d_state_in, of_state, state_in, of_state), "linear_attention_backward: d_state_in must not overlap state_in, from which dq is formed");
+  REQUIRE(!shifted(d_state_in, d_state_out, of_state), "linear_attention_backward: d_state_in must be d_state_out or not overlap it");
   TRY(check_device());
   return launch_linear_attention_bwd(LinearCall{q, k, v, log_decay, lengths, batch, seq, n_q_heads, n_kv_heads, head_dim, scale}, state_in,
                                      d_o, d_state_out, dq, dk, dv, d_state_in, workspace, (hipStream_t)stream);
@@ -703,6 +727,8 @@ int linear_attention_step(const void* q, const void* k, const void* v, const flo
   TRY(linear_shape_ok("linear_attention_step", batch, 1, n_q_heads, n_kv_heads, head_dim));
   REQUIRE_PTR(q); REQUIRE_PTR(k); REQUIRE_PTR(v); REQUIRE_PTR(state); REQUIRE_PTR(o);
   REQUIRE(log_decay != nullptr, "linear_attention_step: log_decay is null");
+  const uint64_t of_q = heads_bytes(batch, 1, n_q_heads, head_dim), of_kv = heads_bytes(batch, 1, n_kv_heads, head_dim);
+  REQUIRE(!over_inputs(o, of_q, q, nullptr, of_q, k, v, of_kv), "linear_attention_step: o must not overlap q, k or v");
   TRY(check_device());
   return launch_linear_attention_step(LinearCall{q, k, v, log_decay, lengths, batch, 1, n_q_heads, n_kv_heads, head_dim, scale}, state, o,
                                       (hipStream_t)stream);
