@@ -430,11 +430,16 @@ int issue_rate_probe(int family, int variant, int waves_per_simd, double* result
  * 3 256x256, persistent workgroups), tile of the second launch or -1, rows (of all n together) in the first.
  *
  * attention_backward_pieces: workgroups that share the work of 128 keys in the dK/dV pass of attention_backward (0: a shape
- * it rejects).                                                                                       */
+ * it rejects).
+ *
+ * linear_attention_plan: how linear_attention_forward (backward 0) or _backward (1) cuts its work.  plan (3 ints): chunks of 64 tokens in a
+ * segment, segments of a sequence, parts into which the query heads of a group are dealt for o (dq), each of as many heads as the first but the last.  */
 int gemm_route(int32_t operands, int32_t epilogue, int32_t head_dim, int32_t compute_units, int32_t n,
                const int64_t* M, const int64_t* N, const int64_t* K, int32_t* route);
 int attention_backward_pieces(int64_t batch, int64_t seq, int64_t n_q_heads, int64_t n_kv_heads,
                               int64_t head_dim, int32_t compute_units);
+int linear_attention_plan(int64_t batch, int64_t seq, int64_t n_q_heads, int64_t n_kv_heads, int64_t head_dim, int32_t backward,
+                          int32_t* plan);
 
 #ifdef __cplusplus
 }

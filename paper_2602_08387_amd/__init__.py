@@ -23,6 +23,7 @@ _BINDING_NAMES = (
     "linear_attention_step",
     "swiglu_forward", "swiglu_backward", "embed_forward", "embed_backward_workspace_bytes", "embed_backward",
     "grad_sq_norm_workspace_bytes", "grad_sq_norm", "adamw_step", "issue_rate_probe", "gemm_route", "attention_backward_pieces",
+    "linear_attention_plan",
     "EXPORTED_SYMBOLS", "WEIGHT_FIELDS",
 )
 

@@ -22,6 +22,7 @@ EXPORTED_SYMBOLS = (
     "linear_attention_step",
     "swiglu_forward", "swiglu_backward", "embed_forward", "embed_backward_workspace_bytes", "embed_backward",
     "grad_sq_norm_workspace_bytes", "grad_sq_norm", "adamw_step", "issue_rate_probe", "gemm_route", "attention_backward_pieces",
+    "linear_attention_plan",
 )
 
 
@@ -110,6 +111,7 @@ def _load():
         "issue_rate_probe": (C.c_int, [C.c_int, C.c_int, C.c_int, vp, vp]),
         "gemm_route": (C.c_int, [i32, i32, i32, i32, i32, vp, vp, vp, vp]),
         "attention_backward_pieces": (C.c_int, [i64, i64, i64, i64, i64, i32]),
+        "linear_attention_plan": (C.c_int, [i64, i64, i64, i64, i64, i32, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(l, name)
@@ -403,3 +405,10 @@ def gemm_route(operands, epilogue, Ms, Ns, Ks, head_dim=0, compute_units=0):
 
 def attention_backward_pieces(batch, seq, n_q_heads, n_kv_heads, head_dim, compute_units=0) -> int:
     return lib.attention_backward_pieces(batch, seq, n_q_heads, n_kv_heads, head_dim, compute_units)
+
+
+def linear_attention_plan(batch, seq, n_q_heads, n_kv_heads, head_dim, backward=False):
+    """(chunks in a segment, segments of a sequence, parts of a group's query heads)"""
+    plan = (C.c_int32 * 3)()
+    _check(lib.linear_attention_plan(batch, seq, n_q_heads, n_kv_heads, head_dim, int(backward), plan), "linear_attention_plan")
+    return tuple(plan)

@@ -842,6 +842,13 @@ int attention_backward_pieces(int64_t batch, int64_t seq, int64_t n_q_heads, int
   return attention_bwd_pieces(batch, seq, n_q_heads, n_kv_heads, head_dim, compute_units > 0 ? compute_units : dl::compute_units());
 }
 
+int linear_attention_plan(int64_t batch, int64_t seq, int64_t n_q_heads, int64_t n_kv_heads, int64_t head_dim, int32_t backward, int32_t* plan) {
+  TRY(linear_shape_ok("linear_attention_plan", batch, seq, n_q_heads, n_kv_heads, head_dim));
+  REQUIRE(plan != nullptr && (backward == 0 || backward == 1), "linear_attention_plan: plan is null, or backward not 0 or 1");
+  query_linear_attention_plan(backward != 0, batch, seq, n_q_heads, n_kv_heads, head_dim, plan);
+  return DLAYER_OK;
+}
+
 int issue_rate_probe(int family, int variant, int waves_per_simd, double* result, void* stream) {
   REQUIRE(result != nullptr, "issue_rate_probe: result is null");
   REQUIRE(family >= 0 && family <= 3 && variant >= 0 && variant <= 3, "issue_rate_probe: family 0..3, variant 0..3");

@@ -161,6 +161,8 @@ size_t linear_attention_bwd_workspace(int64_t B, int64_t S, int64_t Hq, int64_t 
 int launch_linear_attention_bwd(const LinearCall& c, const float* s_in, const void* d_o, const float* ds_out, void* dq, void* dk, void* dv,
                                 float* ds_in, void* workspace, hipStream_t st);
 int launch_linear_attention_step(const LinearCall& c, float* state, void* o, hipStream_t st);
+// see linear_attention_plan in dlayer.h
+void query_linear_attention_plan(bool backward, int64_t B, int64_t S, int64_t Hq, int64_t Hkv, int64_t dh, int32_t* plan);
 
 // ---- ce.hip
 size_t ce_workspace(int64_t T, int64_t V);

@@ -928,6 +928,12 @@ static LinearPlan linear_plan(bool backward, int64_t pairs, int64_t S, int64_t H
   }
   return best;
 }
+void query_linear_attention_plan(bool backward, int64_t B, int64_t S, int64_t Hq, int64_t Hkv, int64_t dh, int32_t* plan) {
+  const LinearPlan p = linear_plan(backward, B * Hkv, S, Hq, Hkv, dh);
+  plan[0] = p.seg_chunks;
+  plan[1] = p.nseg;
+  plan[2] = p.parts;
+}
 // room for the states of all segments: a size that does not fall as the call grows
 static size_t segment_bytes(int64_t pairs, int64_t S, int64_t dh) {
   const int64_t chunks = (S + kChunk - 1) / kChunk;
