@@ -155,7 +155,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 __device__ __forceinline__ f32x4 mfma16_f16(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
 // Powers of two that take numbers up to some bound into the upper half of fp16's range (below 2^15, so that what is 2^29 times smaller than
-// the bound keeps its eleven bits, and eleven more in a second term), and back.  exponent: of the bound, as an fp32 has it.
+// the bound keeps its eleven bits, and what these round off, down to 2^40 times smaller, a second fp16), and back.  exponent: of the bound, as an fp32 has it.
 struct Scale {
   float up, down;
   __device__ __forceinline__ explicit Scale(int exponent) {
@@ -235,8 +235,7 @@ __device__ __forceinline__ void weights_from_start(float* w, float log2, float m
   if (threadIdx.x < kChunk) w[threadIdx.x] = mult * power(log2, before + (int)threadIdx.x + 1);
 }
 
-constexpr float kLowTerm = 1.f / 4096;   // unit of the second term of a state as an operand
-// Both terms lie in LDS.  Of a 128 x 128 state, two workgroups' would take 192 of a compute unit's 160 KB: there they take turns in one place.  (One workgroup a
+// Both terms of a state as an operand lie in LDS.  Of a 128 x 128 state, two workgroups' would take 192 of a compute unit's 160 KB: there they take turns in one place.  (One workgroup a
 // compute unit, with registers to load the next tiles ahead: 117 us for 110 in the forward's last kernel, 16384 tokens of 32 and 8 heads of 128, 265
 // for 246 in the gradients'.)
 template <int D> constexpr bool kBothTerms = D < 128;
@@ -330,13 +329,12 @@ struct State {
     m = fmaxf(m, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(m), 0x122, 0xf, 0xf, true)));
     return fmaxf(m, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(m), 0x121, 0xf, 0xf, true)));
   }
-  // to LDS [columns][rows]: an operand along either.  The scaled state is the sum of two fp16: its rounding and, in units of kLowTerm, what that rounds off (at
-  // most 8; no number where the first is infinite, which the clamp keeps out of the product).  The second lies behind the first, or low says which is meant.
+  // to LDS [columns][rows]: an operand along either.  The scaled state is the sum of two fp16: its rounding and what that rounds off (at most 8; no
+  // number where the first is infinite, which the clamp keeps out of the product).  The second lies behind the first, or low says which is meant.
   __device__ __forceinline__ void to_lds(char* t, float up, bool low, int wave, int lane) const {
     if (!holds(wave)) return;
     lane = here(lane);
     up = here(up);   // no conversion ahead of the barrier in front of this
-    const float bound = low ? 8.f : INFINITY, unit = low ? 1.f / kLowTerm : 1.f;
 #pragma unroll
     for (int i = 0; i < RB; ++i)
 #pragma unroll
@@ -344,12 +342,14 @@ struct State {
         f16x4 v, rest;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float x = a[i][j][e] * up, h = (float)(_Float16)x;
+          const float x = a[i][j][e] * up;
+          const _Float16 h = (_Float16)x;
+          const float off = __builtin_amdgcn_fmed3f(x - (float)h, -8.f, 8.f);
           if (kBothTerms<D>) {
-            v[e] = (_Float16)h;
-            rest[e] = (_Float16)(__builtin_amdgcn_fmed3f(x - h, -8.f, 8.f) * (1.f / kLowTerm));
+            v[e] = h;
+            rest[e] = (_Float16)off;
           } else {
-            v[e] = (_Float16)(__builtin_amdgcn_fmed3f(x - (low ? h : 0.f), -bound, bound) * unit);
+            v[e] = (_Float16)(low ? off : x);
           }
         }
         const int r = row(row_block(wave) + i, lane), p = (col_block(wave) + j) * 16 + (lane & 15);
@@ -623,20 +623,17 @@ __device__ __forceinline__ void out_tile(f32x4 (&o)[NB], const bf16x8 (&qf)[D / 
   if (some) {   // last, when the queries as they are need no registers any more
     const ScaledRow<KS> qs(qf);
     const float after = power(log2, tile * 16 + (here(lane) & 15) + 1) * scale * sc.down * qs.down;
-    const auto add = [&](int t, float factor) {
+    const auto add = [&](int t) {
       const uint32_t at = here(sl);
-      add_scaled<KS>(o, qs, factor, [&](int n, int k) { return Rows<D>::along(at, t, n * 16, k); });
+      add_scaled<KS>(o, qs, after, [&](int n, int k) { return Rows<D>::along(at, t, n * 16, k); });
     };
-    if constexpr (kBothTerms<D>) {
-      add(st + D * D * 2, after * kLowTerm);
-      add(st, after);
-    } else {
-      add(st, low ? after * kLowTerm : after);
+    add(st);
+    if constexpr (!kBothTerms<D>) {
       __syncthreads();
       s.to_lds(smem + st, sc.up, !low, wave, lane);
       __syncthreads();
-      add(st, low ? after : after * kLowTerm);
     }
+    add(st + kStateLds<D> - D * D * 2);
   }
 }
 
@@ -812,8 +809,6 @@ __device__ __forceinline__ void segment_keys(const LinearArgs& p, int id, char* 
         }
       };
       add(lt);
-#pragma unroll
-      for (int n = 0; n < NB; ++n) acc[n] *= kLowTerm;
       if constexpr (!kBothTerms<D>) {
         __syncthreads();
         s.to_lds(smem + et, sc.up, false, wave, lane);

@@ -113,6 +113,22 @@ def test_backward(K, B, S, Hq, Hkv, dh, mean, decay, carry):
     _state_close(d_state, ref[3], "d_state_in")
 
 
+@pytest.mark.parametrize("dh,mean", [(32, 1.0), (64, 1.0), (128, 2.0)])
+def test_columns_of_different_size(K, dh, mean):
+    """Values whose columns' sizes span 2^16: every column of o is right by itself (o = S^T q keeps them apart), although the state meets queries scaled as a whole."""
+    B, S, Hq, Hkv = 1, 1500, 2, 1
+    bits = _inputs(B, S, Hq, Hkv, dh, mean, dh + 5)
+    size = 2.0 ** -(np.arange(dh) * 16 // (dh - 1))
+    bits["v"] = si.f32_to_bf16_bits((si.bf16_bits_to_f64(bits["v"]) * size).astype(np.float32))   # exact
+    q, k, v = (dev_bf16(bits[n]) for n in "qkv")
+    log, o, scale = np.full(Hkv, SLOW, np.float32), torch.empty_like(q), dh ** -0.5
+    K.linear_attention_forward(q, k, v, torch.from_numpy(log).cuda(), None, None, B, S, Hq, Hkv, dh, scale, o, None,
+                               torch.empty(K.linear_attention_workspace_bytes(B, S, Hq, Hkv, dh), dtype=torch.uint8, device="cuda"))
+    o_ref, _ = otm.linear_attention_fwd(*(si.bf16_bits_to_f64(bits[n]) for n in "qkv"), log.astype(np.float64), scale)
+    for c in range(dh):
+        _close(o[..., c], o_ref[..., c], f"column {c}, of size {size[c]}")
+
+
 @pytest.mark.parametrize("dh", [32, 64, 128])
 def test_an_infinite_element_of_a_state_stays_in_its_column(K, dh):
     B, S, Hq, Hkv = 1, 100, 2, 1
