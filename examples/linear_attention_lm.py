@@ -3,7 +3,7 @@
 
     python examples/linear_attention_lm.py
 
-One block between an embedding and an LM head, all of it the library's kernels (torch holds the memory and picks the likeliest token):
+One block between an embedding and an LM head, all of it the library's kernels (torch holds the memory, puts the gradients of q, k and v side by side and picks the likeliest token):
 
     h = RMSNorm(x);  q, k, v = h Wq^T, h Wk^T, h Wv^T;  q, k <- qk_norm_rope(q, k);  y = x + linear_attention(q, k, v) Wo^T
 

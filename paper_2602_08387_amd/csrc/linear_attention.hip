@@ -11,9 +11,10 @@
 //   E' = lambda^64 E + scale sum_i (lambda^(i+1) q_i) do_i^T
 // A chain of 64-token steps is long, so a sequence is cut into segments (linear_plan) that run side by side: a first kernel forms
 // what each segment adds to the state, a second adds these up from segment to segment, and the third does the chunks of a segment, starting
-// from the state it begins (ends) with.  Bound by memory: what this reads twice, and the states between the kernels, are the distance to one
-// pass over the data (16384 tokens of 32 and 8 heads of 128: 117 us, 0.54 GB; a pass over them 0.34 GB, 70 us.  Backward: 288 us, 1.23 GB;
-// 0.54 GB, 113 us); the bytes that move do so at 4.3 to 4.6 TB/s, where a copy reaches 4.76.
+// from the state it begins (ends) with.  16384 tokens of 32 and 8 heads of 128 take 138 us, and 0.54 GB move (one pass over the data: 0.34 GB, 70 us at a
+// copy's 4.76 TB/s; the rest is k and v read twice and the states between the kernels); backward 309 us and 1.24 GB (0.54 GB, 113 us).  Nothing is at its
+// limit alone.  The sums over segments wait for their loads (3.8 to 4.5 TB/s; as long without their products); the kernels that do the chunks move 3.1 to
+// 3.4 TB/s, and the vector units issue in 56 to 69 % of the cycles beside 15 to 32 % of the matrix units'.
 //
 // Precision.  States are fp32, in the accumulators and in memory; as operands they are the sum of two fp16, scaled by a power of two: 22 bits, and queries,
 // scaled too, are exact in fp16.  Keys and values that have means make a state a large rank-one part and, in front of it, what tells tokens apart, which is all that
@@ -408,7 +409,7 @@ __device__ __forceinline__ Scale state_scale(const float* largest) {
 
 // A 16 x 16 block of scores, whose lane holds four keys of one query (STEP -1) or four queries of one key (STEP 1), times mult lambda^(place of the query -
 // place of the key); what is not causal becomes 0.  blocks: from the key's to the query's, -1 .. 3.  The same work for every block, without branches, so
-// that two of them, their reads and products, pass together: with branches around what is not causal, and one power of the lane's for the blocks off the
+// that two of them, their reads and products, pass together (times with a state of one term): with branches around what is not causal, and one power of the lane's for the blocks off the
 // diagonal, dk, dv and dq of 4096 tokens of 32 heads of 64 on one KV head take 49.6 us for 44.7, the forward's last kernel 80 for 78 (16384 tokens
 // of 32 and 8 heads of 128); heads of 64 that share nothing 36.9 for 37.4.
 // (Beside a state of 128 x 128 no register is left for what a lane derives from its number and keeps: the caller passes here(lane).)
@@ -489,8 +490,8 @@ __device__ __forceinline__ float log2_decay(float g) { return (float)(decay_log(
 // ------------------------------------------------------------------------------------------
 // What a segment of m tokens adds to the state that passes through it: sum_t lambda^(m-1-t) k_t v_t^T, from k and v;
 // GRADIENT: to the state's gradient, sum over t and the group's heads of scale lambda^(t+1) q_t do_t^T, from q and d_o.
-// Bound by its loads: without its products it takes as long.  25 us at 16384 tokens of 8 KV heads of 128 (0.1 GB), 86 us in their backward with
-// 32 heads (0.37 GB); the gradients' sums dealt to workgroups by heads, so that they end with the states', came to the same, and cost the scan.
+// Bound by its loads: without its products it takes as long.  27 us at 16384 tokens of 8 KV heads of 128 (0.1 GB, 3.8 TB/s), 86 us in their backward with
+// 32 heads (0.37 GB, 4.3 TB/s); the gradients' sums dealt to workgroups by heads, so that they end with the states', came to the same, and cost the scan.
 // ------------------------------------------------------------------------------------------
 template <int D, int SPLIT, bool GRADIENT>
 __device__ __forceinline__ void segment_sum(const LinearArgs& p, char* smem) {
@@ -547,7 +548,7 @@ __global__ __launch_bounds__(64 * kLinWaves, 4) void linear_segment_kernel(const
 // ------------------------------------------------------------------------------------------
 // From segment to segment: what each adds is replaced by the state it begins with; GRADIENT: by the gradient of the state it ends
 // with.  A thread holds four elements of a state in fp64 (a decay of many tokens has no second fp32), eight segments ahead in flight.
-// 13.6 us for 512 states of 128 x 128 (67 MB read and written, 4.9 TB/s).
+// 14 us for 512 states of 128 x 128 (67 MB read and written, 4.8 TB/s).
 // ------------------------------------------------------------------------------------------
 template <int D, bool GRADIENT>
 __device__ __forceinline__ void segment_scan(const LinearArgs& p) {
@@ -593,7 +594,8 @@ __global__ __launch_bounds__(256) void linear_scan_kernel(const LinearArgs a, co
 // ------------------------------------------------------------------------------------------
 // o of a segment (dq of one, from d_o, v, k): its chunks from the first to the last, the state in the accumulators and, as an operand, in
 // LDS.  Four waves take 16 queries of a head each, the other four those of the next head; an odd last head is shared, half of the columns
-// for either.  78 us at 16384 tokens of 32 and 8 heads of 128 (0.37 GB, 4.7 TB/s).
+// for either.  110 to 120 us at 16384 tokens of 32 and 8 heads of 128 (0.37 GB, 3.1 to 3.4 TB/s), of which the state's second term is 30: 10 its
+// products, 12 its conversion, 8 the barriers (each timed without it).
 // SPLIT: 3 where the state goes on to the caller, 2 where it serves this kernel's products alone.
 // ------------------------------------------------------------------------------------------
 // NB blocks of 16 columns from n0 of o for the query that the lane's row is.  some: there is a state, scaled by sc; low: of its terms the second is in LDS,
@@ -856,8 +858,8 @@ __device__ __forceinline__ void segment_keys(const LinearArgs& p, int id, char* 
   if (!p.seg && p.s_out) s.store_matrix(p.s_out + (int64_t)pair * D * D, wave, lane);
 }
 
-// The three gradients of a call in one launch: first the workgroups for dk and dv of `g`, which take longest, then those for dq of `a`.  192 us at 16384
-// tokens of 32 and 8 heads of 128 (0.79 GB, 4.1 TB/s).  (Both kinds alternating by eights, so that a segment's do, k and v would come from memory
+// The three gradients of a call in one launch: first the workgroups for dk and dv of `g`, which take longest, then those for dq of `a`.  233 us at 16384
+// tokens of 32 and 8 heads of 128 (0.80 GB, 3.4 TB/s).  (With a state of one term: both kinds alternating by eights, so that a segment's do, k and v would come from memory
 // once for both: 256 us when this order took 227.  A head's q and do asked for while the one before is worked on: no change, but for heads of
 // 64 of which very many share a KV head, a fifth less at 32 of one.)
 template <int D, int SPLIT>
@@ -880,9 +882,9 @@ struct LinearPlan { int seg_chunks, nseg, parts; };
 
 // Time in us of a call whose sequences are cut into n: chains of chunks, or the bytes that move where they take longer.  The constants (us for a chunk, D 128,
 // 64, 32: a workgroup of linear_out_kernel with up to two heads, and for a further two; one for dk and dv, and for each head of the group; one tile pair of
-// linear_segment_kernel) are 1.3 times what single workgroups take with their inputs in the caches.  Workgroups that share compute units take 1.3 (1.6)
-// times as long; 4.3 TB/s.  Over 152 shapes of 128 to 8192 tokens, timed with every power of two, the choice is 1 % slower than the best on average, at
-// worst 1.25 times (75 us for 60); one segment throughout would be 3.8 times slower, always the most 1.2 times.
+// linear_segment_kernel) are 1.3 times what single workgroups took with their inputs in the caches and a state of one term.  Workgroups that share compute
+// units take 1.3 (1.6) times as long; 4.3 TB/s.  Over 152 shapes of 128 to 8192 tokens, timed with every power of two, the choice is 1 % slower than the
+// best on average, at worst 1.24 times (92 us for 74); one segment throughout would be 3.9 times slower, always the most 1.2 times.
 static double linear_time(bool backward, double pairs, int chunks, int G, int64_t D, int n, LinearPlan* plan) {
   static const double kStep[3][5] = {{6.5, 3.3, 4.7, 3.6, 2.9}, {3.5, 1.7, 2.5, 2.2, 1.6}, {2.5, 1.0, 1.7, 1.4, 1.2}};
   const double* c = kStep[D == 128 ? 0 : D == 64 ? 1 : 2];
@@ -1020,10 +1022,10 @@ int launch_linear_attention_bwd(const LinearCall& c, const float* s_in, const vo
 }
 
 // ------------------------------------------------------------------------------------------
-// One token for every batch row.  Bound by HBM: the state is read and written once, 8 bytes an element: 256 rows of 8 states of 128 x 128 in 46.5
-// us (0.28 GB, 6.0 TB/s); of one row by what waits for each other, 4.1 us.  Workgroup: COLS columns of one state; a thread holds four columns of
+// One token for every batch row.  Bound by HBM: the state is read and written once, 8 bytes an element: 256 rows of 8 states of 128 x 128 in 60
+// us (0.28 GB, 4.7 TB/s, a copy's rate; 46.5 us where the memory's side cache holds a part of them from call to call); of one row by what waits for each other, 3.9 us.  Workgroup: COLS columns of one state; a thread holds four columns of
 // every RG-th row, so that the state stays in registers between its update and the products with the group's queries.  HEADS of these at once, read
-// before the state is: one after the other a group of four takes 4.6 and 49 us; but four where there is one, 6.6 us for 4.6 (40 rows of 12
+// before the state is: one after the other a group of four takes 4.6 and, from that cache, 49 us; but four where there is one, 6.6 us for 4.6 (40 rows of 12
 // heads of 64), and one of two 4.6 for 4.2.
 // ------------------------------------------------------------------------------------------
 template <int D, int COLS, int HEADS>

@@ -3,8 +3,8 @@
 //   forward   z = x rstd gamma,  rstd = (mean x^2 + eps)^(-1/2) over the head's dh values;  y = R(p) z
 //   backward  dz = R(-p) dy;  dgamma = sum dz x rstd;  dxh = dz gamma;  dx = rstd (dxh - x rstd mean(dxh x rstd))
 //
-// Both are bound by HBM: 4 bytes an element forward, 6 backward; 16384 tokens of 32 and 8 heads of 128 in 71 and 97 us (0.34 and 0.51 GB, 4.8 and
-// 5.2 TB/s), one token in 3.3, the launch.  A head's row is dh / 8 lanes of 16 bytes, so a wave holds
+// Both are bound by HBM: 4 bytes an element forward, 6 backward; 16384 tokens of 32 and 8 heads of 128 in 70 us (0.34 GB, 4.8 TB/s) and 102 (0.51 GB, 5.1 TB/s
+// in the kernel's 98, and the gains' sums), one token in 3.3, the launch.  A head's row is dh / 8 lanes of 16 bytes, so a wave holds
 // 4 to 16 rows and everything a row needs stays within 4 to 16 lanes: the mean and, for split pairs, the other member of a
 // pair come from lane exchanges in the register file (DPP), not through LDS.  A wave takes a token (or, of few tokens, a part of its
 // heads), so that the token's angles are evaluated once: in fp64, one pair a lane, handed to the lanes that need them through LDS as fp32.
