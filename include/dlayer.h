@@ -367,6 +367,84 @@ int linear_attention_step(const void* q, const void* k, const void* v, const flo
                           float scale, void* o, void* stream);
 
 /* ------------------------------------------------------------------------------------------
+ * Generating with the softmax attention: a paged cache of keys and values, attention of new tokens over it, and log-probabilities of
+ * tokens.  Not part of the layer the paper benchmarks; the layer's weights run with it (rmsnorm_forward, linear_forward and
+ * linear_swiglu_forward take any number of tokens).
+ *
+ * Position p of batch row b lies in page page_table[b, p / page_size], slot p % page_size.  A page that does not exist (an entry outside
+ * 0 .. n_pages - 1) and positions behind the table (p >= max_pages * page_size) or below 0 hold nothing: what would be written there is
+ * dropped, and what is read from there is not there.  Rows may share pages that nothing is written to (a common prefix).  start and
+ * lengths are those of the token mixing above: start[b] tokens of row b are in the cache before the call, its lengths[b] new ones have
+ * positions start[b] ...; NULL: 0, and seq.  What a page holds behind a row's last token is never read, padding neither.
+ * The cache may exceed 4 GiB.  batch, seq: any positive numbers; max_pages * page_size, seq * n_q_heads and the workgroups of a call
+ * stay below 2^31.
+ * ------------------------------------------------------------------------------------------ */
+
+#define DLAYER_CACHE_BF16 0
+/* Each vector (a token's head) as head_dim e4m3 values (largest 448, no infinities) in units of a power of two of its own, the smallest
+ * that brings the vector's largest magnitude within 448 (not below 2^-110).  Values that are not finite are held as NaN.  What is held is read exactly.          */
+#define DLAYER_CACHE_E4M3 1
+
+typedef struct dlayer_kv_cache {
+  void *k, *v;                 /* [n_pages, n_kv_heads, page_size, head_dim], bf16 or e4m3                     */
+  void *k_scale, *v_scale;     /* e4m3: the powers of two, [n_pages, n_kv_heads, page_size], a byte (exponent + 127) each; else NULL */
+  const int32_t* page_table;   /* [batch, max_pages] on the device                                             */
+  int32_t n_pages, n_kv_heads, page_size, head_dim, batch, max_pages;   /* page_size: a power of two from 16 to 4096 */
+  int32_t dtype;               /* DLAYER_CACHE_BF16 or DLAYER_CACHE_E4M3                                       */
+} dlayer_kv_cache;
+
+/* New keys and values into the cache: k, v [B*S, Hkv, dh] bf16, token t of row b at position start[b] + t.
+ * rope_base > 0: keys are rotated to their positions on the way (angle and pairings as in dlayer_cfg, evaluated in fp64), and the queries
+ * q [B*S, Hq, dh] bf16 beside them, into q_out (may be q; padding is written as 0); q and q_out may both be NULL (n_q_heads is then
+ * ignored).  rope_base 0: no rotation (of keys rotated before, as by qk_norm_rope_forward), q and q_out NULL.
+ * Rounded once, from fp32, into the cache's type.  No two rows of the batch may write to one page; k and v must not overlap the cache.       */
+int kv_cache_append(const dlayer_kv_cache* cache, const void* q, const void* k, const void* v, const int64_t* start,
+                    const int64_t* lengths, int64_t seq, int64_t n_q_heads, float rope_base, int32_t rope_layout, void* q_out,
+                    void* stream);
+
+/* Keys and values of positions start[b] .. start[b] + lengths[b] - 1 back from the cache: k, v [B*S, Hkv, dh] bf16, the values that are held; 0 for
+ * padding and where the cache holds nothing.                                                                 */
+int kv_cache_read(const dlayer_kv_cache* cache, const int64_t* start, const int64_t* lengths, int64_t seq, void* k, void* v,
+                  void* stream);
+
+/* Attention of new tokens over the cache, their own keys and values among it (kv_cache_append comes first).  The token at position p
+ * sees the positions 0 .. p that the cache holds:
+ *   o = sum_s exp(scale q . k_s - lse) v_s,   lse = log sum_s exp(scale q . k_s)
+ * with query head h reading KV head h / (Hq / Hkv).  One new token a row (generation) or many (a prompt, or a piece of one).
+ * q, o [B*S, Hq, dh] bf16, lse [B, Hq, S] f32 or NULL.  A token that sees nothing, and padding, have o = 0 and lse = -infinity.
+ * scale > 0.  A value that is not finite shows in the results of those tokens that see it, and of no others.  o must not overlap q or the cache.
+ * workspace: paged_attention_workspace_bytes(cache, seq, n_q_heads), which reads the sizes of cache only and does not fall as batch, seq
+ * or max_pages grows.                                                                                        */
+size_t paged_attention_workspace_bytes(const dlayer_kv_cache* cache, int64_t seq, int64_t n_q_heads);
+int paged_attention_forward(const dlayer_kv_cache* cache, const void* q, const int64_t* start, const int64_t* lengths, int64_t seq,
+                            int64_t n_q_heads, float scale, void* o, float* lse, void* workspace, void* stream);
+
+/* Log-probabilities of given tokens under z = inverse_temperature * logits (a policy's scores, or what was just generated), the entropy of
+ * each row's distribution, and its likeliest tokens:
+ *   lse = log sum_v exp(z_v),  logprobs = z[targets] - lse,  entropy = -sum_v p_v log p_v,  p = exp(z - lse)
+ * logits: T rows of V bf16, ld elements apart (ld % 8 == 0, V <= ld: what lies behind the vocabulary is not read for any result).  targets
+ * [T] int64: a row whose target lies outside 0 .. V - 1 is not scored, its results are 0 and its top_ids -1; targets NULL: every row counts, and
+ * logprobs is NULL.  logprobs, entropy, lse [T] f32; top_ids [T, n_top] int64 and top_logprobs [T, n_top] f32: the n_top (0 .. 64, at
+ * most V) likeliest tokens, likeliest first, of equal logits the lower index first.  Any output may be NULL; top_ids and top_logprobs are where n_top is 0.
+ * Sums in fp32.  Logits of -infinity have probability 0; a row of nothing else has lse and logprobs of -infinity and entropy 0.  A row
+ * that holds NaN or +infinity has NaN for results; NaN are not among its top_ids (which end in -1 where others are too few).
+ * T below 2^22, V and ld below 2^24.  workspace: token_logprobs_workspace_bytes(T, V, n_top), at most 528 KiB; it does not fall as T, V or n_top grows.   */
+size_t token_logprobs_workspace_bytes(int64_t T, int64_t V, int64_t n_top);
+int token_logprobs_forward(const void* logits, const int64_t* targets, int64_t T, int64_t V, int64_t ld, float inverse_temperature,
+                           int64_t n_top, float* logprobs, float* entropy, float* lse, int64_t* top_ids, float* top_logprobs,
+                           void* workspace, void* stream);
+
+/* Gradient of logprobs and entropy: given d_logprobs and d_entropy [T] f32 (either may be NULL for zeros), the logits and targets of the forward and
+ * the lse and entropy that it left,
+ *   dlogits_v = inverse_temperature * (d_logprobs * [v == target] - p_v * (d_logprobs + d_entropy * (log p_v + entropy)))
+ * dlogits [T, ld] bf16, may be logits; written as 0: columns behind the vocabulary, rows that are not scored, and rows of which a mask of -infinity
+ * or of bf16's lowest value has left nothing (an lse of -1e30 or less).
+ * entropy may be NULL where d_entropy is, targets (every row counts) where d_logprobs is.                       */
+int token_logprobs_backward(const void* logits, const int64_t* targets, const float* lse, const float* entropy,
+                            const float* d_logprobs, const float* d_entropy, int64_t T, int64_t V, int64_t ld,
+                            float inverse_temperature, void* dlogits, void* stream);
+
+/* ------------------------------------------------------------------------------------------
  * Optimizer step.  The paper's Training Pipeline paragraph speaks of training steps and names no
  * optimizer; the reading taken is the usual one for this model family: clipping of the gradients by
  * their global norm, then AdamW (Adam with decoupled weight decay).  Parameters and gradients are

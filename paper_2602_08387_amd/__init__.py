@@ -21,6 +21,8 @@ _BINDING_NAMES = (
     "qk_norm_rope_forward", "qk_norm_rope_backward_workspace_bytes", "qk_norm_rope_backward",
     "linear_attention_workspace_bytes", "linear_attention_forward", "linear_attention_backward_workspace_bytes", "linear_attention_backward",
     "linear_attention_step",
+    "KVCache", "DLAYER_CACHE_BF16", "DLAYER_CACHE_E4M3", "kv_cache_append", "kv_cache_read", "paged_attention_workspace_bytes", "paged_attention_forward",
+    "token_logprobs_workspace_bytes", "token_logprobs_forward", "token_logprobs_backward",
     "swiglu_forward", "swiglu_backward", "embed_forward", "embed_backward_workspace_bytes", "embed_backward",
     "grad_sq_norm_workspace_bytes", "grad_sq_norm", "adamw_step", "issue_rate_probe", "gemm_route", "attention_backward_pieces",
     "linear_attention_plan",

@@ -20,6 +20,8 @@ EXPORTED_SYMBOLS = (
     "qk_norm_rope_forward", "qk_norm_rope_backward_workspace_bytes", "qk_norm_rope_backward",
     "linear_attention_workspace_bytes", "linear_attention_forward", "linear_attention_backward_workspace_bytes", "linear_attention_backward",
     "linear_attention_step",
+    "kv_cache_append", "kv_cache_read", "paged_attention_workspace_bytes", "paged_attention_forward",
+    "token_logprobs_workspace_bytes", "token_logprobs_forward", "token_logprobs_backward",
     "swiglu_forward", "swiglu_backward", "embed_forward", "embed_backward_workspace_bytes", "embed_backward",
     "grad_sq_norm_workspace_bytes", "grad_sq_norm", "adamw_step", "issue_rate_probe", "gemm_route", "attention_backward_pieces",
     "linear_attention_plan",
@@ -30,6 +32,8 @@ DLAYER_ACCUMULATE_WGRADS = 1
 DLAYER_REUSE_TRANSPOSED_WEIGHTS = 2
 DLAYER_RECOMPUTE_NORMS = 1
 DLAYER_RECOMPUTE_SWIGLU = 2
+DLAYER_CACHE_BF16 = 0
+DLAYER_CACHE_E4M3 = 1
 
 
 class DLayerError(RuntimeError):
@@ -51,6 +55,33 @@ class LayerCfg(C.Structure):
         return cls(*(getattr(cfg, n, 0) for n, _ in cls._fields_))
 
 
+class KVCache(C.Structure):
+    """Mirror of `dlayer_kv_cache`; keeps the tensors that it points to."""
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("page_table", C.c_void_p),
+                ("n_pages", C.c_int32), ("n_kv_heads", C.c_int32), ("page_size", C.c_int32), ("head_dim", C.c_int32),
+                ("batch", C.c_int32), ("max_pages", C.c_int32), ("dtype", C.c_int32)]
+
+    @classmethod
+    def of(cls, k, v, page_table, k_scale=None, v_scale=None) -> "KVCache":
+        """k, v: [n_pages, n_kv_heads, page_size, head_dim], bfloat16, or float8_e4m3fn or uint8 with k_scale, v_scale [n_pages,
+        n_kv_heads, page_size] uint8; page_table: [batch, max_pages] int32."""
+        if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype:
+            raise DLayerError("KVCache: k and v are [n_pages, n_kv_heads, page_size, head_dim], of one shape and type")
+        if page_table.dim() != 2 or str(page_table.dtype) != "torch.int32":
+            raise DLayerError("KVCache: page_table is [batch, max_pages] int32")
+        kind = str(k.dtype)
+        if kind not in ("torch.bfloat16", "torch.float8_e4m3fn", "torch.uint8"):
+            raise DLayerError(f"KVCache: k and v are bfloat16, float8_e4m3fn or uint8 (the bytes of e4m3), not {kind}")
+        e4m3 = kind != "torch.bfloat16"
+        scales = [t for t in (k_scale, v_scale) if t is not None]
+        if len(scales) != (2 if e4m3 else 0) or any(t.shape != k.shape[:3] or str(t.dtype) != "torch.uint8" for t in scales):
+            raise DLayerError("KVCache: e4m3 comes with k_scale and v_scale, [n_pages, n_kv_heads, page_size] uint8; bfloat16 without")
+        c = cls(_p(k), _p(v), _p(k_scale), _p(v_scale), _p(page_table), *k.shape, *page_table.shape,
+                DLAYER_CACHE_E4M3 if e4m3 else DLAYER_CACHE_BF16)
+        c.tensors = (k, v, k_scale, v_scale, page_table)
+        return c
+
+
 class _Ptrs(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in WEIGHT_FIELDS]
 
@@ -64,6 +95,7 @@ def _load():
     vp, i64, sz, i32, f32 = C.c_void_p, C.c_int64, C.c_size_t, C.c_int32, C.c_float
     cfgp = C.POINTER(LayerCfg)
     ptrs = C.POINTER(_Ptrs)
+    cachep = C.POINTER(KVCache)
     sig = {
         "dlayer_version": (C.c_int, []),
         "dlayer_last_error": (C.c_char_p, []),
@@ -100,6 +132,13 @@ def _load():
         "linear_attention_backward_workspace_bytes": (sz, [i64, i64, i64, i64, i64]),
         "linear_attention_backward": (C.c_int, [vp, vp, vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, i64, f32, vp, vp, vp, vp, vp, vp]),
         "linear_attention_step": (C.c_int, [vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, f32, vp, vp]),
+        "kv_cache_append": (C.c_int, [cachep, vp, vp, vp, vp, vp, i64, i64, f32, i32, vp, vp]),
+        "kv_cache_read": (C.c_int, [cachep, vp, vp, i64, vp, vp, vp]),
+        "paged_attention_workspace_bytes": (sz, [cachep, i64, i64]),
+        "paged_attention_forward": (C.c_int, [cachep, vp, vp, vp, i64, i64, f32, vp, vp, vp, vp]),
+        "token_logprobs_workspace_bytes": (sz, [i64, i64, i64]),
+        "token_logprobs_forward": (C.c_int, [vp, vp, i64, i64, i64, f32, i64, vp, vp, vp, vp, vp, vp, vp]),
+        "token_logprobs_backward": (C.c_int, [vp, vp, vp, vp, vp, vp, i64, i64, i64, f32, vp, vp]),
         "swiglu_forward": (C.c_int, [vp, vp, i64, vp, vp]),
         "swiglu_backward": (C.c_int, [vp, vp, vp, i64, vp, vp, vp]),
         "embed_forward": (C.c_int, [vp, vp, i64, i64, i64, vp, vp]),
@@ -338,6 +377,39 @@ def linear_attention_backward(q, k, v, log_decay, lengths, state_in, d_o, d_stat
 def linear_attention_step(q, k, v, log_decay, lengths, state, batch, n_q_heads, n_kv_heads, head_dim, scale, o, stream=None):
     _check(lib.linear_attention_step(_p(q), _p(k), _p(v), _p(log_decay), _p(lengths), _p(state), batch, n_q_heads, n_kv_heads, head_dim,
                                      scale, _p(o), _stream(stream)), "linear_attention_step")
+
+
+def kv_cache_append(cache, q, k, v, start, lengths, seq, n_q_heads, rope_base, rope_layout, q_out, stream=None):
+    _check(lib.kv_cache_append(C.byref(cache), _p(q), _p(k), _p(v), _p(start), _p(lengths), seq, n_q_heads, rope_base, rope_layout, _p(q_out),
+                               _stream(stream)), "kv_cache_append")
+
+
+def kv_cache_read(cache, start, lengths, seq, k, v, stream=None):
+    _check(lib.kv_cache_read(C.byref(cache), _p(start), _p(lengths), seq, _p(k), _p(v), _stream(stream)), "kv_cache_read")
+
+
+def paged_attention_workspace_bytes(cache, seq, n_q_heads) -> int:
+    return lib.paged_attention_workspace_bytes(C.byref(cache), seq, n_q_heads)
+
+
+def paged_attention_forward(cache, q, start, lengths, seq, n_q_heads, scale, o, lse, workspace, stream=None):
+    _check(lib.paged_attention_forward(C.byref(cache), _p(q), _p(start), _p(lengths), seq, n_q_heads, scale, _p(o), _p(lse), _p(workspace),
+                                       _stream(stream)), "paged_attention_forward")
+
+
+def token_logprobs_workspace_bytes(T, V, n_top=0) -> int:
+    return lib.token_logprobs_workspace_bytes(T, V, n_top)
+
+
+def token_logprobs_forward(logits, targets, T, V, ld, inverse_temperature, n_top, logprobs, entropy, lse, top_ids, top_logprobs, workspace,
+                           stream=None):
+    _check(lib.token_logprobs_forward(_p(logits), _p(targets), T, V, ld, inverse_temperature, n_top, _p(logprobs), _p(entropy), _p(lse),
+                                      _p(top_ids), _p(top_logprobs), _p(workspace), _stream(stream)), "token_logprobs_forward")
+
+
+def token_logprobs_backward(logits, targets, lse, entropy, d_logprobs, d_entropy, T, V, ld, inverse_temperature, dlogits, stream=None):
+    _check(lib.token_logprobs_backward(_p(logits), _p(targets), _p(lse), _p(entropy), _p(d_logprobs), _p(d_entropy), T, V, ld,
+                                       inverse_temperature, _p(dlogits), _stream(stream)), "token_logprobs_backward")
 
 
 def swiglu_forward(g, u, n, a, stream=None):

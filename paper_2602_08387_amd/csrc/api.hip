@@ -1,5 +1,6 @@
 // C-ABI entry points declared in include/dlayer.h: argument validation, buffer carving and the
 // order of kernel launches.  No arithmetic of the layer lives here.
+#include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
 #include <string.h>
@@ -732,6 +733,129 @@ int linear_attention_step(const void* q, const void* k, const void* v, const flo
   TRY(check_device());
   return launch_linear_attention_step(LinearCall{q, k, v, log_decay, lengths, batch, 1, n_q_heads, n_kv_heads, head_dim, scale}, state, o,
                                       (hipStream_t)stream);
+}
+
+// The cache's sizes; and, where its memory is used, its pointers.
+static int cache_ok(const char* who, const dlayer_kv_cache* c, int64_t seq, bool memory) {
+  REQUIRE(c != nullptr, "%s: cache is null", who);
+  REQUIRE(c->n_pages > 0 && c->n_kv_heads > 0 && c->batch > 0 && c->max_pages > 0 && seq > 0, "%s: non-positive dimension", who);
+  REQUIRE(c->head_dim == 32 || c->head_dim == 64 || c->head_dim == 128, "%s: head_dim must be 32, 64 or 128", who);
+  REQUIRE(c->page_size >= 16 && c->page_size <= 4096 && (c->page_size & (c->page_size - 1)) == 0,
+          "%s: page_size must be a power of two from 16 to 4096", who);
+  REQUIRE(c->dtype == DLAYER_CACHE_BF16 || c->dtype == DLAYER_CACHE_E4M3, "%s: unknown cache dtype", who);
+  REQUIRE(c->n_kv_heads < 65536 && seq < ((int64_t)1 << 31) && (int64_t)c->batch * seq < ((int64_t)1 << 40), "%s: batch, seq or head count too large", who);
+  REQUIRE((int64_t)c->max_pages * c->page_size < (int64_t)1 << 31, "%s: a row's pages hold 2^31 tokens or more", who);
+  if (!memory) return 0;
+  REQUIRE(c->k && c->v && aligned16(c->k) && aligned16(c->v), "%s: the cache's k or v is null or not 16-byte aligned", who);
+  REQUIRE(c->page_table != nullptr, "%s: page_table is null", who);
+  if (c->dtype == DLAYER_CACHE_E4M3)
+    REQUIRE(c->k_scale && c->v_scale && aligned16(c->k_scale) && aligned16(c->v_scale), "%s: an e4m3 cache needs k_scale and v_scale, 16-byte aligned", who);
+  else
+    REQUIRE(!c->k_scale && !c->v_scale, "%s: a bf16 cache has no k_scale and v_scale", who);
+  return 0;
+}
+static CacheCall cache_call(const dlayer_kv_cache* c, const int64_t* start, const int64_t* lengths) {
+  return CacheCall{c->k, c->v, c->k_scale, c->v_scale, c->page_table, c->n_pages, c->n_kv_heads, c->page_size, c->head_dim, c->batch, c->max_pages,
+                   c->dtype == DLAYER_CACHE_E4M3, start, lengths};
+}
+static bool over_cache(const dlayer_kv_cache* c, const void* p, uint64_t bytes) {
+  const uint64_t vectors = (uint64_t)c->n_pages * c->n_kv_heads * c->page_size, held = vectors * c->head_dim * (c->dtype == DLAYER_CACHE_E4M3 ? 1 : 2);
+  return overlap(p, bytes, c->k, held) || overlap(p, bytes, c->v, held) || overlap(p, bytes, c->k_scale, vectors) || overlap(p, bytes, c->v_scale, vectors) ||
+         overlap(p, bytes, c->page_table, (uint64_t)c->batch * c->max_pages * sizeof(int32_t));
+}
+
+int kv_cache_append(const dlayer_kv_cache* cache, const void* q, const void* k, const void* v, const int64_t* start, const int64_t* lengths, int64_t seq,
+                    int64_t n_q_heads, float rope_base, int32_t rope_layout, void* q_out, void* stream) {
+  TRY(cache_ok("kv_cache_append", cache, seq, true));
+  REQUIRE_PTR(k); REQUIRE_PTR(v);
+  REQUIRE((q == nullptr) == (q_out == nullptr), "kv_cache_append: q and q_out go together");
+  REQUIRE(rope_base >= 0.f && rope_base < INFINITY, "kv_cache_append: rope_base must be positive, or 0 for no rotation");
+  REQUIRE(rope_layout == 0 || rope_layout == 1, "kv_cache_append: rope_layout must be 0 or 1");
+  const uint64_t of_kv = heads_bytes(cache->batch, seq, cache->n_kv_heads, cache->head_dim);
+  REQUIRE(!over_cache(cache, k, of_kv) && !over_cache(cache, v, of_kv), "kv_cache_append: k and v must not overlap the cache");
+  if (q) {
+    REQUIRE(rope_base > 0.f, "kv_cache_append: q is given to be rotated, but rope_base is 0");
+    REQUIRE(n_q_heads > 0 && n_q_heads < 65536, "kv_cache_append: n_q_heads must be positive and below 65536");
+    REQUIRE_PTR(q); REQUIRE_PTR(q_out);
+    const uint64_t of_q = heads_bytes(cache->batch, seq, n_q_heads, cache->head_dim);
+    REQUIRE(!shifted(q_out, q, of_q), "kv_cache_append: q_out must be q or not overlap it");
+    REQUIRE(!overlap(q_out, of_q, k, of_kv) && !overlap(q_out, of_q, v, of_kv) && !over_cache(cache, q_out, of_q) && !over_cache(cache, q, of_q),
+            "kv_cache_append: q and q_out must not overlap the cache, nor q_out k or v");
+  }
+  TRY(check_device());
+  return launch_kv_cache_append(cache_call(cache, start, lengths), q, k, v, seq, n_q_heads, rope_base, rope_layout, q_out, (hipStream_t)stream);
+}
+
+int kv_cache_read(const dlayer_kv_cache* cache, const int64_t* start, const int64_t* lengths, int64_t seq, void* k, void* v, void* stream) {
+  TRY(cache_ok("kv_cache_read", cache, seq, true));
+  REQUIRE_PTR(k); REQUIRE_PTR(v);
+  const uint64_t of_kv = heads_bytes(cache->batch, seq, cache->n_kv_heads, cache->head_dim);
+  REQUIRE(!over_cache(cache, k, of_kv) && !over_cache(cache, v, of_kv) && !overlap(k, of_kv, v, of_kv), "kv_cache_read: k and v must not overlap the cache or each other");
+  TRY(check_device());
+  return launch_kv_cache_read(cache_call(cache, start, lengths), seq, k, v, (hipStream_t)stream);
+}
+
+static int paged_shape_ok(const char* who, const dlayer_kv_cache* c, int64_t seq, int64_t Hq, bool memory) {
+  TRY(cache_ok(who, c, seq, memory));
+  REQUIRE(Hq > 0 && Hq < 65536 && Hq % c->n_kv_heads == 0, "%s: n_q_heads must be a multiple of the cache's n_kv_heads, and below 65536", who);
+  const int64_t rows = seq * (Hq / c->n_kv_heads);
+  REQUIRE(seq * Hq < ((int64_t)1 << 31) - 256 && (int64_t)c->batch * c->n_kv_heads * ((rows + 15) / 16) < (int64_t)1 << 31, "%s: batch, seq or head count too large", who);
+  return 0;
+}
+
+size_t paged_attention_workspace_bytes(const dlayer_kv_cache* cache, int64_t seq, int64_t n_q_heads) {
+  if (paged_shape_ok("paged_attention_workspace_bytes", cache, seq, n_q_heads, false)) return 0;
+  return paged_attention_workspace(cache->batch, seq, n_q_heads, cache->n_kv_heads, cache->head_dim, (int64_t)cache->max_pages * cache->page_size);
+}
+
+int paged_attention_forward(const dlayer_kv_cache* cache, const void* q, const int64_t* start, const int64_t* lengths, int64_t seq, int64_t n_q_heads,
+                            float scale, void* o, float* lse, void* workspace, void* stream) {
+  TRY(paged_shape_ok("paged_attention_forward", cache, seq, n_q_heads, true));
+  REQUIRE_PTR(q); REQUIRE_PTR(o); REQUIRE_PTR(workspace);
+  REQUIRE(scale > 0.f && scale < INFINITY, "paged_attention_forward: scale must be positive and finite");
+  const uint64_t of_q = heads_bytes(cache->batch, seq, n_q_heads, cache->head_dim);
+  REQUIRE(!overlap(o, of_q, q, of_q) && !over_cache(cache, o, of_q), "paged_attention_forward: o must not overlap q or the cache");
+  TRY(check_device());
+  return launch_paged_attention(cache_call(cache, start, lengths), q, seq, n_q_heads, scale, o, lse, workspace, (hipStream_t)stream);
+}
+
+static int logprobs_ok(const char* who, int64_t T, int64_t V, int64_t ld) {
+  REQUIRE(T > 0 && T < (int64_t)1 << 22 && V > 0 && V <= ld && ld < (int64_t)1 << 24 && ld % 8 == 0,
+          "%s: need 0 < T < 2^22, 0 < V <= ld < 2^24, ld a multiple of 8", who);
+  return 0;
+}
+
+size_t token_logprobs_workspace_bytes(int64_t T, int64_t V, int64_t n_top) {
+  if (logprobs_ok("token_logprobs_workspace_bytes", T, V, (V + 7) & ~(int64_t)7) || n_top < 0 || n_top > 64 || n_top > V) return 0;
+  return token_logprobs_workspace(T, V, n_top);
+}
+
+int token_logprobs_forward(const void* logits, const int64_t* targets, int64_t T, int64_t V, int64_t ld, float inverse_temperature, int64_t n_top,
+                           float* logprobs, float* entropy, float* lse, int64_t* top_ids, float* top_logprobs, void* workspace, void* stream) {
+  TRY(logprobs_ok("token_logprobs_forward", T, V, ld));
+  REQUIRE_PTR(logits); REQUIRE_PTR(workspace);
+  REQUIRE(inverse_temperature > 0.f && inverse_temperature < INFINITY, "token_logprobs_forward: inverse_temperature must be positive and finite");
+  REQUIRE(n_top >= 0 && n_top <= 64 && n_top <= V, "token_logprobs_forward: n_top must be 0 .. 64 and at most V");
+  REQUIRE(targets || !logprobs, "token_logprobs_forward: logprobs is of targets, which is null");
+  REQUIRE(n_top || (!top_ids && !top_logprobs), "token_logprobs_forward: top_ids and top_logprobs are null where n_top is 0");
+  TRY(check_device());
+  return launch_token_logprobs_fwd(LogprobsCall{logits, targets, T, V, ld, inverse_temperature}, (int)n_top, logprobs, entropy, lse, top_ids, top_logprobs,
+                                   workspace, (hipStream_t)stream);
+}
+
+int token_logprobs_backward(const void* logits, const int64_t* targets, const float* lse, const float* entropy, const float* d_logprobs,
+                            const float* d_entropy, int64_t T, int64_t V, int64_t ld, float inverse_temperature, void* dlogits, void* stream) {
+  TRY(logprobs_ok("token_logprobs_backward", T, V, ld));
+  REQUIRE_PTR(logits); REQUIRE_PTR(dlogits);
+  REQUIRE(inverse_temperature > 0.f && inverse_temperature < INFINITY, "token_logprobs_backward: inverse_temperature must be positive and finite");
+  REQUIRE(lse != nullptr, "token_logprobs_backward: lse is null");
+  REQUIRE(d_logprobs || d_entropy, "token_logprobs_backward: neither d_logprobs nor d_entropy is given");
+  REQUIRE(targets || !d_logprobs, "token_logprobs_backward: d_logprobs is of targets, which is null");
+  REQUIRE(entropy || !d_entropy, "token_logprobs_backward: d_entropy needs the forward's entropy");
+  REQUIRE(!shifted(dlogits, logits, (uint64_t)T * ld * 2), "token_logprobs_backward: dlogits must be logits or not overlap it");
+  TRY(check_device());
+  return launch_token_logprobs_bwd(LogprobsCall{logits, targets, T, V, ld, inverse_temperature}, lse, entropy, d_logprobs, d_entropy, dlogits,
+                                   (hipStream_t)stream);
 }
 
 static int opt_args_ok(const char* who, int32_t n, const int64_t* numel) {

@@ -164,6 +164,36 @@ int launch_linear_attention_step(const LinearCall& c, float* state, void* o, hip
 // see linear_attention_plan in dlayer.h
 void query_linear_attention_plan(bool backward, int64_t B, int64_t S, int64_t Hq, int64_t Hkv, int64_t dh, int32_t* plan);
 
+// ---- kv_cache.hip, paged_attention.hip
+// a paged cache (see dlayer_kv_cache in dlayer.h) and the rows of a call: start, lengths (device, [batch]) may be null
+struct CacheCall {
+  void *k, *v, *k_scale, *v_scale;
+  const int32_t* table;
+  int64_t n_pages, heads, page_size, dh, batch, columns;
+  bool e4m3;
+  const int64_t *start, *lengths;
+};
+int launch_kv_cache_append(const CacheCall& c, const void* q, const void* k, const void* v, int64_t seq, int64_t Hq, float base, int layout,
+                           void* q_out, hipStream_t st);
+int launch_kv_cache_read(const CacheCall& c, int64_t seq, void* k, void* v, hipStream_t st);
+size_t paged_attention_workspace(int64_t batch, int64_t seq, int64_t Hq, int64_t Hkv, int64_t dh, int64_t max_tokens);
+int launch_paged_attention(const CacheCall& c, const void* q, int64_t seq, int64_t Hq, float scale, void* o, float* lse, void* workspace,
+                           hipStream_t st);
+
+// ---- logprobs.hip
+// logits [T][ld] bf16, of which V columns are the vocabulary; targets null: every row counts
+struct LogprobsCall {
+  const void* logits;
+  const int64_t* targets;
+  int64_t T, V, ld;
+  float inverse_temperature;
+};
+size_t token_logprobs_workspace(int64_t T, int64_t V, int64_t n_top);
+int launch_token_logprobs_fwd(const LogprobsCall& c, int n_top, float* logprobs, float* entropy, float* lse, int64_t* top_ids, float* top_logprobs,
+                              void* workspace, hipStream_t st);
+int launch_token_logprobs_bwd(const LogprobsCall& c, const float* lse, const float* entropy, const float* d_logprobs, const float* d_entropy,
+                              void* dlogits, hipStream_t st);
+
 // ---- ce.hip
 size_t ce_workspace(int64_t T, int64_t V);
 int launch_ce(const void* logits, const int64_t* targets, int64_t T, int64_t V, float grad_scale,

@@ -1,0 +1,399 @@
+// Log-probabilities of given tokens under rows of bf16 logits, with each row's entropy and its likeliest tokens; and the gradient.
+//
+//   z = x / temperature, M = max z, S = sum exp(z - M), U = sum exp(z - M) (z - M):
+//   lse = M + ln S;  logp(v) = (z_v - M) - ln S;  entropy = ln S - U / S                          (no difference of large numbers)
+//   dx_v = ([v = target] dlp - p_v (dlp + dH (logp_v + entropy))) / temperature
+//
+// Forward: one pass, bound by the reading of the logits (2 bytes each; some 10 vector instructions an element, of which the exponential takes four).
+// A thread keeps S and U relative to its own running maximum, which it raises once in 32 elements.  Exponents are formed as (x - max) times a
+// constant: of a row that is all but certain S is then 1 and a little, exactly, where one FMA against the rounded product max * constant would be
+// off by that rounding (and infinite for a row masked with the type's lowest value).
+//
+// The likeliest tokens: a wave keeps a list of 64 sorted over its lanes.  An element has to pass the list's n-th; those that do (some n ln(row / first
+// elements)) go to a buffer in LDS and are sorted into the list 64 at a time.  The first threshold is the n-th largest of the lanes' own maxima
+// over their first 32 elements.  An order without ties: a 64-bit key of the logit's bits as a whole number of the same order, then the lower index.
+//
+// Few rows are cut into parts, joined by a second kernel.
+#include "common.h"
+#include "kernels.h"
+
+namespace dl {
+
+constexpr int kLpThreads = 256, kLpWaves = kLpThreads / 64, kLpUnroll = 4;
+constexpr int kLpBuffer = 64 + 512;      // candidates of a wave: those left from before, and a whole vector from every lane
+constexpr float kLpLn2 = 0.6931471805599453f;
+
+struct LogprobsArgs {
+  const bf16_t* logits;
+  const int64_t* targets;                // null: every row counts
+  int64_t ld;
+  int V, parts, per_part, n_top;         // per_part: vectors of 8
+  float inverse, inverse_log2e;
+  float *logprobs, *entropy, *lse, *top_logprobs;   // each may be null
+  int64_t* top_ids;
+  float* part_sums;                      // [row][part][4]: maximum (of x), S, U (in log2 units)
+  uint64_t* part_top;                    // [row][part][n_top]
+};
+
+__device__ __forceinline__ bool row_counts(const LogprobsArgs& a, int64_t row) {
+  if (!a.targets) return true;
+  const int64_t t = a.targets[row];
+  return t >= 0 && t < a.V;
+}
+
+// Keys: larger for a larger logit, for equal ones for the lower index; 0 is below every key.  -0 and 0 are equal.
+__device__ __forceinline__ uint64_t key_of(uint32_t bits, int index) {
+  const int s = (int)(int16_t)bits, order = s >= 0 ? s : -32768 - s;
+  return (uint64_t)(uint32_t)(order + 65536) << 32 | (0xffffffffu - (uint32_t)index);
+}
+__device__ __forceinline__ int key_index(uint64_t key) { return (int)(0xffffffffu - (uint32_t)key); }
+__device__ __forceinline__ float key_logit(uint64_t key) {
+  const int order = (int)(key >> 32) - 65536;
+  return __uint_as_float((uint32_t)(uint16_t)(order >= 0 ? order : -32768 - order) << 16);
+}
+__device__ __forceinline__ uint64_t max64(uint64_t a, uint64_t b) { return a > b ? a : b; }
+__device__ __forceinline__ uint64_t min64(uint64_t a, uint64_t b) { return a > b ? b : a; }
+
+// The last steps of a bitonic sort: a bitonic sequence over the 64 lanes into descending order.
+__device__ __forceinline__ uint64_t merge_descending(uint64_t k, int lane) {
+#pragma unroll
+  for (int j = 32; j > 0; j >>= 1) {
+    const uint64_t o = __shfl_xor(k, j, 64);
+    k = (lane & j) ? min64(k, o) : max64(k, o);
+  }
+  return k;
+}
+// 64 lanes into descending order: keys, or floats that are not NaN.
+template <typename T>
+__device__ __forceinline__ T sort_descending(T k, int lane) {
+#pragma unroll
+  for (int n = 2; n <= 64; n <<= 1)
+#pragma unroll
+    for (int j = n >> 1; j > 0; j >>= 1) {
+      const T o = __shfl_xor(k, j, 64);
+      const bool low = ((lane & j) != 0) != ((lane & n) != 0);     // a run in which n is set ascends
+      k = (o > k) == low ? k : o;
+    }
+  return k;
+}
+// The 64 largest of two descending sequences, descending.
+__device__ __forceinline__ uint64_t join_descending(uint64_t a, uint64_t b, int lane) {
+  return merge_descending(max64(a, __shfl(b, 63 - lane, 64)), lane);
+}
+
+struct Sums { float m, s, u; };          // maximum of x, S and U relative to it; m = -inf: nothing but -inf so far
+
+// Sums relative to another maximum.
+__device__ __forceinline__ Sums relative_to(const Sums& v, float top, float inverse_log2e) {
+  if (v.m == -INFINITY) return {top, v.s, v.u};        // zeros, or NaN
+  const float d = fmaxf((v.m - top) * inverse_log2e, -1e4f);
+  const float f = __builtin_amdgcn_exp2f(d);
+  return {top, f * v.s, f * (v.u + d * v.s)};
+}
+
+// A row's results from its sums; list: its likeliest, one a lane of the calling wave.
+__device__ __forceinline__ void finish_row(const LogprobsArgs& a, int64_t row, const Sums& v, uint64_t list, int lane) {
+  const bool empty = v.m == -INFINITY && v.s == 0.f;    // nothing but -inf
+  const float log_s = empty ? 0.f : logf(v.s);
+  const auto logp = [&](float x) { return x == -INFINITY ? (v.s == v.s ? -INFINITY : v.s) : (x - v.m) * a.inverse - log_s; };
+  if (lane == 0) {
+    if (a.logprobs) a.logprobs[row] = logp((float)a.logits[row * a.ld + a.targets[row]]);
+    if (a.entropy) a.entropy[row] = empty ? 0.f : log_s - kLpLn2 * (v.u / v.s);
+    if (a.lse) a.lse[row] = empty ? -INFINITY : v.m * a.inverse + log_s;
+  }
+  if (lane < a.n_top) {
+    if (a.top_ids) a.top_ids[row * a.n_top + lane] = list ? key_index(list) : -1;
+    if (a.top_logprobs) a.top_logprobs[row * a.n_top + lane] = list ? logp(key_logit(list)) : NAN;
+  }
+}
+__device__ __forceinline__ void finish_uncounted(const LogprobsArgs& a, int64_t row) {
+  if (threadIdx.x == 0) {
+    if (a.logprobs) a.logprobs[row] = 0.f;
+    if (a.entropy) a.entropy[row] = 0.f;
+    if (a.lse) a.lse[row] = 0.f;
+  }
+  if ((int)threadIdx.x < a.n_top) {
+    if (a.top_ids) a.top_ids[row * a.n_top + threadIdx.x] = -1;
+    if (a.top_logprobs) a.top_logprobs[row * a.n_top + threadIdx.x] = 0.f;
+  }
+}
+
+// A wave's list of the likeliest, with the buffer in front of it.
+struct TopList {
+  uint64_t list;                         // descending over the lanes
+  uint64_t* buffer;
+  int held;                              // in the buffer
+  float threshold;                       // of x: what is not above it cannot enter (once the list is full)
+  bool full;
+
+  __device__ __forceinline__ void drain(int lane, int n_top) {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    for (int i = 0; i < held; i += 64) list = join_descending(list, sort_descending(i + lane < held ? buffer[i + lane] : 0, lane), lane);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    held = 0;
+    const uint64_t last = __shfl(list, n_top - 1, 64);
+    full = last != 0;
+    threshold = full ? key_logit(last) : -INFINITY;
+  }
+  __device__ __forceinline__ bool passes(float x) const { return full ? x > threshold : x >= threshold; }
+  __device__ __forceinline__ void push(bool take, uint32_t bits, int index, int lane) {
+    const uint64_t who = __builtin_amdgcn_ballot_w64(take);
+    if (who == 0) return;
+    if (take) buffer[held + __popcll(who & ((1ull << lane) - 1))] = key_of(bits, index);
+    held += __popcll(who);
+  }
+};
+
+template <bool TOP>
+__global__ __launch_bounds__(kLpThreads) void logprobs_kernel(const LogprobsArgs a) {
+  __shared__ float red[kLpWaves][4];
+  __shared__ uint64_t lists[TOP ? kLpWaves : 1][64];
+  __shared__ uint64_t buffer[TOP ? kLpWaves : 1][TOP ? kLpBuffer : 1];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t row = blockIdx.x / a.parts;
+  const int part = (int)(blockIdx.x % a.parts);
+  if (!row_counts(a, row)) {
+    if (a.parts == 1) finish_uncounted(a, row);
+    return;
+  }
+  const u32x4* in = reinterpret_cast<const u32x4*>(a.logits + row * a.ld);
+  const int whole = a.V >> 3, vectors = (a.V + 7) >> 3;          // the last vector may hold columns behind the vocabulary
+  const int first = part * a.per_part, end = min(vectors, first + a.per_part);
+
+  Sums v{-INFINITY, 0.f, 0.f};
+  TopList top{0, buffer[TOP ? wave : 0], 0, -INFINITY, false};
+  bool begun = false;
+
+  for (int c0 = first + wave * 64; c0 < end; c0 += kLpThreads * kLpUnroll) {
+    u32x4 w[kLpUnroll];
+#pragma unroll
+    for (int i = 0; i < kLpUnroll; ++i) {
+      const int c = c0 + i * kLpThreads + lane;
+      w[i] = c < end ? in[c] : u32x4{0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u};      // -inf
+      if (c == whole) {                  // columns behind the vocabulary
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (c * 8 + e >= a.V) w[i][e >> 1] = (e & 1) ? (w[i][e >> 1] & 0xffffu) | 0xff800000u : (w[i][e >> 1] & 0xffff0000u) | 0xff80u;
+      }
+    }
+    float vmax[kLpUnroll], mx = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kLpUnroll; ++i) {
+      float t = -INFINITY;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) t = fmaxf(t, fmaxf(__uint_as_float(w[i][e] << 16), __uint_as_float(w[i][e] & 0xffff0000u)));
+      vmax[i] = t;
+      mx = fmaxf(mx, t);
+    }
+    if (mx > v.m) v = relative_to(v, mx, a.inverse_log2e);
+    const float ref = v.m == -INFINITY ? 0.f : v.m;
+#pragma unroll
+    for (int i = 0; i < kLpUnroll; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float x = __uint_as_float((e & 1) ? w[i][e >> 1] & 0xffff0000u : w[i][e >> 1] << 16);
+        const float t = (x - ref) * a.inverse_log2e, p = __builtin_amdgcn_exp2f(t);
+        v.s += p;
+        v.u = __builtin_fmaf(p, fmaxf(t, -1e4f), v.u);           // t may be -inf where p is 0
+      }
+    if constexpr (TOP) {
+      // Until the list is full its threshold is a bound that may be met: the n-th largest of the lanes' largest of the first batch, then nothing.  From then on
+      // an element equal to the list's n-th comes behind it, since a wave's indices ascend from vector to vector.
+      if (!begun) top.threshold = __shfl(sort_descending(mx, lane), a.n_top - 1, 64);
+      begun = true;
+      if (__builtin_amdgcn_ballot_w64(top.passes(mx))) {
+#pragma unroll
+        for (int i = 0; i < kLpUnroll; ++i) {
+          if (!__builtin_amdgcn_ballot_w64(top.passes(vmax[i]))) continue;
+          const int index = (c0 + i * kLpThreads + lane) * 8, left = c0 + i * kLpThreads + lane < end ? a.V - index : 0;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const uint32_t bits = (w[i][e >> 1] >> ((e & 1) * 16)) & 0xffffu;
+            top.push(e < left && top.passes(__uint_as_float(bits << 16)), bits, index + e, lane);
+          }
+          if (top.held > 64) top.drain(lane, a.n_top);
+        }
+        if (!top.full) top.drain(lane, a.n_top);
+      }
+    }
+  }
+  // the waves' sums and lists, joined by the first wave
+  const float mw = wave_max(v.m);
+  Sums r = relative_to(v, mw, a.inverse_log2e);
+  r.s = wave_sum(r.s);
+  r.u = wave_sum(r.u);
+  if (lane == 0) { red[wave][0] = mw; red[wave][1] = r.s; red[wave][2] = r.u; }
+  if constexpr (TOP) {
+    if (top.held > 0) top.drain(lane, a.n_top);
+    lists[wave][lane] = top.list;
+  }
+  __syncthreads();
+  if (wave != 0) return;
+  float m = red[0][0];
+#pragma unroll
+  for (int i = 1; i < kLpWaves; ++i) m = fmaxf(m, red[i][0]);
+  Sums sum{m, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < kLpWaves; ++i) {
+    const Sums o{red[i][0], red[i][1], red[i][2]}, p = relative_to(o, m, a.inverse_log2e);
+    sum.s += p.s;
+    sum.u += p.u;
+  }
+  uint64_t list = 0;
+  if constexpr (TOP) {
+    list = top.list;
+#pragma unroll
+    for (int i = 1; i < kLpWaves; ++i) list = join_descending(list, lists[i][lane], lane);
+  }
+  if (a.parts == 1) {
+    finish_row(a, row, sum, list, lane);
+  } else {
+    const int64_t at = row * a.parts + part;
+    if (lane == 0) *reinterpret_cast<f32x4*>(a.part_sums + at * 4) = f32x4{sum.m, sum.s, sum.u, 0.f};
+    if (TOP && lane < a.n_top) a.part_top[at * a.n_top + lane] = list;
+  }
+}
+
+// Joins the parts of a row: a workgroup a row, its waves taking turns with the lists.
+template <bool TOP>
+__global__ __launch_bounds__(kLpThreads) void logprobs_join_kernel(const LogprobsArgs a) {
+  __shared__ uint64_t lists[TOP ? kLpWaves : 1][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t row = blockIdx.x;
+  if (!row_counts(a, row)) {
+    finish_uncounted(a, row);
+    return;
+  }
+  uint64_t list = 0;
+  if constexpr (TOP) {
+    for (int i = wave; i < a.parts; i += kLpWaves)
+      list = join_descending(list, lane < a.n_top ? a.part_top[(row * a.parts + i) * a.n_top + lane] : 0, lane);
+    lists[wave][lane] = list;
+    __syncthreads();
+  }
+  if (wave != 0) return;
+  if constexpr (TOP)
+#pragma unroll
+    for (int i = 1; i < kLpWaves; ++i) list = join_descending(list, lists[i][lane], lane);
+  Sums mine{-INFINITY, 0.f, 0.f};
+  float m = -INFINITY;
+  const float* parts = a.part_sums + row * a.parts * 4;
+  for (int i = lane; i < a.parts; i += 64) m = fmaxf(m, parts[i * 4]);
+  m = wave_max(m);
+  for (int i = lane; i < a.parts; i += 64) {
+    const Sums o{parts[i * 4], parts[i * 4 + 1], parts[i * 4 + 2]}, p = relative_to(o, m, a.inverse_log2e);
+    mine.s += p.s;
+    mine.u += p.u;
+  }
+  finish_row(a, row, Sums{m, wave_sum(mine.s), wave_sum(mine.u)}, list, lane);
+}
+
+// Parts of a row: where there are fewer rows than fill the chip, of no fewer than two vectors a thread.
+constexpr int64_t kLpWorkgroups = 1024;
+static int64_t lp_most_parts(int64_t V) { return (V + 16 * kLpThreads - 1) / (16 * kLpThreads); }
+
+// sums and lists of the parts; rows * parts is within kLpWorkgroups wherever there are parts
+static int64_t lp_parts_held(int64_t T, int64_t V) {
+  const int64_t n = T < kLpWorkgroups ? T * lp_most_parts(V) : kLpWorkgroups;
+  return n < kLpWorkgroups ? n : kLpWorkgroups;
+}
+size_t token_logprobs_workspace(int64_t T, int64_t V, int64_t n_top) { return (size_t)lp_parts_held(T, V) * (16 + 8 * (size_t)n_top); }
+
+int launch_token_logprobs_fwd(const LogprobsCall& c, int n_top, float* logprobs, float* entropy, float* lse, int64_t* top_ids, float* top_logprobs,
+                              void* workspace, hipStream_t st) {
+  LogprobsArgs a{};
+  a.logits = (const bf16_t*)c.logits;
+  a.targets = c.targets;
+  a.ld = c.ld;
+  a.V = (int)c.V;
+  a.inverse = c.inverse_temperature;
+  a.inverse_log2e = (float)((double)c.inverse_temperature * 1.4426950408889634);
+  a.logprobs = logprobs; a.entropy = entropy; a.lse = lse;
+  a.top_ids = top_ids; a.top_logprobs = top_logprobs;
+  a.n_top = n_top;
+  const int64_t most = lp_most_parts(c.V), wanted = kLpWorkgroups / c.T, vectors = (c.V + 7) / 8;
+  const int64_t parts = wanted < 1 ? 1 : wanted < most ? wanted : most;
+  a.per_part = (int)((vectors + parts - 1) / parts);
+  a.parts = (int)((vectors + a.per_part - 1) / a.per_part);
+  a.part_sums = (float*)workspace;
+  a.part_top = (uint64_t*)((char*)workspace + 16 * lp_parts_held(c.T, c.V));
+  const dim3 grid((unsigned)(c.T * a.parts)), block(kLpThreads);
+  if (n_top) hipLaunchKernelGGL((logprobs_kernel<true>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((logprobs_kernel<false>), grid, block, 0, st, a);
+  if (int rc = check_launch("token_logprobs_forward")) return rc;
+  if (a.parts == 1) return 0;
+  if (n_top) hipLaunchKernelGGL((logprobs_join_kernel<true>), dim3((unsigned)c.T), block, 0, st, a);
+  else hipLaunchKernelGGL((logprobs_join_kernel<false>), dim3((unsigned)c.T), block, 0, st, a);
+  return check_launch("token_logprobs_forward, joining parts");
+}
+
+struct LogprobsGradArgs {
+  const bf16_t* logits;
+  bf16_t* dlogits;                       // may be logits: a vector is read by the thread that writes it, before it does
+  const int64_t* targets;
+  const float *lse, *entropy, *d_logprobs, *d_entropy;   // the last two: one may be null
+  int64_t ld;
+  int V, blocks;                         // workgroups of a row
+  float inverse;
+};
+constexpr float kLpNothing = -1e30f;     // the lse of a row of which a mask (-infinity, or the type's lowest value) has left nothing
+
+__global__ __launch_bounds__(kLpThreads) void logprobs_grad_kernel(const LogprobsGradArgs a) {
+  const int64_t row = blockIdx.x / a.blocks;
+  const int c0 = (int)(blockIdx.x % a.blocks) * (kLpThreads * kLpUnroll) + threadIdx.x;
+  const int64_t tgt = a.targets ? a.targets[row] : 0;
+  const float lse = a.lse[row];
+  const bool counts = tgt >= 0 && tgt < a.V && !(lse <= kLpNothing);
+  const float dlp = a.d_logprobs ? a.d_logprobs[row] : 0.f, dh = a.d_entropy ? a.d_entropy[row] : 0.f;
+  // dx = p (A + B t), t = log p, and for the target dlp / temperature more
+  const float A = -(dlp + (a.d_entropy ? dh * a.entropy[row] : 0.f)) * a.inverse, B = -dh * a.inverse;
+  const u32x4* in = reinterpret_cast<const u32x4*>(a.logits + row * a.ld);
+  u32x4* out = reinterpret_cast<u32x4*>(a.dlogits + row * a.ld);
+  const int vectors = (int)(a.ld >> 3);
+  u32x4 w[kLpUnroll];
+#pragma unroll
+  for (int i = 0; i < kLpUnroll; ++i) {
+    const int c = c0 + i * kLpThreads;
+    if (counts && c < vectors && c * 8 < a.V) w[i] = in[c];
+  }
+#pragma unroll
+  for (int i = 0; i < kLpUnroll; ++i) {
+    const int c = c0 + i * kLpThreads;
+    if (c >= vectors) continue;
+    bf16x8 y = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (counts && c * 8 < a.V) {
+      float d[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float x = __uint_as_float((e & 1) ? w[i][e >> 1] & 0xffff0000u : w[i][e >> 1] << 16);
+        const float t = __builtin_fmaf(x, a.inverse, -lse), p = __builtin_amdgcn_exp2f(t * kLog2e);
+        d[e] = p * __builtin_fmaf(B, fmaxf(t, -1e4f), A);
+      }
+      if (a.d_logprobs && c == (int)(tgt >> 3))
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d[e] += e == (int)(tgt & 7) ? dlp * a.inverse : 0.f;
+      if (c * 8 + 8 > a.V)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d[e] = c * 8 + e < a.V ? d[e] : 0.f;
+      y = pack8(d);
+    }
+    out[c] = __builtin_bit_cast(u32x4, y);
+  }
+}
+
+int launch_token_logprobs_bwd(const LogprobsCall& c, const float* lse, const float* entropy, const float* d_logprobs, const float* d_entropy,
+                              void* dlogits, hipStream_t st) {
+  LogprobsGradArgs a{};
+  a.logits = (const bf16_t*)c.logits;
+  a.dlogits = (bf16_t*)dlogits;
+  a.targets = c.targets;
+  a.lse = lse; a.entropy = entropy; a.d_logprobs = d_logprobs; a.d_entropy = d_entropy;
+  a.ld = c.ld;
+  a.V = (int)c.V;
+  a.inverse = c.inverse_temperature;
+  a.blocks = (int)((c.ld / 8 + kLpThreads * kLpUnroll - 1) / (kLpThreads * kLpUnroll));
+  hipLaunchKernelGGL(logprobs_grad_kernel, dim3((unsigned)(c.T * a.blocks)), dim3(kLpThreads), 0, st, a);
+  return check_launch("token_logprobs_backward");
+}
+
+}  // namespace dl
