@@ -7,8 +7,8 @@
 //
 // tile_kernel: workgroup = 128 rows of one (batch row, KV head), four waves of 32; score tiles S^T[key][row] = K Q^T on v_mfma_f32_32x32x16_bf16, whose
 // layout is that of the next product's operand, O^T[d][row] += V^T P^T.  Tiles of 64 keys stream to LDS, double buffered; a wave loads the 16 keys of
-// its own part of the tile, which lie in one page (a page has 16 tokens or a multiple), so a tile needs one page number a wave.  bf16 pages go to LDS
-// directly; e4m3 comes through registers, where it becomes the bf16 values that it stands for.  The keys can be split over workgroups, whose sums
+// its own part of the tile, which lie in one page (a page has 16 tokens or a multiple), so a tile needs one page number a wave.  Loads go to LDS
+// directly; a wave then writes its 16 keys of e4m3, in their place, as the bf16 values that they stand for.  The keys can be split over workgroups, whose sums
 // combine_kernel joins.
 //
 // Rows behind a tile's last key and pages that do not exist are behind the end of the buffer that a load is given, and read as zeros: what a page
@@ -30,7 +30,7 @@ struct AttendArgs {
   bf16_t* o;
   float* lse;                          // [batch][Hq][seq] or null
   float *sums, *stats;                 // parts of a split: [pair][tile][split][rows][DH], and maximum and sum of a row [..][rows][2]
-  int seq, Hq, group, tiles, splits;
+  int seq, Hq, group, tiles, splits, least;   // least: tiles of keys in a part
   float scale_log2;
 };
 
@@ -49,6 +49,52 @@ __device__ __forceinline__ int page_of_wave(const PagedCache& c, int b, int p) {
   return (uint32_t)page < (uint32_t)c.n_pages ? page : -1;
 }
 
+// Workgroup -> (place in its pair's queue, pair of batch row and KV head).  Ids go to the eight XCDs in turn, each with an L2 of its own: a pair's workgroups,
+// which share its keys, stay on one XCD where the pairs are a multiple of 8, and the pairs of a batch row, which may be much longer than another,
+// are spread over all (5 rows of 0 to 1037 tokens and 8 heads in contiguous shares: 3.8 times as long).
+__device__ __forceinline__ void work_of(int id, int pairs, int& j, int& pair) {
+  if (pairs & 7) {
+    j = id / pairs;
+    pair = id % pairs;
+  } else {
+    const int per_xcd = pairs >> 3, slot = id >> 3;
+    j = slot / per_xcd;
+    pair = (slot % per_xcd) * 8 + (id & 7);
+  }
+}
+
+// Memory to LDS without registers between, 16 bytes a lane: lane l's go to `to` + 16 l.  As assembly, which names no register as an output: behind the builtin the
+// compiler waits for all such loads in front of every transposing read, of which it does not know that it stays clear of the stage being
+// filled.  The kernels wait for them themselves (wait_loads), so nothing counts on the compiler here.
+typedef int32_t i32x2 __attribute__((ext_vector_type(2)));
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ i32x4 descriptor(const void* p, uint32_t bytes) {
+  const uint64_t at = (uint64_t)(uintptr_t)p;
+  return i32x4{(int)(uint32_t)at, (int)((uint32_t)(at >> 32) & 0xffffu), (int)bytes, 0x00020000};
+}
+__device__ __forceinline__ void load_to_lds(const i32x4& from, uint32_t to, int offset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(offset), "s"(from) : "memory");
+}
+// Until LEFT of them are under way.  The builtin tells the compiler that its own loads are done too (it does not read assembly, and would wait for them, and so for
+// the loads to LDS, at their next use).
+template <int LEFT>
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory");
+  if constexpr (LEFT == 0) __builtin_amdgcn_s_waitcnt(0x0f70);
+}
+__device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(LDS_PTR(const char))p; }
+
+// Whether x holds for a thread of the workgroup; word: of LDS.
+__device__ __forceinline__ bool any_of_workgroup(bool x, int* word) {
+  if (threadIdx.x == 0) *word = 0;
+  __syncthreads();
+  if (x) *word = 1;
+  __syncthreads();
+  const bool any = *word != 0;
+  __syncthreads();
+  return any;
+}
+
 // The keys of one wave's 16 rows of a tile: first vector in the cache, and how many of the 16 there are.
 struct Keys16 { int64_t vec; int n; };
 __device__ __forceinline__ Keys16 keys16(const PagedCache& c, int b, int hk, int p, int end) {
@@ -58,7 +104,43 @@ __device__ __forceinline__ Keys16 keys16(const PagedCache& c, int b, int hk, int
   return {vector_of(c, page, hk, p), n < 16 ? n : 16};
 }
 
-// Whether one of 8 bf16 is infinite or NaN; and: those out of v, with a 1 for each in count.
+// LDS addresses of a lane's operands in a tile of RowTile's layout.  Its swizzle is an XOR of chunk numbers, so that the steps along head_dim are XORs of one address
+// and steps of 16 rows an offset: key(kk, i) of keys 32 i + lane % 32, step kk; value(t2, ks) of columns 32 t2 .., keys 16 ks .., as frag_cols.
+template <int DH>
+struct Operands {
+  using Tile = RowTile<kTileKeys, DH, 4>;
+  uint32_t k, v;
+  __device__ __forceinline__ Operands(uint32_t tiles, int lane) {
+    const int row = lane & 31, grp = lane >> 4, s = lane & 15, vrow = ((grp >> 1) << 2) + (s >> 2), col = ((grp & 1) << 4) + ((s & 3) << 2);
+    k = tiles + row * Tile::ROW_B + (((lane >> 5) ^ Tile::swz(row)) << 4);
+    v = tiles + Tile::BYTES + vrow * Tile::ROW_B + ((((col >> 3) ^ Tile::swz(vrow)) << 4) | ((col & 7) << 1));
+  }
+  __device__ __forceinline__ bf16x8 key(int kk, int i) const {
+    return *(LDS_PTR(const bf16x8))(uintptr_t)((k ^ (kk << 5)) + i * (32 * Tile::ROW_B));
+  }
+  __device__ __forceinline__ bf16x8 value(int t2, int ks) const {
+    const uint32_t lo = v ^ (t2 << 6), hi = v ^ (t2 << 6) ^ 32;       // swz(row + 8) = swz(row) ^ 2
+    bf16x8 x;
+    x.lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)(lo + ks * 16 * Tile::ROW_B));
+    x.hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)(hi + (ks * 16 + 8) * Tile::ROW_B));
+    return x;
+  }
+};
+
+// Values that are not finite out of v, with a 1 for each in count.
+__device__ __forceinline__ void split_not_finite(bf16x8& v, bf16x8& count) {
+  u32x4 u = __builtin_bit_cast(u32x4, v), n;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t odd = ((u[i] & 0x7f80u) == 0x7f80u ? 0xffffu : 0) | ((u[i] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0);
+    n[i] = odd & 0x3f803f80u;          // 1.0
+    u[i] &= ~odd;
+  }
+  v = __builtin_bit_cast(bf16x8, u);
+  count = __builtin_bit_cast(bf16x8, n);
+}
+
+// Whether one of 8 bf16 is infinite or NaN.
 __device__ __forceinline__ bool any_not_finite(const bf16x8& v) {
   const u32x4 u = __builtin_bit_cast(u32x4, v);
   bool odd = false;
@@ -66,26 +148,18 @@ __device__ __forceinline__ bool any_not_finite(const bf16x8& v) {
   for (int i = 0; i < 4; ++i) odd |= (u[i] & 0x7f80u) == 0x7f80u || (u[i] & 0x7f800000u) == 0x7f800000u;
   return odd;
 }
-__device__ __forceinline__ void split_not_finite(bf16x8& v, bf16x8& count) {
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const bool odd = !(fabsf((float)v[e]) < INFINITY);
-    count[e] = (bf16_t)(odd ? 1.f : 0.f);
-    if (odd) v[e] = (bf16_t)0.f;
-  }
-}
 
 template <int DH, bool E4M3>
 __global__ __launch_bounds__(256, 2) void tile_kernel(const AttendArgs a) {
   using Tile = RowTile<kTileKeys, DH, 4>;
   constexpr int STAGE = 2 * Tile::BYTES;
-  // e4m3: a lane's part of a wave's 16 keys
-  constexpr int PER_LANE = DH / 4, CHUNK = PER_LANE < 16 ? PER_LANE : 16, NLOAD = PER_LANE / CHUNK, LANES = DH / CHUNK, ROWS = 64 / LANES;
+  // e4m3: a wave's 16 keys as they are held; CHUNK bytes a lane and load, LANES of them a key
+  constexpr int HELD = 16 * DH, CHUNK = HELD < 1024 ? 8 : 16, NLOAD = HELD / (64 * CHUNK), LANES = DH / CHUNK, ROWS = 64 / LANES;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const PagedCache& c = a.cache;
   int j, pair;
-  split_block_id((int)blockIdx.x, c.batch * c.heads, j, pair);
+  work_of((int)blockIdx.x, c.batch * c.heads, j, pair);
   const int b = pair / c.heads, hk = pair % c.heads;
   const int tile = a.tiles - 1 - j / a.splits, split = j % a.splits;     // long rows (late tokens) first
   const int lq = lane & 31, half = lane >> 5;
@@ -99,6 +173,8 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttendArgs a) {
   const int lim = n_rows > 0 ? last_key(min(r, n_rows - 1)) : -1, lim0 = __builtin_amdgcn_readfirstlane(lim);
   // the last key that any of the wave's rows sees; none for a wave behind the last row
   const int lim1 = row0 + wave * 32 < n_rows ? __builtin_amdgcn_readlane(lim, 31) : -1;
+  const int first_lim = n_rows > 0 ? __builtin_amdgcn_readfirstlane(last_key(min(row0, n_rows - 1))) : -1;     // the first row's
+  int* first_odd = reinterpret_cast<int*>(smem + 2 * STAGE);       // the first key with a value that is not finite, of each column; whether there is any
   const int all = (end + kTileKeys - 1) / kTileKeys, per = (all + a.splits - 1) / a.splits;
   const int t0 = split * per, t1 = min(all, t0 + per);
 
@@ -114,7 +190,8 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttendArgs a) {
     bool missing = false;
     for (int i = (t0 * kTileKeys >> c.shift) + threadIdx.x, n = (min(end, t1 * kTileKeys) - 1) >> c.shift; i <= n; i += 256)
       missing |= (uint32_t)c.table[(int64_t)b * c.columns + i] >= (uint32_t)c.n_pages;
-    missing = __syncthreads_or(missing);
+    if (threadIdx.x <= DH) first_odd[threadIdx.x] = threadIdx.x < DH ? 0x7fffffff : 0;
+    missing = any_of_workgroup(missing, reinterpret_cast<int*>(smem));
 
     bf16x8 qf[DH / 16];
     {
@@ -124,59 +201,91 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttendArgs a) {
       for (int kk = 0; kk < DH / 16; ++kk) qf[kk] = *reinterpret_cast<const bf16x8*>(qp + kk * 16);
     }
 
-    u32x4 raw[2][NLOAD];               // e4m3: the next tile's
-    float scl[2][NLOAD];
+    // e4m3: of the wave's 16 keys of the next tile in lanes 0 .. 15, of its values in the next 16; and how many of the keys there are
+    uint32_t scales = 0;
+    int there = 0;
     const auto load = [&](int t, int stage) {
       const Keys16 k16 = keys16(c, b, hk, t * kTileKeys + wave * 16, end);
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
+        const uint32_t to = lds_address(smem) + stage * STAGE + w * Tile::BYTES + wave * (16 * Tile::ROW_B);
         if constexpr (!E4M3) {
-          const auto rs = attn_rsrc(c.x[w] + k16.vec * (DH * 2), (uint32_t)(k16.n * DH * 2));
-          char* to = smem + stage * STAGE + w * Tile::BYTES + wave * (16 * DH * 2);
+          const i32x4 from = descriptor(c.x[w] + k16.vec * (DH * 2), (uint32_t)(k16.n * DH * 2));
 #pragma unroll
           for (int i = 0; i < Tile::PER_WAVE; ++i) {
             const int row = i * Tile::RPI + lane / Tile::LPR, ch = (lane % Tile::LPR) ^ Tile::swz(row);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (LDS_PTR(void))(to + i * 1024), 16, row * (DH * 2) + (ch << 4), 0, 0, 0);
+            load_to_lds(from, to + i * 1024, row * (DH * 2) + (ch << 4));
           }
         } else {
-          const auto rs = attn_rsrc(c.x[w] + k16.vec * DH, (uint32_t)(k16.n * DH));
-          const auto ss = attn_rsrc(c.scale[w] + k16.vec, (uint32_t)k16.n);
+          const i32x4 from = descriptor(c.x[w] + k16.vec * DH, (uint32_t)(k16.n * DH));
+#pragma unroll
+          for (int i = 0; i < (HELD + 1023) / 1024; ++i)
+            if (HELD >= 1024 || lane < HELD / 16) load_to_lds(from, to + i * 1024, i * 1024 + lane * 16);
+        }
+      }
+      if constexpr (E4M3) {
+        scales = ((lane & 16 ? c.scale[1] : c.scale[0]) + k16.vec)[lane & 15];
+        there = k16.n;
+      }
+    };
+    // what a wave has loaded, made ready for all: e4m3 in its place as bf16; and, of a tile that some row sees in part, values that are not finite taken
+    // out, since a weight of 0 times one of them is NaN: the first key that has one in a column is remembered, and the rows that see it get NaN at the end
+    const auto arrived = [&](int t, int stage) {
+      wait_loads<0>();
+      if constexpr (E4M3) {
+        scales = (lane & 15) < there ? scales << 23 : 0;        // keys that are not there are zeros times whatever was read
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          char* own = smem + stage * STAGE + w * Tile::BYTES + wave * (16 * Tile::ROW_B);
+          u32x2 raw[NLOAD][CHUNK / 8];
+#pragma unroll
+          for (int i = 0; i < NLOAD; ++i)
+#pragma unroll
+            for (int h = 0; h < CHUNK / 8; ++h) raw[i][h] = *reinterpret_cast<const u32x2*>(own + (i * 64 + lane) * CHUNK + h * 8);
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // all of it is read before any of it is written over
 #pragma unroll
           for (int i = 0; i < NLOAD; ++i) {
-            const int row = i * ROWS + lane / LANES, at = row * DH + (lane % LANES) * CHUNK;
-            if constexpr (CHUNK == 16) raw[w][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, at, 0, 0));
-            else { const u32x2 u = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rs, at, 0, 0)); raw[w][i][0] = u[0]; raw[w][i][1] = u[1]; }
-            scl[w][i] = __uint_as_float((uint32_t)__builtin_amdgcn_raw_buffer_load_b8(ss, row, 0, 0) << 23);
+            const int key = i * ROWS + lane / LANES, ch = (lane % LANES) * (CHUNK / 8);
+            const float scale = __uint_as_float((uint32_t)__shfl((int)scales, w * 16 + key, 64));
+#pragma unroll
+            for (int h = 0; h < CHUNK / 8; ++h)
+              *reinterpret_cast<bf16x8*>(own + key * Tile::ROW_B + (((ch + h) ^ Tile::swz(key)) << 4)) = unpack_e4m3(raw[i][h], scale);
           }
         }
       }
-    };
-    const auto unpack = [&](int stage) {
-      if constexpr (E4M3) {
+      if (t * kTileKeys + kTileKeys - 1 > first_lim) {
+        char* own = smem + stage * STAGE + Tile::BYTES + wave * (16 * Tile::ROW_B);
+#pragma unroll 1
+        for (int i = 0; i < Tile::PER_WAVE; ++i) {
+          bf16x8* at = reinterpret_cast<bf16x8*>(own + i * 1024 + lane * 16);
+          bf16x8 v = *at;
+          if (!any_not_finite(v)) continue;
+          const int key = i * Tile::RPI + lane / Tile::LPR, ch = (lane % Tile::LPR) ^ Tile::swz(key);
 #pragma unroll
-        for (int w = 0; w < 2; ++w)
-#pragma unroll
-          for (int i = 0; i < NLOAD; ++i) {
-            const int row = wave * 16 + i * ROWS + lane / LANES, ch = (lane % LANES) * (CHUNK / 8);
-            char* to = smem + stage * STAGE + w * Tile::BYTES + row * Tile::ROW_B;
-#pragma unroll
-            for (int h = 0; h < CHUNK / 8; ++h)
-              *reinterpret_cast<bf16x8*>(to + (((ch + h) ^ Tile::swz(row)) << 4)) = unpack_e4m3(u32x2{raw[w][i][2 * h], raw[w][i][2 * h + 1]}, scl[w][i]);
-          }
+          for (int e = 0; e < 8; ++e)
+            if (!(fabsf((float)v[e]) < INFINITY)) {
+              atomicMin(&first_odd[ch * 8 + e], t * kTileKeys + wave * 16 + key);
+              v[e] = (bf16_t)0.f;
+            }
+          *at = v;
+          first_odd[DH] = 1;
+        }
       }
     };
 
+    const Operands<DH> operands(lds_address(smem), lane);
     load(t0, 0);
-    unpack(0);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    arrived(t0, 0);
     __syncthreads();
     int stage = 0;
     for (int t = t0; t < t1; ++t) {
       if (t + 1 < t1) load(t + 1, stage ^ 1);
       const int kv0 = t * kTileKeys;
-      const char* tk = smem + stage * STAGE;
-      const char* tv = tk + Tile::BYTES;
       if (kv0 <= lim1) {
+      Operands<DH> at = operands;
+      at.k += stage * STAGE;
+      at.v += stage * STAGE;
+      asm volatile("" : "+v"(at.k), "+v"(at.v));                 // their XORs are formed here, and take no registers across the loop
       f32x16 s[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i)
@@ -186,10 +295,9 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttendArgs a) {
       for (int kk = 0; kk < DH / 16; ++kk)
 #pragma unroll
         for (int i = 0; i < 2; ++i)
-          s[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(Tile::frag_rows(tk, i * 32, kk, lane), qf[kk], s[i], 0, 0, 0);
+          s[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at.key(kk, i), qf[kk], s[i], 0, 0, 0);
       // keys after the row's own position (only on tiles that reach past this wave's first row)
-      const bool masked = kv0 + kTileKeys - 1 > lim0;
-      if (masked) mask_rows_above<2>(s, lim - kv0 - (half << 2), -INFINITY);
+      if (kv0 + kTileKeys - 1 > lim0) mask_rows_above<2>(s, lim - kv0 - (half << 2), -INFINITY);
       if (missing) {
 #pragma unroll
         for (int g = 0; g < 4; ++g)
@@ -224,48 +332,23 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttendArgs a) {
           psum += pv;
         }
       lsum += psum;
-      // a weight of 0 times a value that is not finite is NaN: where a masked tile holds such values, they are counted apart, for the rows that see them
-      bool odd = false;
-      if (masked) {
-        for (int ks = 0; ks < 4; ++ks)
 #pragma unroll
-          for (int t2 = 0; t2 < DH / 32; ++t2) odd |= any_not_finite(Tile::frag_cols(tv, t2 * 32, ks * 16, lane));
-        odd = __builtin_amdgcn_ballot_w64(odd) != 0;
-      }
-      if (!odd) {
+      for (int ks = 0; ks < 4; ++ks) {
+        const bf16x8 pf = pack_slots(s[ks >> 1], (ks & 1) * 8);
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
-          const bf16x8 pf = pack_slots(s[ks >> 1], (ks & 1) * 8);
-#pragma unroll
-          for (int t2 = 0; t2 < DH / 32; ++t2)
-            oacc[t2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(Tile::frag_cols(tv, t2 * 32, ks * 16, lane), pf, oacc[t2], 0, 0, 0);
-        }
-      } else {
-#pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
-          const bf16x8 pf = pack_slots(s[ks >> 1], (ks & 1) * 8);
-          bf16x8 seen;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) seen[e] = (bf16_t)(kv0 + ks * 16 + ((e >> 2) << 3) + (half << 2) + (e & 3) <= lim ? 1.f : 0.f);
-#pragma unroll
-          for (int t2 = 0; t2 < DH / 32; ++t2) {
-            bf16x8 v = Tile::frag_cols(tv, t2 * 32, ks * 16, lane), count;
-            split_not_finite(v, count);
-            f32x16 n;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) n[e] = 0.f;
-            n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(count, seen, n, 0, 0, 0);
-            oacc[t2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pf, oacc[t2], 0, 0, 0);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) oacc[t2][e] = n[e] > 0.f ? NAN : oacc[t2][e];
-          }
-        }
+        for (int t2 = 0; t2 < DH / 32; ++t2) oacc[t2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at.value(t2, ks), pf, oacc[t2], 0, 0, 0);
       }
       }
-      if (t + 1 < t1) unpack(stage ^ 1);
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      if (t + 1 < t1) arrived(t + 1, stage ^ 1);
       __syncthreads();
       stage ^= 1;
+    }
+    if (first_odd[DH]) {
+#pragma unroll
+      for (int t2 = 0; t2 < DH / 32; ++t2)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (first_odd[t2 * 32 + ((e >> 2) << 3) + (half << 2) + (e & 3)] <= lim) oacc[t2][e] = NAN;
     }
     lsum = sum_across_halves(lsum);
   }
@@ -304,30 +387,367 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttendArgs a) {
   if (a.lse && half == 0) a.lse[((int64_t)b * a.Hq + at.h) * a.seq + at.t] = any ? (m + log2f(lsum)) * kLn2 : -INFINITY;
 }
 
-// Joins the parts of split rows: DH / 4 lanes a row.
-template <int DH>
-__global__ __launch_bounds__(256) void combine_kernel(const AttendArgs a, int64_t rows, int rows_per_tile) {
-  constexpr int LPR = DH / 4;
+// max (sum) over the four lanes l, l ^ 16, l ^ 32, l ^ 48, in all of them
+__device__ __forceinline__ float max_across_quarters(float x) {
+  x = max_across_halves(x);
+  return fmaxf(x, __shfl_xor(x, 16, 64));
+}
+__device__ __forceinline__ float sum_across_quarters(float x) {
+  x = sum_across_halves(x);
+  return x + __shfl_xor(x, 16, 64);
+}
+
+// A wave's tile of 32 keys, or values, in LDS as the cache holds it: rows of ROW_B bytes, 16-byte chunk c of row r at chunk c ^ swz(r).  Free of bank conflicts (the LDS serves
+// 256 B of banks a clock) for both of its reads:
+//   row reads: 16 lanes, 16 consecutive rows, one chunk;
+//   transposing reads: 32 lanes, which take 32 B (bf16) of rows 0 .. 7 or 8 .. 15 of 16, or 16 B (e4m3) of rows 0 .. 7 and 16 .. 23, or 8 .. 15 and 24 .. 31.
+template <int DH, bool E4M3>
+struct HeldTile {
+  static constexpr int ROW_B = DH * (E4M3 ? 1 : 2), CHUNKS = ROW_B / 16, BYTES = 32 * ROW_B;
+  static constexpr int WIDTH = ROW_B == 32 ? 4 : 16;                 // bytes a lane loads: a load's rows lie in one group of 16
+  static constexpr int RPI = 64 * WIDTH / ROW_B, LOADS = 32 / RPI;   // rows of a load, loads
+  static __device__ __forceinline__ int swz(int r) {
+    constexpr int SHARE = 16 / CHUNKS;                               // rows that 256 B hold
+    const int j = (r / SHARE) & (CHUNKS - 1);
+    if constexpr (E4M3) return j ^ (((r >> 4) & 1) * (CHUNKS / 2));
+    else return ((j << 1) | (j >> (CHUNKS == 16 ? 3 : CHUNKS == 8 ? 2 : 1))) & (CHUNKS - 1);
+  }
+  // loads a group of 16 rows, of which the first vector starts at p and n are there (the others are zeros)
+  static __device__ __forceinline__ void load(const char* p, int n, uint32_t to, int group, int lane) {
+    const i32x4 from = descriptor(p, (uint32_t)(n * ROW_B));
+#pragma unroll
+    for (int i = 0; i < LOADS / 2; ++i) {
+      const int at = lane * WIDTH, row = i * RPI + at / ROW_B, ch = (at % ROW_B) / 16 ^ swz(group * 16 + row);
+      const int offset = row * ROW_B + ch * 16 + at % 16;
+      const uint32_t dst = to + (group * (LOADS / 2) + i) * (64 * WIDTH);
+      if constexpr (WIDTH == 16) load_to_lds(from, dst, offset);
+      else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(dst)), "v"(offset), "s"(from) : "memory");
+    }
+  }
+};
+
+// Few rows (NR groups of 16), many keys: bound by the reading of the cache.  Each of the workgroup's four waves takes every fourth tile of 32 keys, which it loads to LDS for
+// itself, a tile ahead, so that the waves wait for nothing but their own loads; the four results are joined in LDS at the end.
+//   S[key][row] = K Q^T and O[d][row] += V^T P^T on v_mfma_f32_16x16x32_bf16: lane l has row l % 16 of its group, keys 4 (l / 16) .. + 3 of each half of the tile, and those are the
+//   slots that it gives the second product, whose other operand (transposing reads) is taken in that order.
+// e4m3 is read as it is held; scores and weights take the powers of two of their keys and values, exactly.
+template <int DH, bool E4M3, int NR>
+__global__ __launch_bounds__(256, NR == 1 ? 2 : 1) void rows_kernel(const AttendArgs a) {
+  using Tile = HeldTile<DH, E4M3>;
+  constexpr int STAGE = 2 * Tile::BYTES + (E4M3 ? 64 : 0), ROWS = 16 * NR;      // keys, values, and their 32 + 32 powers of two
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const PagedCache& c = a.cache;
-  const int64_t i = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;      // (pair, row of the pair)
-  if (i >= rows) return;
-  const int per_pair = a.seq * a.group, d = (threadIdx.x % LPR) * 4;
+  int j, pair;
+  work_of((int)blockIdx.x, c.batch * c.heads, j, pair);
+  const int b = pair / c.heads, hk = pair % c.heads, tile = a.tiles - 1 - j / a.splits, split = j % a.splits;
+  const int lr = lane & 15, quarter = lane >> 4;
+  const int n_rows = row_length(a.lengths, b, a.seq) * a.group, row0 = tile * ROWS;
+  const int64_t start = row_start(a.start, b), cap = (int64_t)c.columns << c.shift;
+  const auto last_key = [&](int row) { const int64_t p = start + row / a.group; return (int)(p < -1 ? -1 : p >= cap ? cap - 1 : p); };
+  const int end = row0 < n_rows ? last_key(min(row0 + ROWS, n_rows) - 1) + 1 : 0;
+  const int lim0 = n_rows > 0 ? __builtin_amdgcn_readfirstlane(last_key(min(row0, n_rows - 1))) : -1;
+  const int all = (end + 31) / 32, per = max((all + a.splits - 1) / a.splits, a.least);
+  const int u0 = split * per, u1 = min(all, u0 + per);
+
+  f32x4 acc[NR][DH / 16];
+  float m[NR], lsum[NR];
+  int lim[NR];
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+    m[n] = kNoKey;
+    lsum[n] = 0.f;
+    lim[n] = n_rows > 0 ? last_key(min(row0 + n * 16 + lr, n_rows - 1)) : -1;
+#pragma unroll
+    for (int t = 0; t < DH / 16; ++t) acc[n][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  if (u0 < u1) {
+    bool missing = false;
+    for (int i = (u0 * 32 >> c.shift) + threadIdx.x, n = (min(end, u1 * 32) - 1) >> c.shift; i <= n; i += 256)
+      missing |= (uint32_t)c.table[(int64_t)b * c.columns + i] >= (uint32_t)c.n_pages;
+    missing = any_of_workgroup(missing, reinterpret_cast<int*>(smem));
+
+    bf16x8 qf[NR][DH / 32];
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+      const RowPlace at = row_place(a, hk, min(row0 + n * 16 + lr, n_rows - 1));
+      const bf16_t* qp = a.q + (((int64_t)b * a.seq + at.t) * a.Hq + at.h) * DH;
+      // e4m3: a 16-byte read of a key holds the slots of two steps
+#pragma unroll
+      for (int kk = 0; kk < DH / 32; ++kk)
+        qf[n][kk] = *reinterpret_cast<const bf16x8*>(qp + (E4M3 && DH >= 64 ? (kk >> 1) * 64 + quarter * 16 + (kk & 1) * 8 : kk * 32 + quarter * 8));
+    }
+
+    const uint32_t own = lds_address(smem) + wave * (2 * STAGE);
+    const auto load = [&](int u, int stage) {
+      const Keys16 k16[2] = {keys16(c, b, hk, u * 32, end), keys16(c, b, hk, u * 32 + 16, end)};
+#pragma unroll
+      for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int w = 0; w < 2; ++w) Tile::load(c.x[w] + k16[g].vec * Tile::ROW_B, k16[g].n, own + stage * STAGE + w * Tile::BYTES, g, lane);
+      if constexpr (E4M3) {
+        // four lanes for each of (keys, values) x (first 16, last 16), from addresses of their own; where there are no keys, of others that take no part
+        const uint8_t* from = (lane & 8 ? c.scale[1] : c.scale[0]) + (lane & 4 ? k16[1].vec : k16[0].vec) + (lane & 3) * 4;
+        if (lane < 16)
+          asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(__builtin_amdgcn_readfirstlane(own + stage * STAGE + 2 * Tile::BYTES)), "v"(from) : "memory");
+      }
+    };
+    // a byte of 255 is no power of two, and may stand where there is no key: finite, so that a weight of 0 times it is 0
+    const auto scale_of = [](uint32_t four, int e) { return __uint_as_float(min((four >> (8 * e)) & 0xffu, 254u) << 23); };
+
+    int u = u0 + wave, stage = 0;
+    if (u < u1) load(u, 0);
+    for (; u < u1; u += 4) {
+      wait_loads<0>();
+      if (u + 4 < u1) load(u + 4, stage ^ 1);
+      const uint32_t tk = own + stage * STAGE, tv = tk + Tile::BYTES;
+      const int kv0 = u * 32;
+      uint32_t ks[2] = {}, vs[2] = {};           // of four keys of each half
+      if constexpr (E4M3)
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          ks[g] = *(LDS_PTR(const uint32_t))(uintptr_t)(tv + Tile::BYTES + g * 16 + quarter * 4);
+          vs[g] = *(LDS_PTR(const uint32_t))(uintptr_t)(tv + Tile::BYTES + 32 + g * 16 + quarter * 4);
+        }
+      f32x4 s[NR][2];
+#pragma unroll
+      for (int n = 0; n < NR; ++n)
+#pragma unroll
+        for (int g = 0; g < 2; ++g) s[n][g] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        const int row = g * 16 + lr;
+        if constexpr (E4M3 && DH >= 64) {
+#pragma unroll
+          for (int k2 = 0; k2 < DH / 64; ++k2) {
+            const u32x4 raw = *(LDS_PTR(const u32x4))(uintptr_t)(tk + row * Tile::ROW_B + (((k2 * 4 + quarter) ^ Tile::swz(row)) << 4));
+            const bf16x8 k0 = unpack_e4m3(u32x2{raw[0], raw[1]}, 1.f), k1 = unpack_e4m3(u32x2{raw[2], raw[3]}, 1.f);
+#pragma unroll
+            for (int n = 0; n < NR; ++n) {
+              s[n][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, qf[n][2 * k2], s[n][g], 0, 0, 0);
+              s[n][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, qf[n][2 * k2 + 1], s[n][g], 0, 0, 0);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int kk = 0; kk < DH / 32; ++kk) {
+            bf16x8 kf;
+            if constexpr (E4M3) kf = unpack_e4m3(*(LDS_PTR(const u32x2))(uintptr_t)(tk + row * Tile::ROW_B + (((quarter >> 1) ^ Tile::swz(row)) << 4) + (quarter & 1) * 8), 1.f);
+            else kf = *(LDS_PTR(const bf16x8))(uintptr_t)(tk + row * Tile::ROW_B + (((kk * 4 + quarter) ^ Tile::swz(row)) << 4));
+#pragma unroll
+            for (int n = 0; n < NR; ++n) s[n][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[n][kk], s[n][g], 0, 0, 0);
+          }
+        }
+      }
+      if constexpr (E4M3)
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float k = scale_of(ks[g], e);
+#pragma unroll
+            for (int n = 0; n < NR; ++n) s[n][g][e] *= k;
+          }
+      const bool masked = kv0 + 31 > lim0;
+      if (masked) {
+#pragma unroll
+        for (int n = 0; n < NR; ++n)
+#pragma unroll
+          for (int g = 0; g < 2; ++g)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[n][g][e] = kv0 + g * 16 + quarter * 4 + e > lim[n] ? -INFINITY : s[n][g][e];
+      }
+      if (missing) {
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+          if (page_of_wave(c, b, kv0 + g * 16) < 0)
+#pragma unroll
+            for (int n = 0; n < NR; ++n) s[n][g] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+      }
+      bf16x8 pf[NR];
+#pragma unroll
+      for (int n = 0; n < NR; ++n) {
+        float mx = fmaxf(fmaxf(fmaxf(s[n][0][0], s[n][0][1]), fmaxf(s[n][0][2], s[n][0][3])), fmaxf(fmaxf(s[n][1][0], s[n][1][1]), fmaxf(s[n][1][2], s[n][1][3]))) * a.scale_log2;
+        // the reference is raised only where some row's maximum grew by more than 2^8; until then the lanes of a row need not know each other's
+        if (__builtin_amdgcn_ballot_w64(mx > m[n] + 8.0f) != 0) {
+          const float m_new = fmaxf(m[n], max_across_quarters(mx)), alpha = fast_exp2(m[n] - m_new);
+          lsum[n] *= alpha;
+          m[n] = m_new;
+#pragma unroll
+          for (int t = 0; t < DH / 16; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[n][t][e] *= alpha;
+        }
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float p = fast_exp2(__builtin_fmaf(s[n][g][e], a.scale_log2, -m[n]));
+            lsum[n] += p;
+            pf[n][g * 4 + e] = (bf16_t)(E4M3 ? p * scale_of(vs[g], e) : p);
+          }
+      }
+      const auto value = [&](int t) {
+        if constexpr (E4M3) {
+          const int row = (lr >> 1) < 4 ? quarter * 4 + (lr >> 1) : 16 + quarter * 4 + (lr >> 1) - 4;
+          return unpack_e4m3(__builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((LDS_PTR(i32x2))(uintptr_t)(tv + row * Tile::ROW_B + ((t ^ Tile::swz(row)) << 4) + (lr & 1) * 8))), 1.f);
+        } else {
+          const int row = quarter * 4 + (lr >> 2), ch = t * 2 + ((lr & 3) >> 1), in = (lr & 1) * 8;
+          bf16x8 x;
+          x.lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)(tv + row * Tile::ROW_B + ((ch ^ Tile::swz(row)) << 4) + in));
+          x.hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)(tv + (row + 16) * Tile::ROW_B + ((ch ^ Tile::swz(row + 16)) << 4) + in));
+          return x;
+        }
+      };
+      if (!masked || a.seq == 1) {
+#pragma unroll
+        for (int t = 0; t < DH / 16; ++t) {
+          const bf16x8 vf = value(t);
+#pragma unroll
+          for (int n = 0; n < NR; ++n) acc[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[n], acc[n][t], 0, 0, 0);
+        }
+      } else {
+        // a weight of 0 times a value that is not finite is NaN: of a tile that some row does not see whole, such values are counted apart, for the rows that see them
+#pragma unroll
+        for (int t = 0; t < DH / 16; ++t) {
+          bf16x8 vf = value(t), count;
+          const bool odd = __builtin_amdgcn_ballot_w64(any_not_finite(vf)) != 0;
+          if (odd) split_not_finite(vf, count);
+#pragma unroll
+          for (int n = 0; n < NR; ++n) {
+            acc[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[n], acc[n][t], 0, 0, 0);
+            if (odd) {
+              bf16x8 seen;
+#pragma unroll
+              for (int e = 0; e < 8; ++e) seen[e] = (bf16_t)(kv0 + (e >> 2) * 16 + quarter * 4 + (e & 3) <= lim[n] ? 1.f : 0.f);
+              const f32x4 k = __builtin_amdgcn_mfma_f32_16x16x32_bf16(count, seen, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) acc[n][t][e] = k[e] > 0.f ? NAN : acc[n][t][e];
+            }
+          }
+        }
+      }
+      stage ^= 1;
+    }
+  }
+
+  // the four waves' results: every wave's maximum and sum, and its rows relative to the largest maximum, added up by all threads
+  float* stats = reinterpret_cast<float*>(smem);                       // [wave][ROWS][2]
+  float* rows = stats + 4 * ROWS * 2;                                  // [wave][ROWS][DH + 4]
+  __syncthreads();
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+    lsum[n] = sum_across_quarters(lsum[n]);
+    if (quarter == 0) {
+      stats[(wave * ROWS + n * 16 + lr) * 2] = m[n];
+      stats[(wave * ROWS + n * 16 + lr) * 2 + 1] = lsum[n];
+    }
+#pragma unroll
+    for (int t = 0; t < DH / 16; ++t) *reinterpret_cast<f32x4*>(rows + (wave * ROWS + n * 16 + lr) * (DH + 4) + t * 16 + quarter * 4) = acc[n][t];
+  }
+  __syncthreads();
+  constexpr int LPR = DH / 4;
+  for (int i = threadIdx.x; i < ROWS * LPR; i += 256) {
+    const int row = i / LPR, d = (i % LPR) * 4, r = row0 + row;
+    if (r >= a.seq * a.group) continue;
+    float top = stats[row * 2];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) top = fmaxf(top, stats[(w * ROWS + row) * 2]);
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    float sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float l = stats[(w * ROWS + row) * 2 + 1], f = l == 0.f ? 0.f : fast_exp2(stats[(w * ROWS + row) * 2] - top);
+      sum += f * l;
+      const f32x4 x = *reinterpret_cast<const f32x4*>(rows + (w * ROWS + row) * (DH + 4) + d);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] += f * x[e];
+    }
+    if (a.splits > 1) {
+      const int64_t at = (((int64_t)pair * a.tiles + tile) * a.splits + split) * ROWS + row;
+      if (d == 0) {
+        a.stats[at * 2] = top;
+        a.stats[at * 2 + 1] = sum;
+      }
+      if (u0 < u1) *reinterpret_cast<f32x4*>(a.sums + at * DH + d) = o;
+      continue;
+    }
+    const bool any = r < n_rows && sum != 0.f;
+    const float inv = any ? 1.0f / sum : 0.f;
+    const RowPlace at = row_place(a, hk, r);
+    bf16x4 ov;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) ov[e] = (bf16_t)(any ? o[e] * inv : 0.f);
+    *reinterpret_cast<bf16x4*>(a.o + (((int64_t)b * a.seq + at.t) * a.Hq + at.h) * DH + d) = ov;
+    if (a.lse && d == 0) a.lse[((int64_t)b * a.Hq + at.h) * a.seq + at.t] = any ? (top + log2f(sum)) * kLn2 : -INFINITY;
+  }
+}
+
+// Joins the parts of split rows.  DH / 4 lanes hold a row; `side` such groups of lanes share a row's parts, four of which they have under way at a time, and are joined in LDS.
+template <int DH>
+__global__ __launch_bounds__(1024) void combine_kernel(const AttendArgs a, int64_t rows, int rows_per_tile, int side) {
+  constexpr int LPR = DH / 4;
+  __shared__ float stats[1024 / LPR][2];
+  __shared__ f32x4 sums[1024];
+  const PagedCache& c = a.cache;
+  const int group = threadIdx.x / LPR, lane = threadIdx.x % LPR, here = blockDim.x / LPR;
+  const int64_t i = (int64_t)blockIdx.x * (here / side) + group / side;      // (pair, row of the pair)
+  const int per_pair = a.seq * a.group, d = lane * 4;
   const int64_t pair = i / per_pair;
   const int r = (int)(i % per_pair), b = (int)(pair / c.heads), hk = (int)(pair % c.heads);
   const int64_t first = (pair * a.tiles + r / rows_per_tile) * a.splits;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   float m = kNoKey, sum = 0.f;
-  if (r < row_length(a.lengths, b, a.seq) * a.group) {
-    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.stats[((first + s) * rows_per_tile + r % rows_per_tile) * 2]);
-    for (int s = 0; s < a.splits; ++s) {
-      const int64_t at = (first + s) * rows_per_tile + r % rows_per_tile;
-      const float l = a.stats[at * 2 + 1];
-      if (l == 0.f) continue;
-      const float w = fast_exp2(a.stats[at * 2] - m);
-      sum += w * l;
-      acc += w * *reinterpret_cast<const f32x4*>(a.sums + at * DH + d);
+  if (i < rows && r < row_length(a.lengths, b, a.seq) * a.group) {
+    const int64_t at0 = first * rows_per_tile + r % rows_per_tile;
+    for (int s0 = group % side; s0 < a.splits; s0 += 4 * side) {
+      float ms[4], ls[4], top = m;
+      f32x4 x[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int s = min(s0 + k * side, a.splits - 1);
+        const int64_t at = at0 + (int64_t)s * rows_per_tile;
+        ms[k] = a.stats[at * 2];
+        ls[k] = s0 + k * side < a.splits ? a.stats[at * 2 + 1] : 0.f;
+        x[k] = *reinterpret_cast<const f32x4*>(a.sums + at * DH + d);        // of a part without keys: whatever is there, and not used
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) top = ls[k] == 0.f ? top : fmaxf(top, ms[k]);
+      const float old = sum == 0.f ? 0.f : fast_exp2(m - top);
+      sum *= old;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] = old == 0.f ? 0.f : acc[e] * old;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (ls[k] == 0.f) continue;
+        const float w = fast_exp2(ms[k] - top);
+        sum += w * ls[k];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] += w * x[k][e];
+      }
+      m = top;
     }
   }
+  if (side > 1) {
+    if (lane == 0) { stats[group][0] = m; stats[group][1] = sum; }
+    sums[threadIdx.x] = acc;
+    __syncthreads();
+    if (group % side) return;
+    for (int k = 1; k < side; ++k) m = stats[group + k][1] == 0.f ? m : fmaxf(m, stats[group + k][0]);
+    const float w0 = sum == 0.f ? 0.f : fast_exp2(stats[group][0] - m);
+    sum = sum == 0.f ? 0.f : sum * w0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] = w0 == 0.f ? 0.f : acc[e] * w0;
+    for (int k = 1; k < side; ++k) {
+      if (stats[group + k][1] == 0.f) continue;
+      const float w = fast_exp2(stats[group + k][0] - m);
+      sum += w * stats[group + k][1];
+      const f32x4 x = sums[threadIdx.x + k * LPR];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] += w * x[e];
+    }
+  }
+  if (i >= rows) return;
   const RowPlace at = row_place(a, hk, r);
   const float inv = sum != 0.f ? 1.0f / sum : 0.f;
   bf16x4 ov;
@@ -337,55 +757,79 @@ __global__ __launch_bounds__(256) void combine_kernel(const AttendArgs a, int64_
   if (a.lse && d == 0) a.lse[((int64_t)b * a.Hq + at.h) * a.seq + at.t] = sum != 0.f ? (m + log2f(sum)) * kLn2 : -INFINITY;
 }
 
-// Which way a call goes.  Rows of tile_kernel's workgroups, tiles of a pair, and parts of a tile's keys: as many as fill the chip twice over, of no
-// fewer than 4 tiles of keys each.
-struct AttendPlan { int rows, tiles, splits; int64_t pairs; };
-constexpr int kWorkgroupsWanted = 512;
+// Which way a call goes: rows of a workgroup (16 or 32: rows_kernel; 128: tile_kernel), tiles of a pair's rows, and parts of a tile's keys.  Up to 32 rows the cache's bytes
+// are what counts and rows_kernel is as fast as they come; tile_kernel's matrix products of 32 rows a wave are for more.
+struct AttendPlan { int rows, tiles, splits, least; int64_t pairs; };
+constexpr int64_t kRowsWanted = 4096 * 16, kTilesWanted = 512;       // workgroups times rows of rows_kernel; workgroups of tile_kernel
+constexpr int64_t kKeysLeast = 256;                                  // of a part
+static int64_t most_splits(int64_t max_tokens) { return (max_tokens + kKeysLeast - 1) / kKeysLeast; }
 static AttendPlan attend_plan(int64_t batch, int64_t seq, int64_t Hkv, int64_t group, int64_t max_tokens) {
   AttendPlan p;
-  p.rows = kTileRows;
+  const int64_t rows = seq * group;
+  p.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : kTileRows;
   p.pairs = batch * Hkv;
-  p.tiles = (int)((seq * group + p.rows - 1) / p.rows);
-  const int64_t have = p.pairs * p.tiles, most = (max_tokens + 4 * kTileKeys - 1) / (4 * kTileKeys);
-  int64_t splits = have >= kWorkgroupsWanted ? 1 : kWorkgroupsWanted / have;
-  if (splits > most) splits = most;
-  p.splits = (int)(splits < 1 ? 1 : splits);
+  p.tiles = (int)((rows + p.rows - 1) / p.rows);
+  const int64_t wanted = (p.rows == kTileRows ? kTilesWanted : kRowsWanted / p.rows) / (p.pairs * p.tiles), most = most_splits(max_tokens);
+  p.splits = (int)(wanted < 1 ? 1 : wanted < most ? wanted : most);
+  p.least = (int)(kKeysLeast / 32);
   return p;
 }
 
-// Sums and statistics of the parts.  Rows of all workgroups of a split call, bounded so that the size does not fall as the call grows: pairs * tiles *
-// splits stays within kWorkgroupsWanted wherever there is a split at all.
+// Sums and statistics of the parts: pairs * tiles * splits * rows is within kRowsWanted wherever there is a split, and within pairs * (rows, filled up) * most_splits,
+// neither of which falls as the call grows.
+static int64_t rows_held(int64_t batch, int64_t seq, int64_t Hkv, int64_t group, int64_t max_tokens) {
+  const AttendPlan p = attend_plan(batch, seq, Hkv, group, max_tokens);
+  const int64_t rows = p.pairs * p.tiles, most = most_splits(max_tokens);
+  return rows < kRowsWanted && rows * p.rows < kRowsWanted && most < kRowsWanted && rows * p.rows * most < kRowsWanted ? rows * p.rows * most : kRowsWanted;
+}
 size_t paged_attention_workspace(int64_t batch, int64_t seq, int64_t Hq, int64_t Hkv, int64_t dh, int64_t max_tokens) {
-  return (size_t)kWorkgroupsWanted * kTileRows * (dh + 2) * sizeof(float);
+  return (size_t)rows_held(batch, seq, Hkv, Hq / Hkv, max_tokens) * (dh + 2) * sizeof(float);
 }
 
+template <int DH, bool E4M3, int NR>
+static int launch_rows(const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
+  constexpr int tiles = 4 * 2 * (2 * HeldTile<DH, E4M3>::BYTES + (E4M3 ? 64 : 0)), results = 4 * 16 * NR * (DH + 6) * (int)sizeof(float), lds = tiles > results ? tiles : results;
+  static std::atomic<unsigned long long> done{0};
+  if (int rc = reserve_lds(rows_kernel<DH, E4M3, NR>, lds, done, "paged_attention_forward")) return rc;
+  hipLaunchKernelGGL((rows_kernel<DH, E4M3, NR>), dim3((unsigned)(p.pairs * p.tiles * p.splits)), dim3(256), lds, st, a);
+  return check_launch("paged_attention_forward");
+}
 template <int DH, bool E4M3>
-static int launch_attend(AttendArgs& a, const AttendPlan& p, hipStream_t st) {
-  constexpr int lds = 2 * 2 * kTileKeys * DH * 2;
+static int launch_tiles(const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
+  constexpr int lds = 2 * 2 * kTileKeys * DH * 2 + (DH + 4) * (int)sizeof(int);
   static std::atomic<unsigned long long> done{0};
   if (int rc = reserve_lds(tile_kernel<DH, E4M3>, lds, done, "paged_attention_forward")) return rc;
   hipLaunchKernelGGL((tile_kernel<DH, E4M3>), dim3((unsigned)(p.pairs * p.tiles * p.splits)), dim3(256), lds, st, a);
-  if (int rc = check_launch("paged_attention_forward")) return rc;
-  if (p.splits == 1) return 0;
+  return check_launch("paged_attention_forward");
+}
+template <int DH, bool E4M3>
+static int launch_attend(const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
+  const int rc = p.rows == 16 ? launch_rows<DH, E4M3, 1>(a, p, st) : p.rows == 32 ? launch_rows<DH, E4M3, 2>(a, p, st) : launch_tiles<DH, E4M3>(a, p, st);
+  if (rc || p.splits == 1) return rc;
+  // groups of lanes to a row: enough that each has no more than four parts, as far as a workgroup of 1024 threads goes
+  constexpr int LPR = DH / 4;
+  int side = 1;
+  while (side < 1024 / LPR && side * 4 < p.splits) side *= 2;
+  const int threads = side * LPR > 256 ? side * LPR : 256, per = threads / (side * LPR);
   const int64_t rows = p.pairs * a.seq * a.group;
-  constexpr int per = 256 / (DH / 4);
-  hipLaunchKernelGGL((combine_kernel<DH>), dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, st, a, rows, p.rows);
+  hipLaunchKernelGGL((combine_kernel<DH>), dim3((unsigned)((rows + per - 1) / per)), dim3(threads), 0, st, a, rows, p.rows, side);
   return check_launch("paged_attention_forward, joining parts");
 }
 
 int launch_paged_attention(const CacheCall& c, const void* q, int64_t seq, int64_t Hq, float scale, void* o, float* lse, void* workspace,
                            hipStream_t st) {
-  const AttendPlan p = attend_plan(c.batch, seq, c.heads, Hq / c.heads, c.columns * c.page_size);
+  const int64_t group = Hq / c.heads, max_tokens = c.columns * c.page_size;
+  const AttendPlan p = attend_plan(c.batch, seq, c.heads, group, max_tokens);
   AttendArgs a{};
   a.cache = paged_cache(c);
   a.q = (const bf16_t*)q;
   a.start = c.start; a.lengths = c.lengths;
   a.o = (bf16_t*)o;
   a.lse = lse;
-  a.stats = (float*)workspace;
-  a.sums = a.stats + (int64_t)kWorkgroupsWanted * kTileRows * 2;
-  a.seq = (int)seq; a.Hq = (int)Hq; a.group = (int)(Hq / c.heads);
-  a.tiles = p.tiles; a.splits = p.splits;
+  a.sums = (float*)workspace;
+  a.stats = a.sums + rows_held(c.batch, seq, c.heads, group, max_tokens) * c.dh;
+  a.seq = (int)seq; a.Hq = (int)Hq; a.group = (int)group;
+  a.tiles = p.tiles; a.splits = p.splits; a.least = p.least;
   a.scale_log2 = scale * kLog2e;
   if (c.e4m3) return c.dh == 128 ? launch_attend<128, true>(a, p, st) : c.dh == 64 ? launch_attend<64, true>(a, p, st) : launch_attend<32, true>(a, p, st);
   return c.dh == 128 ? launch_attend<128, false>(a, p, st) : c.dh == 64 ? launch_attend<64, false>(a, p, st) : launch_attend<32, false>(a, p, st);
