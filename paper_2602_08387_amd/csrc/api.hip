@@ -805,7 +805,8 @@ static int paged_shape_ok(const char* who, const dlayer_kv_cache* c, int64_t seq
 
 size_t paged_attention_workspace_bytes(const dlayer_kv_cache* cache, int64_t seq, int64_t n_q_heads) {
   if (paged_shape_ok("paged_attention_workspace_bytes", cache, seq, n_q_heads, false)) return 0;
-  return paged_attention_workspace(cache->batch, seq, n_q_heads, cache->n_kv_heads, cache->head_dim, (int64_t)cache->max_pages * cache->page_size);
+  return paged_attention_workspace(cache->batch, seq, n_q_heads, cache->n_kv_heads, cache->head_dim, cache->dtype == DLAYER_CACHE_E4M3,
+                                   (int64_t)cache->max_pages * cache->page_size);
 }
 
 int paged_attention_forward(const dlayer_kv_cache* cache, const void* q, const int64_t* start, const int64_t* lengths, int64_t seq, int64_t n_q_heads,

@@ -176,7 +176,7 @@ struct CacheCall {
 int launch_kv_cache_append(const CacheCall& c, const void* q, const void* k, const void* v, int64_t seq, int64_t Hq, float base, int layout,
                            void* q_out, hipStream_t st);
 int launch_kv_cache_read(const CacheCall& c, int64_t seq, void* k, void* v, hipStream_t st);
-size_t paged_attention_workspace(int64_t batch, int64_t seq, int64_t Hq, int64_t Hkv, int64_t dh, int64_t max_tokens);
+size_t paged_attention_workspace(int64_t batch, int64_t seq, int64_t Hq, int64_t Hkv, int64_t dh, bool e4m3, int64_t max_tokens);
 int launch_paged_attention(const CacheCall& c, const void* q, int64_t seq, int64_t Hq, float scale, void* o, float* lse, void* workspace,
                            hipStream_t st);
 

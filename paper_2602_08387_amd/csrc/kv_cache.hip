@@ -9,23 +9,13 @@
 // of them), so that its angles are evaluated once: in fp64, one pair a lane, handed on through LDS as fp32.
 #include "common.h"
 #include "kernels.h"
+#include "lane_exchange.h"
 #include "paged_cache.h"
 
 namespace dl {
 
 constexpr int kCacheWaves = 4;        // waves of a workgroup
 
-// x of lane l ^ M, within 16 lanes
-template <int M>
-__device__ __forceinline__ float lane_xor(float f) {
-  const int x = __float_as_int(f);
-  int r;
-  if constexpr (M == 1) r = __builtin_amdgcn_mov_dpp(x, 0xB1, 0xf, 0xf, true);        // quad_perm 1, 0, 3, 2
-  else if constexpr (M == 2) r = __builtin_amdgcn_mov_dpp(x, 0x4E, 0xf, 0xf, true);   // quad_perm 2, 3, 0, 1
-  else if constexpr (M == 4) r = __builtin_amdgcn_mov_dpp(__builtin_amdgcn_mov_dpp(x, 0x141, 0xf, 0xf, true), 0x1B, 0xf, 0xf, true);   // mirrored in 8 lanes, then in 4
-  else r = __builtin_amdgcn_mov_dpp(x, 0x128, 0xf, 0xf, true);                        // rotated by 8 of 16
-  return __int_as_float(r);
-}
 // the largest over the LPR lanes of a vector, in every lane of it
 template <int LPR>
 __device__ __forceinline__ float vector_max(float x) {
@@ -53,8 +43,6 @@ __global__ __launch_bounds__(64 * kCacheWaves) void append_kernel(const AppendAr
   constexpr int LPR = DH / 8, RPW = 64 / LPR;
   __shared__ float angle[kCacheWaves][2][DH / 2];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lr = lane % LPR, row = lane / LPR;
-  float* cs = angle[wave][0];
-  float* sn = angle[wave][1];
   const double theta = lane < DH / 2 ? exp2(-2.0 * (double)lane / (double)DH * a.log2_base) : 0.0;
 
   const int64_t tasks = a.tokens * a.parts, stride = (int64_t)gridDim.x * kCacheWaves;
@@ -67,16 +55,25 @@ __global__ __launch_bounds__(64 * kCacheWaves) void append_kernel(const AppendAr
     const int64_t p = row_start(a.start, b) + t;
     const int page = valid ? page_of(a.cache, b, p) : -1;
     const int g0 = part * a.per_part, g1 = min(g0 + a.per_part, a.first[3]);
+    float cs[8] = {}, sn[8] = {};
     if (valid && a.layout >= 0 && g0 < a.first[2]) {
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // the lanes are done with the angles of the token before
       if (lane < DH / 2) {
         double s, c;
         sincos((double)p * theta, &s, &c);
-        cs[lane] = (float)c;
-        sn[lane] = (float)s;
+        angle[wave][0][lane] = (float)c;
+        angle[wave][1][lane] = (float)s;
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
+      // y[e] = x[e] cs[e] + partner[e] sn[e], with the sign of the rotation in sn
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int i = a.layout == 0 ? (lr * 8 + e) & (DH / 2 - 1) : lr * 4 + (e >> 1);
+        const bool minus = a.layout == 0 ? lr < LPR / 2 : !(e & 1);
+        cs[e] = angle[wave][0][i];
+        sn[e] = minus ? -angle[wave][1][i] : angle[wave][1][i];
+      }
     }
     for (int gi = g0; gi < g1; ++gi) {
       const int w = gi >= a.first[2] ? 2 : gi >= a.first[1] ? 1 : 0;
@@ -98,17 +95,9 @@ __global__ __launch_bounds__(64 * kCacheWaves) void append_kernel(const AppendAr
 #pragma clang fp contract(off)
         float z[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) z[e] = y[e];
-        const bool second = lr >= LPR / 2;
+        for (int e = 0; e < 8; ++e) z[e] = (a.layout == 0 ? lane_xor<LPR / 2>(y[e]) : y[e ^ 1]) * sn[e];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int i = a.layout == 0 ? (lr * 8 + e) & (DH / 2 - 1) : lr * 4 + (e >> 1);
-          const float c = cs[i], s = sn[i];
-          const float other = a.layout == 0 ? lane_xor<LPR / 2>(z[e]) : z[e ^ 1];
-          const bool minus = a.layout == 0 ? !second : !(e & 1);
-          const float u = z[e] * c, v = other * s;
-          y[e] = minus ? u - v : u + v;
-        }
+        for (int e = 0; e < 8; ++e) y[e] = y[e] * cs[e] + z[e];
       }
       if (w == 0) {
         *reinterpret_cast<bf16x8*>(a.q_out + at) = pack8(y);

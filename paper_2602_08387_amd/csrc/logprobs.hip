@@ -16,11 +16,13 @@
 // Few rows are cut into parts, joined by a second kernel.
 #include "common.h"
 #include "kernels.h"
+#include "lane_exchange.h"
 
 namespace dl {
 
 constexpr int kLpThreads = 256, kLpWaves = kLpThreads / 64, kLpUnroll = 4;
-constexpr int kLpBuffer = 64 + 512;      // candidates of a wave: those left from before, and a whole vector from every lane
+constexpr int kLpBuffer = 64 + 512;      // candidates of a wave: those that wait, and a whole vector from every lane
+constexpr int kLpSingly = 24;           // candidates that go into the list one by one (11 instructions each; sorting 64 takes some 300)
 constexpr float kLpLn2 = 0.6931471805599453f;
 
 struct LogprobsArgs {
@@ -52,33 +54,33 @@ __device__ __forceinline__ float key_logit(uint64_t key) {
   return __uint_as_float((uint32_t)(uint16_t)(order >= 0 ? order : -32768 - order) << 16);
 }
 __device__ __forceinline__ uint64_t max64(uint64_t a, uint64_t b) { return a > b ? a : b; }
-__device__ __forceinline__ uint64_t min64(uint64_t a, uint64_t b) { return a > b ? b : a; }
 
-// The last steps of a bitonic sort: a bitonic sequence over the 64 lanes into descending order.
-__device__ __forceinline__ uint64_t merge_descending(uint64_t k, int lane) {
-#pragma unroll
-  for (int j = 32; j > 0; j >>= 1) {
-    const uint64_t o = __shfl_xor(k, j, 64);
-    k = (lane & j) ? min64(k, o) : max64(k, o);
-  }
+// One step of a bitonic sort: of lanes l and l ^ J the larger in the lane without J's bit; turned round where `turned`.
+template <int J, typename T>
+__device__ __forceinline__ T sort_step(T k, int lane, bool turned) {
+  const T o = lane_xor<J>(k);
+  return (o > k) == (((lane & J) != 0) != turned) ? k : o;
+}
+// A bitonic sequence over N lanes into order.
+template <int N, typename T>
+__device__ __forceinline__ T merge_step(T k, int lane, bool turned) {
+  k = sort_step<N / 2>(k, lane, turned);
+  if constexpr (N > 2) k = merge_step<N / 2>(k, lane, turned);
   return k;
 }
 // 64 lanes into descending order: keys, or floats that are not NaN.
 template <typename T>
 __device__ __forceinline__ T sort_descending(T k, int lane) {
-#pragma unroll
-  for (int n = 2; n <= 64; n <<= 1)
-#pragma unroll
-    for (int j = n >> 1; j > 0; j >>= 1) {
-      const T o = __shfl_xor(k, j, 64);
-      const bool low = ((lane & j) != 0) != ((lane & n) != 0);     // a run in which n is set ascends
-      k = (o > k) == low ? k : o;
-    }
-  return k;
+  k = merge_step<2>(k, lane, (lane & 2) != 0);
+  k = merge_step<4>(k, lane, (lane & 4) != 0);
+  k = merge_step<8>(k, lane, (lane & 8) != 0);
+  k = merge_step<16>(k, lane, (lane & 16) != 0);
+  k = merge_step<32>(k, lane, (lane & 32) != 0);
+  return merge_step<64>(k, lane, false);
 }
 // The 64 largest of two descending sequences, descending.
 __device__ __forceinline__ uint64_t join_descending(uint64_t a, uint64_t b, int lane) {
-  return merge_descending(max64(a, __shfl(b, 63 - lane, 64)), lane);
+  return merge_step<64>(max64(a, __shfl(b, 63 - lane, 64)), lane, false);
 }
 
 struct Sums { float m, s, u; };          // maximum of x, S and U relative to it; m = -inf: nothing but -inf so far
@@ -118,35 +120,60 @@ __device__ __forceinline__ void finish_uncounted(const LogprobsArgs& a, int64_t 
   }
 }
 
+// A float that is not NaN as a whole number of the same order, and back.
+__device__ __forceinline__ int ordered(float x) { const int i = (int)__float_as_uint(x); return i ^ ((i >> 31) & 0x7fffffff); }
+__device__ __forceinline__ float from_ordered(int i) { return __uint_as_float((uint32_t)(i ^ ((i >> 31) & 0x7fffffff))); }
+
 // A wave's list of the likeliest, with the buffer in front of it.
 struct TopList {
-  uint64_t list;                         // descending over the lanes
+  uint64_t list = 0;                     // descending over the lanes
   uint64_t* buffer;
-  int held;                              // in the buffer
-  float threshold;                       // of x: what is not above it cannot enter (once the list is full)
-  bool full;
+  int held = 0;                          // in the buffer
+  bool full = false;                     // whether the list has n
+  float last = -INFINITY;                // its n-th
+  float least = -INFINITY;               // what an element has to be to enter
 
-  __device__ __forceinline__ void drain(int lane, int n_top) {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    for (int i = 0; i < held; i += 64) list = join_descending(list, sort_descending(i + lane < held ? buffer[i + lane] : 0, lane), lane);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    held = 0;
-    const uint64_t last = __shfl(list, n_top - 1, 64);
-    full = last != 0;
-    threshold = full ? key_logit(last) : -INFINITY;
-  }
-  __device__ __forceinline__ bool passes(float x) const { return full ? x > threshold : x >= threshold; }
+  // An element equal to the list's n-th comes behind it, since a wave's indices ascend.  bound: n elements of the row's part are not below it; one that is equal may
+  // be among them.
+  __device__ __forceinline__ void raise(float bound) { least = full ? fmaxf(bound, from_ordered(ordered(last) + 1)) : bound; }
   __device__ __forceinline__ void push(bool take, uint32_t bits, int index, int lane) {
     const uint64_t who = __builtin_amdgcn_ballot_w64(take);
     if (who == 0) return;
     if (take) buffer[held + __popcll(who & ((1ull << lane) - 1))] = key_of(bits, index);
     held += __popcll(who);
   }
+  __device__ __forceinline__ void drain(int lane, int n_top) {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll 1
+    for (int i = 0; i < held; i += 64) {
+      const int n = min(held - i, 64);
+      const uint64_t key = lane < n ? buffer[i + lane] : 0;
+      if (n > kLpSingly) {
+        list = join_descending(list, sort_descending(key, lane), lane);
+      } else {
+        // one after the other: the smaller ones move up a lane, the key takes the place of the first of them
+        for (int k = 0; k < n; ++k) {
+          const uint64_t one = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(key >> 32), k) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)key, k);
+          const uint64_t up = (uint64_t)(uint32_t)__builtin_amdgcn_update_dpp(0, (int)(list >> 32), 0x138, 0xf, 0xf, false) << 32 |
+                              (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)list, 0x138, 0xf, 0xf, false);
+          const uint64_t above = __builtin_amdgcn_ballot_w64(list > one);
+          list = list > one ? list : lane == __popcll(above) ? one : up;
+        }
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    held = 0;
+    const uint64_t nth = __shfl(list, n_top - 1, 64);
+    full = nth != 0;
+    if (full) last = key_logit(nth);
+  }
 };
 
 template <bool TOP>
-__global__ __launch_bounds__(kLpThreads) void logprobs_kernel(const LogprobsArgs a) {
+__global__ __launch_bounds__(kLpThreads, 6) void logprobs_kernel(const LogprobsArgs a) {
   __shared__ float red[kLpWaves][4];
+  __shared__ int bound, quarter[kLpWaves];   // the largest of the waves' n-th, and the (n / 4)-th of each
+  __shared__ float maxima[TOP ? kLpWaves : 1][64];
   __shared__ uint64_t lists[TOP ? kLpWaves : 1][64];
   __shared__ uint64_t buffer[TOP ? kLpWaves : 1][TOP ? kLpBuffer : 1];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -161,8 +188,16 @@ __global__ __launch_bounds__(kLpThreads) void logprobs_kernel(const LogprobsArgs
   const int first = part * a.per_part, end = min(vectors, first + a.per_part);
 
   Sums v{-INFINITY, 0.f, 0.f};
-  TopList top{0, buffer[TOP ? wave : 0], 0, -INFINITY, false};
+  TopList top;
+  top.buffer = buffer[TOP ? wave : 0];
   bool begun = false;
+  const int few = a.n_top >> 1;             // candidates that wait for others
+  const bool all_begin = first + (kLpWaves - 1) * 64 < end;
+  if constexpr (TOP) {
+    if (threadIdx.x == 0) bound = ordered(-INFINITY);
+    if (threadIdx.x < kLpWaves) quarter[threadIdx.x] = ordered(-INFINITY);
+    __syncthreads();
+  }
 
   for (int c0 = first + wave * 64; c0 < end; c0 += kLpThreads * kLpUnroll) {
     u32x4 w[kLpUnroll];
@@ -197,23 +232,50 @@ __global__ __launch_bounds__(kLpThreads) void logprobs_kernel(const LogprobsArgs
         v.u = __builtin_fmaf(p, fmaxf(t, -1e4f), v.u);           // t may be -inf where p is 0
       }
     if constexpr (TOP) {
-      // Until the list is full its threshold is a bound that may be met: the n-th largest of the lanes' largest of the first batch, then nothing.  From then on
-      // an element equal to the list's n-th comes behind it, since a wave's indices ascend from vector to vector.
-      if (!begun) top.threshold = __shfl(sort_descending(mx, lane), a.n_top - 1, 64);
-      begun = true;
-      if (__builtin_amdgcn_ballot_w64(top.passes(mx))) {
+      // the first bound: the n-th largest of the threads' largest, or, of a part too short for all waves, of the wave's lanes'.  A wave's bounds hold for all
+      if (!begun) {
+        float largest = sort_descending(mx, lane);
+        if (all_begin) {
+          maxima[wave][lane] = largest;
+          __syncthreads();
 #pragma unroll
-        for (int i = 0; i < kLpUnroll; ++i) {
-          if (!__builtin_amdgcn_ballot_w64(top.passes(vmax[i]))) continue;
-          const int index = (c0 + i * kLpThreads + lane) * 8, left = c0 + i * kLpThreads + lane < end ? a.V - index : 0;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const uint32_t bits = (w[i][e >> 1] >> ((e & 1) * 16)) & 0xffffu;
-            top.push(e < left && top.passes(__uint_as_float(bits << 16)), bits, index + e, lane);
-          }
-          if (top.held > 64) top.drain(lane, a.n_top);
+          for (int i = 1; i < kLpWaves; ++i) largest = merge_step<64>(fmaxf(largest, maxima[(wave + i) % kLpWaves][63 - lane]), lane, false);
         }
-        if (!top.full) top.drain(lane, a.n_top);
+        const float nth = __shfl(largest, a.n_top - 1, 64);
+        if (lane == 0) __hip_atomic_fetch_max(&bound, ordered(nth), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        begun = true;
+      }
+      // n elements are not below what one wave has as its n-th, nor below the least of what the four have as their (n / 4)-th
+      int known = __hip_atomic_load(&quarter[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+#pragma unroll
+      for (int i = 1; i < kLpWaves; ++i) known = min(known, __hip_atomic_load(&quarter[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP));
+      top.raise(from_ordered(max(known, __hip_atomic_load(&bound, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP))));
+      if (__builtin_amdgcn_ballot_w64(mx >= top.least)) {
+        static_assert(kLpUnroll == 4, "vectors in turn");
+        u32x4 x = w[0], x1 = w[1], x2 = w[2], x3 = w[3];
+        float m0 = vmax[0], m1 = vmax[1], m2 = vmax[2], m3 = vmax[3];
+#pragma unroll 1
+        for (int c = c0 + lane; c < c0 + lane + kLpUnroll * kLpThreads; c += kLpThreads) {       // a loop: one copy of the code
+          if (__builtin_amdgcn_ballot_w64(m0 >= top.least)) {
+            const int left = c < end ? a.V - c * 8 : 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const uint32_t bits = (x[e >> 1] >> ((e & 1) * 16)) & 0xffffu;
+              top.push(__uint_as_float(bits << 16) >= top.least && e < left, bits, c * 8 + e, lane);
+            }
+            if (top.held > few) {
+              top.drain(lane, a.n_top);
+              const uint64_t part = __shfl(top.list, (a.n_top - 1) / kLpWaves, 64);
+              if (part != 0 && lane == 0) __hip_atomic_store(&quarter[wave], ordered(key_logit(part)), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+              if (top.full) {
+                top.raise(top.least);
+                if (lane == 0) __hip_atomic_fetch_max(&bound, ordered(top.last), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+              }
+            }
+          }
+          x = x1; x1 = x2; x2 = x3;
+          m0 = m1; m1 = m2; m2 = m3;
+        }
       }
     }
   }
@@ -254,43 +316,54 @@ __global__ __launch_bounds__(kLpThreads) void logprobs_kernel(const LogprobsArgs
   }
 }
 
-// Joins the parts of a row: a workgroup a row, its waves taking turns with the lists.
+// Joins the parts of a row: a workgroup a row, whose waves take some lists each and then halve their number.
+constexpr int kLpJoinWaves = 16;
 template <bool TOP>
-__global__ __launch_bounds__(kLpThreads) void logprobs_join_kernel(const LogprobsArgs a) {
-  __shared__ uint64_t lists[TOP ? kLpWaves : 1][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+__global__ __launch_bounds__(64 * kLpJoinWaves) void logprobs_join_kernel(const LogprobsArgs a) {
+  __shared__ uint64_t lists[TOP ? kLpJoinWaves / 2 : 1][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
   const int64_t row = blockIdx.x;
   if (!row_counts(a, row)) {
     finish_uncounted(a, row);
     return;
   }
+  Sums sum{-INFINITY, 0.f, 0.f};
+  if (wave == 0) {
+    const f32x4* parts = reinterpret_cast<const f32x4*>(a.part_sums) + row * a.parts;
+    float m = -INFINITY;
+    for (int i = lane; i < a.parts; i += 64) m = fmaxf(m, parts[i][0]);
+    sum.m = wave_max(m);
+    for (int i = lane; i < a.parts; i += 64) {
+      const Sums p = relative_to(Sums{parts[i][0], parts[i][1], parts[i][2]}, sum.m, a.inverse_log2e);
+      sum.s += p.s;
+      sum.u += p.u;
+    }
+    sum.s = wave_sum(sum.s);
+    sum.u = wave_sum(sum.u);
+  }
   uint64_t list = 0;
   if constexpr (TOP) {
-    for (int i = wave; i < a.parts; i += kLpWaves)
-      list = join_descending(list, lane < a.n_top ? a.part_top[(row * a.parts + i) * a.n_top + lane] : 0, lane);
-    lists[wave][lane] = list;
-    __syncthreads();
-  }
-  if (wave != 0) return;
-  if constexpr (TOP)
+    const uint64_t* from = a.part_top + row * a.parts * a.n_top + lane;
+    for (int i0 = wave; i0 < a.parts; i0 += 4 * waves) {
+      uint64_t some[4];
 #pragma unroll
-    for (int i = 1; i < kLpWaves; ++i) list = join_descending(list, lists[i][lane], lane);
-  Sums mine{-INFINITY, 0.f, 0.f};
-  float m = -INFINITY;
-  const float* parts = a.part_sums + row * a.parts * 4;
-  for (int i = lane; i < a.parts; i += 64) m = fmaxf(m, parts[i * 4]);
-  m = wave_max(m);
-  for (int i = lane; i < a.parts; i += 64) {
-    const Sums o{parts[i * 4], parts[i * 4 + 1], parts[i * 4 + 2]}, p = relative_to(o, m, a.inverse_log2e);
-    mine.s += p.s;
-    mine.u += p.u;
+      for (int k = 0; k < 4; ++k) some[k] = lane < a.n_top && i0 + k * waves < a.parts ? from[(int64_t)(i0 + k * waves) * a.n_top] : 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) list = join_descending(list, some[k], lane);
+    }
+    for (int half = waves / 2; half > 0; half /= 2) {
+      if (wave >= half && wave < 2 * half) lists[wave - half][lane] = list;
+      __syncthreads();
+      if (wave < half) list = join_descending(list, lists[wave][lane], lane);
+      __syncthreads();
+    }
   }
-  finish_row(a, row, Sums{m, wave_sum(mine.s), wave_sum(mine.u)}, list, lane);
+  if (wave == 0) finish_row(a, row, sum, list, lane);
 }
 
-// Parts of a row: where there are fewer rows than fill the chip, of no fewer than two vectors a thread.
+// Parts of a row: where there are fewer rows than fill the chip, of no less than a vector a thread.
 constexpr int64_t kLpWorkgroups = 1024;
-static int64_t lp_most_parts(int64_t V) { return (V + 16 * kLpThreads - 1) / (16 * kLpThreads); }
+static int64_t lp_most_parts(int64_t V) { return (V + 8 * kLpThreads - 1) / (8 * kLpThreads); }
 
 // sums and lists of the parts; rows * parts is within kLpWorkgroups wherever there are parts
 static int64_t lp_parts_held(int64_t T, int64_t V) {
@@ -322,8 +395,9 @@ int launch_token_logprobs_fwd(const LogprobsCall& c, int n_top, float* logprobs,
   else hipLaunchKernelGGL((logprobs_kernel<false>), grid, block, 0, st, a);
   if (int rc = check_launch("token_logprobs_forward")) return rc;
   if (a.parts == 1) return 0;
-  if (n_top) hipLaunchKernelGGL((logprobs_join_kernel<true>), dim3((unsigned)c.T), block, 0, st, a);
-  else hipLaunchKernelGGL((logprobs_join_kernel<false>), dim3((unsigned)c.T), block, 0, st, a);
+  const dim3 joining(!n_top ? 64 : a.parts > 16 ? 64 * kLpJoinWaves : 256);
+  if (n_top) hipLaunchKernelGGL((logprobs_join_kernel<true>), dim3((unsigned)c.T), joining, 0, st, a);
+  else hipLaunchKernelGGL((logprobs_join_kernel<false>), dim3((unsigned)c.T), joining, 0, st, a);
   return check_launch("token_logprobs_forward, joining parts");
 }
 

@@ -687,7 +687,7 @@ __global__ __launch_bounds__(256, NR == 1 ? 2 : 1) void rows_kernel(const Attend
 template <int DH>
 __global__ __launch_bounds__(1024) void combine_kernel(const AttendArgs a, int64_t rows, int rows_per_tile, int side) {
   constexpr int LPR = DH / 4;
-  __shared__ float stats[1024 / LPR][2];
+  __shared__ float stats[1024 / LPR][2], scaled[1024 / LPR];
   __shared__ f32x4 sums[1024];
   const PagedCache& c = a.cache;
   const int group = threadIdx.x / LPR, lane = threadIdx.x % LPR, here = blockDim.x / LPR;
@@ -729,22 +729,26 @@ __global__ __launch_bounds__(1024) void combine_kernel(const AttendArgs a, int64
     }
   }
   if (side > 1) {
+    const int own = group - group % side;              // of the row's groups the first
     if (lane == 0) { stats[group][0] = m; stats[group][1] = sum; }
-    sums[threadIdx.x] = acc;
     __syncthreads();
-    if (group % side) return;
-    for (int k = 1; k < side; ++k) m = stats[group + k][1] == 0.f ? m : fmaxf(m, stats[group + k][0]);
-    const float w0 = sum == 0.f ? 0.f : fast_exp2(stats[group][0] - m);
-    sum = sum == 0.f ? 0.f : sum * w0;
+    float top = kNoKey;
+    for (int k = 0; k < side; ++k) top = stats[own + k][1] == 0.f ? top : fmaxf(top, stats[own + k][0]);
+    const float w = sum == 0.f ? 0.f : fast_exp2(m - top);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) acc[e] = w0 == 0.f ? 0.f : acc[e] * w0;
+    for (int e = 0; e < 4; ++e) acc[e] = sum == 0.f ? 0.f : acc[e] * w;
+    sums[threadIdx.x] = acc;
+    if (lane == 0) scaled[group] = sum == 0.f ? 0.f : sum * w;
+    __syncthreads();
+    if (group != own) return;
+    m = top;
+    sum = scaled[own];
+#pragma unroll 8
     for (int k = 1; k < side; ++k) {
-      if (stats[group + k][1] == 0.f) continue;
-      const float w = fast_exp2(stats[group + k][0] - m);
-      sum += w * stats[group + k][1];
+      sum += scaled[own + k];
       const f32x4 x = sums[threadIdx.x + k * LPR];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[e] += w * x[e];
+      for (int e = 0; e < 4; ++e) acc[e] += x[e];
     }
   }
   if (i >= rows) return;
@@ -758,37 +762,39 @@ __global__ __launch_bounds__(1024) void combine_kernel(const AttendArgs a, int64
 }
 
 // Which way a call goes: rows of a workgroup (16 or 32: rows_kernel; 128: tile_kernel), tiles of a pair's rows, and parts of a tile's keys.  Up to 32 rows the cache's bytes
-// are what counts and rows_kernel is as fast as they come; tile_kernel's matrix products of 32 rows a wave are for more.
+// are what counts and rows_kernel is as fast as they come; tile_kernel's matrix products of 32 rows a wave are for more.  As many parts as fill the chip once: of rows_kernel
+// the workgroups whose tiles the LDS holds (more of them, shorter, take longer: 8 rows over 16000 bf16 tokens 139 us in 4096 workgroups, 99 in 512),
+// of tile_kernel two a compute unit; none shorter than kKeysLeast, and one only where there is no more than twice that, which a second launch would cost more than it saves.
 struct AttendPlan { int rows, tiles, splits, least; int64_t pairs; };
-constexpr int64_t kRowsWanted = 4096 * 16, kTilesWanted = 512;       // workgroups times rows of rows_kernel; workgroups of tile_kernel
-constexpr int64_t kKeysLeast = 256;                                  // of a part
-static int64_t most_splits(int64_t max_tokens) { return (max_tokens + kKeysLeast - 1) / kKeysLeast; }
-static AttendPlan attend_plan(int64_t batch, int64_t seq, int64_t Hkv, int64_t group, int64_t max_tokens) {
+constexpr int64_t kUnits = 256, kKeysLeast = 256;
+static int64_t most_splits(int64_t max_tokens) { return max_tokens <= 2 * kKeysLeast ? 1 : (max_tokens + kKeysLeast - 1) / kKeysLeast; }
+static int rows_lds(int64_t dh, bool e4m3) { return 4 * 2 * (2 * 32 * (int)dh * (e4m3 ? 1 : 2) + (e4m3 ? 64 : 0)); }
+static AttendPlan attend_plan(int64_t batch, int64_t seq, int64_t Hkv, int64_t group, int64_t dh, bool e4m3, int64_t max_tokens) {
   AttendPlan p;
-  const int64_t rows = seq * group;
+  const int64_t rows = seq * group, fit = 160 * 1024 / rows_lds(dh, e4m3);
   p.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : kTileRows;
   p.pairs = batch * Hkv;
   p.tiles = (int)((rows + p.rows - 1) / p.rows);
-  const int64_t wanted = (p.rows == kTileRows ? kTilesWanted : kRowsWanted / p.rows) / (p.pairs * p.tiles), most = most_splits(max_tokens);
+  const int64_t wanted = kUnits * (p.rows == kTileRows || fit > 2 ? 2 : fit) / (p.pairs * p.tiles), most = most_splits(max_tokens);
   p.splits = (int)(wanted < 1 ? 1 : wanted < most ? wanted : most);
   p.least = (int)(kKeysLeast / 32);
   return p;
 }
 
-// Sums and statistics of the parts: pairs * tiles * splits * rows is within kRowsWanted wherever there is a split, and within pairs * (rows, filled up) * most_splits,
-// neither of which falls as the call grows.
-static int64_t rows_held(int64_t batch, int64_t seq, int64_t Hkv, int64_t group, int64_t max_tokens) {
-  const AttendPlan p = attend_plan(batch, seq, Hkv, group, max_tokens);
-  const int64_t rows = p.pairs * p.tiles, most = most_splits(max_tokens);
-  return rows < kRowsWanted && rows * p.rows < kRowsWanted && most < kRowsWanted && rows * p.rows * most < kRowsWanted ? rows * p.rows * most : kRowsWanted;
+// Sums and statistics of the parts, in rows: pairs * tiles * splits * rows of a workgroup is within 512 workgroups of rows wherever there is a split, and within pairs * (rows, filled up) *
+// most_splits, neither of which falls as the call grows.
+static int64_t rows_held(int64_t batch, int64_t seq, int64_t Hkv, int64_t group, int64_t dh, bool e4m3, int64_t max_tokens) {
+  const AttendPlan p = attend_plan(batch, seq, Hkv, group, dh, e4m3, max_tokens);
+  const int64_t rows = p.pairs * p.tiles, most = most_splits(max_tokens), bound = 2 * kUnits * p.rows;
+  return rows < bound && rows * p.rows < bound && most < bound && rows * p.rows * most < bound ? rows * p.rows * most : bound;
 }
-size_t paged_attention_workspace(int64_t batch, int64_t seq, int64_t Hq, int64_t Hkv, int64_t dh, int64_t max_tokens) {
-  return (size_t)rows_held(batch, seq, Hkv, Hq / Hkv, max_tokens) * (dh + 2) * sizeof(float);
+size_t paged_attention_workspace(int64_t batch, int64_t seq, int64_t Hq, int64_t Hkv, int64_t dh, bool e4m3, int64_t max_tokens) {
+  return (size_t)rows_held(batch, seq, Hkv, Hq / Hkv, dh, e4m3, max_tokens) * (dh + 2) * sizeof(float);
 }
 
 template <int DH, bool E4M3, int NR>
 static int launch_rows(const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
-  constexpr int tiles = 4 * 2 * (2 * HeldTile<DH, E4M3>::BYTES + (E4M3 ? 64 : 0)), results = 4 * 16 * NR * (DH + 6) * (int)sizeof(float), lds = tiles > results ? tiles : results;
+  const int tiles = rows_lds(DH, E4M3), results = 4 * 16 * NR * (DH + 6) * (int)sizeof(float), lds = tiles > results ? tiles : results;
   static std::atomic<unsigned long long> done{0};
   if (int rc = reserve_lds(rows_kernel<DH, E4M3, NR>, lds, done, "paged_attention_forward")) return rc;
   hipLaunchKernelGGL((rows_kernel<DH, E4M3, NR>), dim3((unsigned)(p.pairs * p.tiles * p.splits)), dim3(256), lds, st, a);
@@ -819,7 +825,7 @@ static int launch_attend(const AttendArgs& a, const AttendPlan& p, hipStream_t s
 int launch_paged_attention(const CacheCall& c, const void* q, int64_t seq, int64_t Hq, float scale, void* o, float* lse, void* workspace,
                            hipStream_t st) {
   const int64_t group = Hq / c.heads, max_tokens = c.columns * c.page_size;
-  const AttendPlan p = attend_plan(c.batch, seq, c.heads, group, max_tokens);
+  const AttendPlan p = attend_plan(c.batch, seq, c.heads, group, c.dh, c.e4m3, max_tokens);
   AttendArgs a{};
   a.cache = paged_cache(c);
   a.q = (const bf16_t*)q;
@@ -827,7 +833,7 @@ int launch_paged_attention(const CacheCall& c, const void* q, int64_t seq, int64
   a.o = (bf16_t*)o;
   a.lse = lse;
   a.sums = (float*)workspace;
-  a.stats = a.sums + rows_held(c.batch, seq, c.heads, group, max_tokens) * c.dh;
+  a.stats = a.sums + rows_held(c.batch, seq, c.heads, group, c.dh, c.e4m3, max_tokens) * c.dh;
   a.seq = (int)seq; a.Hq = (int)Hq; a.group = (int)group;
   a.tiles = p.tiles; a.splits = p.splits; a.least = p.least;
   a.scale_log2 = scale * kLog2e;
