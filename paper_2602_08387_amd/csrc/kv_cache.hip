@@ -7,6 +7,8 @@
 // Both move bytes and little else.  A head's vector is dh / 8 lanes of 16 bytes, so a wave holds 4 to 16 vectors and the vector's largest
 // magnitude and, for split pairs, the other member of a pair come from lane exchanges (DPP).  A wave takes a token's heads (or, of few tokens, a part
 // of them), so that its angles are evaluated once: in fp64, one pair a lane, handed on through LDS as fp32.
+#include <type_traits>
+
 #include "common.h"
 #include "kernels.h"
 #include "lane_exchange.h"
@@ -15,6 +17,7 @@
 namespace dl {
 
 constexpr int kCacheWaves = 4;        // waves of a workgroup
+constexpr int kAhead = 2;                 // groups of vectors that a wave has under way
 
 // the largest over the LPR lanes of a vector, in every lane of it
 template <int LPR>
@@ -75,54 +78,68 @@ __global__ __launch_bounds__(64 * kCacheWaves) void append_kernel(const AppendAr
         sn[e] = minus ? -angle[wave][1][i] : angle[wave][1][i];
       }
     }
-    for (int gi = g0; gi < g1; ++gi) {
-      const int w = gi >= a.first[2] ? 2 : gi >= a.first[1] ? 1 : 0;
-      const int head = (gi - a.first[w]) * RPW + row, nh = a.heads[w];
-      if (head >= nh) continue;
-      const int64_t at = (tok * nh + head) * DH + lr * 8;
-      if (!valid) {
-        const bf16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
-        if (w == 0) *reinterpret_cast<bf16x8*>(a.q_out + at) = zero;
-        continue;
-      }
-      if (w > 0 && page < 0) continue;
-      bf16x8 xv = *reinterpret_cast<const bf16x8*>(a.x[w] + at);
-      float y[8];
-      unpack8(xv, y);
-      if (w < 2 && a.layout >= 0) {
-        // each product rounded on its own: a fused multiply-add would round the two members of a pair differently, and the largest magnitude of
-        // a vector decides its exponent
+    // the groups of q (W 0), k and v, some of which are under way together
+    const auto vectors = [&](auto WHICH, const bf16_t* x, int nh, int first, int last) {
+      constexpr int W = decltype(WHICH)::value;
+      for (int gi = max(g0, first); gi < min(g1, last); gi += kAhead) {
+        bf16x8 xv[kAhead];
+        int head[kAhead];
+        int64_t at[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+          head[i] = (gi + i - first) * RPW + row;
+          at[i] = (tok * nh + head[i]) * DH + lr * 8;
+          if (gi + i < min(g1, last) && head[i] < nh && valid && (W == 0 || page >= 0)) xv[i] = *reinterpret_cast<const bf16x8*>(x + at[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+          if (gi + i >= min(g1, last) || head[i] >= nh) continue;
+          if (!valid || (W > 0 && page < 0)) {
+            const bf16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
+            if (W == 0) *reinterpret_cast<bf16x8*>(a.q_out + at[i]) = zero;
+            continue;
+          }
+          float y[8];
+          unpack8(xv[i], y);
+          if (W < 2 && a.layout >= 0) {
+            // each product rounded on its own: a fused multiply-add would round the two members of a pair differently, and the largest magnitude of
+            // a vector decides its exponent
 #pragma clang fp contract(off)
-        float z[8];
+            float z[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) z[e] = (a.layout == 0 ? lane_xor<LPR / 2>(y[e]) : y[e ^ 1]) * sn[e];
+            for (int e = 0; e < 8; ++e) z[e] = (a.layout == 0 ? lane_xor<LPR / 2>(y[e]) : y[e ^ 1]) * sn[e];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = y[e] * cs[e] + z[e];
+            for (int e = 0; e < 8; ++e) y[e] = y[e] * cs[e] + z[e];
+          }
+          if constexpr (W == 0) {
+            *reinterpret_cast<bf16x8*>(a.q_out + at[i]) = pack8(y);
+          } else {
+            const int64_t vec = vector_of(a.cache, page, head[i], p);
+            char* out = a.cache.x[W - 1];
+            if constexpr (!E4M3) {
+              *reinterpret_cast<bf16x8*>(out + vec * DH * 2 + lr * 16) = pack8(y);
+            } else {
+              float amax = 0.f;
+#pragma unroll
+              for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(y[e]) < INFINITY ? fabsf(y[e]) : 0.f);
+              const int ex = e4m3_exponent(vector_max<LPR>(amax));
+              const float inv = power_of_two(-ex);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) y[e] *= inv;
+              if (ex >= kScaleMost)          // 256 * 2^120 is above the range of bf16
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] = fabsf(y[e]) < INFINITY ? fminf(fmaxf(y[e], -240.f), 240.f) : y[e];
+              const u32x2 u = {pack_e4m3(y[0], y[1], y[2], y[3]), pack_e4m3(y[4], y[5], y[6], y[7])};
+              *reinterpret_cast<u32x2*>(out + vec * DH + lr * 8) = u;
+              if (lr == 0) a.cache.scale[W - 1][vec] = (uint8_t)(ex + kScaleBias);
+            }
+          }
+        }
       }
-      if (w == 0) {
-        *reinterpret_cast<bf16x8*>(a.q_out + at) = pack8(y);
-        continue;
-      }
-      const int64_t vec = vector_of(a.cache, page, head, p);
-      char* out = w == 1 ? a.cache.x[0] : a.cache.x[1];
-      if constexpr (!E4M3) {
-        *reinterpret_cast<bf16x8*>(out + vec * DH * 2 + lr * 16) = pack8(y);
-      } else {
-        float amax = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(y[e]) < INFINITY ? fabsf(y[e]) : 0.f);
-        const int ex = e4m3_exponent(vector_max<LPR>(amax));
-        const float inv = power_of_two(-ex);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] *= inv;
-        if (ex >= kScaleMost)          // 256 * 2^120 is above the range of bf16
-#pragma unroll
-          for (int e = 0; e < 8; ++e) y[e] = fabsf(y[e]) < INFINITY ? fminf(fmaxf(y[e], -240.f), 240.f) : y[e];
-        const u32x2 u = {pack_e4m3(y[0], y[1], y[2], y[3]), pack_e4m3(y[4], y[5], y[6], y[7])};
-        *reinterpret_cast<u32x2*>(out + vec * DH + lr * 8) = u;
-        if (lr == 0) (w == 1 ? a.cache.scale[0] : a.cache.scale[1])[vec] = (uint8_t)(ex + kScaleBias);
-      }
-    }
+    };
+    vectors(std::integral_constant<int, 0>{}, a.x[0], a.heads[0], 0, a.first[1]);
+    vectors(std::integral_constant<int, 1>{}, a.x[1], a.heads[1], a.first[1], a.first[2]);
+    vectors(std::integral_constant<int, 2>{}, a.x[2], a.heads[1], a.first[2], a.first[3]);
   }
 }
 
