@@ -49,18 +49,37 @@ __device__ __forceinline__ int page_of_wave(const PagedCache& c, int b, int p) {
   return (uint32_t)page < (uint32_t)c.n_pages ? page : -1;
 }
 
-// Workgroup -> (place in its pair's queue, pair of batch row and KV head).  Ids go to the eight XCDs in turn, each with an L2 of its own: a pair's workgroups,
-// which share its keys, stay on one XCD where the pairs are a multiple of 8, and the pairs of a batch row, which may be much longer than another,
-// are spread over all (5 rows of 0 to 1037 tokens and 8 heads in contiguous shares: 3.8 times as long).
-__device__ __forceinline__ void work_of(int id, int pairs, int& j, int& pair) {
-  if (pairs & 7) {
-    j = id / pairs;
-    pair = id % pairs;
-  } else {
-    const int per_xcd = pairs >> 3, slot = id >> 3;
-    j = slot / per_xcd;
-    pair = (slot % per_xcd) * 8 + (id & 7);
+// Positions of a batch row that its new tokens see, all of them together: 0 .. result - 1.
+__device__ __forceinline__ int row_keys(const AttendArgs& a, int b) {
+  const int n = row_length(a.lengths, b, a.seq);
+  const int64_t end = row_start(a.start, b) + n, cap = (int64_t)a.cache.columns << a.cache.shift;
+  return n <= 0 || end <= 0 ? 0 : (int)(end < cap ? end : cap);
+}
+
+// Of up to 64 batch rows, which lie one a lane: the one with the rank-th most keys.
+__device__ __forceinline__ int row_of_rank(const AttendArgs& a, int rank, int lane) {
+  const int batch = a.cache.batch, n = lane < batch ? row_keys(a, lane) : -1;
+  int above = 0;
+  for (int j = 0; j < batch; ++j) {
+    const int other = __builtin_amdgcn_readlane(n, j);
+    above += other > n || (other == n && j < lane);
   }
+  return __builtin_ctzll(__builtin_amdgcn_ballot_w64(lane < batch && above == rank));
+}
+
+// Workgroup -> (batch row, KV head, place in their queue of workgroups).  Ids go to the eight XCDs in turn, each with an L2 of its own: where the heads are a multiple of 8
+// a head's workgroups, which share its keys, stay on one XCD, and every XCD has as much of each batch row.  A queue's places are dealt to the heads in turn, long ones
+// first.  SORTED: the rows with most keys come first, since the last workgroups to start should be short ones (5 rows of 0 to 1037 tokens behind 1600 to
+// 8000, 8 heads: 381 us, 472 in the order of the rows); worth its microsecond where workgroups are long and of different length.
+struct Work { int b, hk, j; };
+template <bool SORTED>
+__device__ __forceinline__ Work work_of(const AttendArgs& a, int id, int queue, int lane) {
+  const PagedCache& c = a.cache;
+  const bool pinned = (c.heads & 7) == 0;
+  const int heads = pinned ? c.heads >> 3 : c.heads, slot = pinned ? id >> 3 : id;       // heads that take turns
+  const int rank = slot / (queue * heads), left = slot % (queue * heads);
+  const int hk = pinned ? (left % heads) * 8 + (id & 7) : left % heads;
+  return {SORTED && c.batch > 1 && c.batch <= 64 ? __builtin_amdgcn_readfirstlane(row_of_rank(a, rank, lane)) : rank, hk, left / heads};
 }
 
 // Memory to LDS without registers between, 16 bytes a lane: lane l's go to `to` + 16 l.  As assembly, which names no register as an output: behind the builtin the
@@ -158,10 +177,9 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttendArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const PagedCache& c = a.cache;
-  int j, pair;
-  work_of((int)blockIdx.x, c.batch * c.heads, j, pair);
-  const int b = pair / c.heads, hk = pair % c.heads;
-  const int tile = a.tiles - 1 - j / a.splits, split = j % a.splits;     // long rows (late tokens) first
+  const Work work = work_of<true>(a, (int)blockIdx.x, a.tiles * a.splits, lane);
+  const int b = work.b, hk = work.hk, pair = b * c.heads + hk;
+  const int tile = a.tiles - 1 - work.j / a.splits, split = work.j % a.splits;     // late tokens first
   const int lq = lane & 31, half = lane >> 5;
   const int n_rows = row_length(a.lengths, b, a.seq) * a.group, row0 = tile * kTileRows;
   const int r = row0 + wave * 32 + lq;
@@ -286,6 +304,8 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttendArgs a) {
       at.k += stage * STAGE;
       at.v += stage * STAGE;
       asm volatile("" : "+v"(at.k), "+v"(at.v));                 // their XORs are formed here, and take no registers across the loop
+      // the wave that has products to issue goes first, so that the other one's exponentials fall beside them and not beside its own products
+      __builtin_amdgcn_s_setprio(1);
       f32x16 s[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i)
@@ -296,6 +316,7 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttendArgs a) {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
           s[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at.key(kk, i), qf[kk], s[i], 0, 0, 0);
+      __builtin_amdgcn_s_setprio(0);
       // keys after the row's own position (only on tiles that reach past this wave's first row)
       if (kv0 + kTileKeys - 1 > lim0) mask_rows_above<2>(s, lim - kv0 - (half << 2), -INFINITY);
       if (missing) {
@@ -332,12 +353,14 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttendArgs a) {
           psum += pv;
         }
       lsum += psum;
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int ks = 0; ks < 4; ++ks) {
         const bf16x8 pf = pack_slots(s[ks >> 1], (ks & 1) * 8);
 #pragma unroll
         for (int t2 = 0; t2 < DH / 32; ++t2) oacc[t2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at.value(t2, ks), pf, oacc[t2], 0, 0, 0);
       }
+      __builtin_amdgcn_s_setprio(0);
       }
       if (t + 1 < t1) arrived(t + 1, stage ^ 1);
       __syncthreads();
@@ -438,9 +461,8 @@ __global__ __launch_bounds__(256, NR == 1 ? 2 : 1) void rows_kernel(const Attend
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const PagedCache& c = a.cache;
-  int j, pair;
-  work_of((int)blockIdx.x, c.batch * c.heads, j, pair);
-  const int b = pair / c.heads, hk = pair % c.heads, tile = a.tiles - 1 - j / a.splits, split = j % a.splits;
+  const Work work = work_of<false>(a, (int)blockIdx.x, a.tiles * a.splits, lane);
+  const int b = work.b, hk = work.hk, pair = b * c.heads + hk, tile = a.tiles - 1 - work.j / a.splits, split = work.j % a.splits;
   const int lr = lane & 15, quarter = lane >> 4;
   const int n_rows = row_length(a.lengths, b, a.seq) * a.group, row0 = tile * ROWS;
   const int64_t start = row_start(a.start, b), cap = (int64_t)c.columns << c.shift;
