@@ -376,8 +376,8 @@ int linear_attention_step(const void* q, const void* k, const void* v, const flo
  * dropped, and what is read from there is not there.  Rows may share pages that nothing is written to (a common prefix).  start and
  * lengths are those of the token mixing above: start[b] tokens of row b are in the cache before the call, its lengths[b] new ones have
  * positions start[b] ...; NULL: 0, and seq.  What a page holds behind a row's last token is never read, padding neither.
- * The cache may exceed 4 GiB.  batch, seq: any positive numbers; max_pages * page_size, seq * n_q_heads and the workgroups of a call
- * stay below 2^31.
+ * The cache may exceed 4 GiB.  batch, seq: any positive numbers; max_pages * page_size and seq * n_q_heads stay below 2^31, batch *
+ * n_kv_heads (times seq * (Hq / Hkv) / 16, rounded up) of the attention below 2^24.
  * ------------------------------------------------------------------------------------------ */
 
 #define DLAYER_CACHE_BF16 0
@@ -412,7 +412,9 @@ int kv_cache_read(const dlayer_kv_cache* cache, const int64_t* start, const int6
  *   o = sum_s exp(scale q . k_s - lse) v_s,   lse = log sum_s exp(scale q . k_s)
  * with query head h reading KV head h / (Hq / Hkv).  One new token a row (generation) or many (a prompt, or a piece of one).
  * q, o [B*S, Hq, dh] bf16, lse [B, Hq, S] f32 or NULL.  A token that sees nothing, and padding, have o = 0 and lse = -infinity.
- * scale > 0.  A value that is not finite shows in the results of those tokens that see it, and of no others.  o must not overlap q or the cache.
+ * scale > 0.  A key or value that is not finite shows in the results of those tokens that see it, and of no others.  Weights are rounded to bf16
+ * for their product with the values, sums are fp32 and divided at the end: values beyond some 1e33 may overflow in them.  o must not overlap q or
+ * the cache.
  * workspace: paged_attention_workspace_bytes(cache, seq, n_q_heads), which reads the sizes of cache only and does not fall as batch, seq
  * or max_pages grows.                                                                                        */
 size_t paged_attention_workspace_bytes(const dlayer_kv_cache* cache, int64_t seq, int64_t n_q_heads);
@@ -428,7 +430,7 @@ int paged_attention_forward(const dlayer_kv_cache* cache, const void* q, const i
  * most V) likeliest tokens, likeliest first, of equal logits the lower index first.  Any output may be NULL; top_ids and top_logprobs are where n_top is 0.
  * Sums in fp32.  Logits of -infinity have probability 0; a row of nothing else has lse and logprobs of -infinity and entropy 0.  A row
  * that holds NaN or +infinity has NaN for results; NaN are not among its top_ids (which end in -1 where others are too few).
- * T below 2^22, V and ld below 2^24.  workspace: token_logprobs_workspace_bytes(T, V, n_top), at most 528 KiB; it does not fall as T, V or n_top grows.   */
+ * T below 2^22, V and ld below 2^24 (and T * ld of the gradient below 2^37).  workspace: token_logprobs_workspace_bytes(T, V, n_top), at most 528 KiB; it does not fall as T, V or n_top grows.   */
 size_t token_logprobs_workspace_bytes(int64_t T, int64_t V, int64_t n_top);
 int token_logprobs_forward(const void* logits, const int64_t* targets, int64_t T, int64_t V, int64_t ld, float inverse_temperature,
                            int64_t n_top, float* logprobs, float* entropy, float* lse, int64_t* top_ids, float* top_logprobs,

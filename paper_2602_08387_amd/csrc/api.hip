@@ -748,6 +748,8 @@ static int cache_ok(const char* who, const dlayer_kv_cache* c, int64_t seq, bool
   if (!memory) return 0;
   REQUIRE(c->k && c->v && aligned16(c->k) && aligned16(c->v), "%s: the cache's k or v is null or not 16-byte aligned", who);
   REQUIRE(c->page_table != nullptr, "%s: page_table is null", who);
+  const uint64_t vectors = (uint64_t)c->n_pages * c->n_kv_heads * c->page_size, held = vectors * c->head_dim * (c->dtype == DLAYER_CACHE_E4M3 ? 1 : 2);
+  REQUIRE(!overlap(c->k, held, c->v, held), "%s: the cache's k and v overlap", who);
   if (c->dtype == DLAYER_CACHE_E4M3)
     REQUIRE(c->k_scale && c->v_scale && aligned16(c->k_scale) && aligned16(c->v_scale), "%s: an e4m3 cache needs k_scale and v_scale, 16-byte aligned", who);
   else
@@ -798,8 +800,10 @@ int kv_cache_read(const dlayer_kv_cache* cache, const int64_t* start, const int6
 static int paged_shape_ok(const char* who, const dlayer_kv_cache* c, int64_t seq, int64_t Hq, bool memory) {
   TRY(cache_ok(who, c, seq, memory));
   REQUIRE(Hq > 0 && Hq < 65536 && Hq % c->n_kv_heads == 0, "%s: n_q_heads must be a multiple of the cache's n_kv_heads, and below 65536", who);
-  const int64_t rows = seq * (Hq / c->n_kv_heads);
-  REQUIRE(seq * Hq < ((int64_t)1 << 31) - 256 && (int64_t)c->batch * c->n_kv_heads * ((rows + 15) / 16) < (int64_t)1 << 31, "%s: batch, seq or head count too large", who);
+  REQUIRE(seq * Hq < ((int64_t)1 << 31) - 256, "%s: seq * n_q_heads reaches 2^31", who);
+  // a launch holds fewer than 2^32 threads: 256 for 16 rows of a KV head at the least
+  const int64_t groups = (seq * (Hq / c->n_kv_heads) + 15) / 16;
+  REQUIRE((int64_t)c->batch * c->n_kv_heads < (int64_t)1 << 24 && (int64_t)c->batch * c->n_kv_heads * groups < (int64_t)1 << 24, "%s: batch, seq or head count too large", who);
   return 0;
 }
 
@@ -827,7 +831,7 @@ static int logprobs_ok(const char* who, int64_t T, int64_t V, int64_t ld) {
 }
 
 size_t token_logprobs_workspace_bytes(int64_t T, int64_t V, int64_t n_top) {
-  if (logprobs_ok("token_logprobs_workspace_bytes", T, V, (V + 7) & ~(int64_t)7) || n_top < 0 || n_top > 64 || n_top > V) return 0;
+  if (V >= (int64_t)1 << 24 || logprobs_ok("token_logprobs_workspace_bytes", T, V, (V + 7) & ~(int64_t)7) || n_top < 0 || n_top > 64 || n_top > V) return 0;
   return token_logprobs_workspace(T, V, n_top);
 }
 
@@ -851,6 +855,7 @@ int token_logprobs_backward(const void* logits, const int64_t* targets, const fl
   REQUIRE(inverse_temperature > 0.f && inverse_temperature < INFINITY, "token_logprobs_backward: inverse_temperature must be positive and finite");
   REQUIRE(lse != nullptr, "token_logprobs_backward: lse is null");
   REQUIRE(d_logprobs || d_entropy, "token_logprobs_backward: neither d_logprobs nor d_entropy is given");
+  REQUIRE(T * ((ld + 8191) / 8192) < (int64_t)1 << 24, "token_logprobs_backward: T * ld reaches 2^37");      // a launch's threads, as above
   REQUIRE(targets || !d_logprobs, "token_logprobs_backward: d_logprobs is of targets, which is null");
   REQUIRE(entropy || !d_entropy, "token_logprobs_backward: d_entropy needs the forward's entropy");
   REQUIRE(!shifted(dlogits, logits, (uint64_t)T * ld * 2), "token_logprobs_backward: dlogits must be logits or not overlap it");

@@ -30,7 +30,7 @@ def refused(K, name, *args):
 
 BAD_CACHES = [dict(n_pages=0), dict(n_kv_heads=0), dict(batch=0), dict(max_pages=0), dict(max_pages=-1), dict(head_dim=96), dict(head_dim=256), dict(page_size=8), dict(page_size=24),
               dict(page_size=8192), dict(page_size=0), dict(dtype=2), dict(dtype=-1), dict(max_pages=1 << 27), dict(k=0), dict(v=0), dict(k=(1 << 32) + 8), dict(page_table=0),
-              dict(k_scale=0), dict(v_scale=(4 << 32) + 4), dict(dtype=0)]
+              dict(v=(1 << 32) + 16), dict(k_scale=0), dict(v_scale=(4 << 32) + 4), dict(dtype=0)]
 A = [(i + 10) << 32 for i in range(8)]        # addresses far from one another and from the cache
 
 
@@ -86,6 +86,8 @@ def test_attention(K):
     call(c, A[0], None, None, S, 7, 0.1, A[1], A[3], A[2])
     call(c, A[0], None, None, S, 0, 0.1, A[1], A[3], A[2])
     call(c, A[0], None, None, 1 << 28, HQ, 0.1, A[1], A[3], A[2])
+    many = C.byref(cache(K, batch=1 << 23, max_pages=1))                      # more workgroups than a launch holds
+    call(many, A[0], None, None, 1, 4, 0.1, A[1], A[3], A[2])
     for scale in (0.0, -1.0, float("nan"), float("inf")):
         call(c, A[0], None, None, S, HQ, scale, A[1], A[3], A[2])
     assert "overlap" in call(c, A[0], None, None, S, HQ, 0.1, A[0], A[3], A[2])
@@ -109,6 +111,7 @@ def test_logprobs(K):
         bad[i] = x
         call(*bad)
     call(A[0], A[1], A[2], A[3], None, None, T, V, ld, 1.0, A[6])
+    call(A[0], A[1], A[2], A[3], A[4], A[5], (1 << 22) - 1, 40000, 40000, 1.0, A[0])
 
 
 def test_workspaces_do_not_fall(K):

@@ -237,3 +237,34 @@ def test_a_cache_of_more_than_4_gib(K):
         assert torch.equal(out[0], k) and torch.equal(out[1], v)
         assert x[0][6:n_pages - 3].view(torch.uint8).max() == 0
         del x, s, cache
+
+
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+def test_more_tokens_than_workgroups(K, e4m3):
+    """A wave takes several tokens one after the other: the same bits as token by token."""
+    b, s, hq, hkv, dh, page = 3, 3001, 3, 1, 32, 16
+    columns = -(-s // page)
+    table = torch.randperm(b * columns, device="cuda").view(b, columns).to(torch.int32)
+    lengths = [s, 0, 1777]
+    q, k, v = (torch.randn((b, s, h, dh), device="cuda").bfloat16() for h in (hq, hkv, hkv))
+    caches, outs = [], []
+    for _ in range(2):
+        x = [torch.zeros((b * columns, hkv, page, dh), dtype=torch.uint8 if e4m3 else torch.bfloat16, device="cuda") for _ in range(2)]
+        sc = [torch.zeros((b * columns, hkv, page), dtype=torch.uint8, device="cuda") if e4m3 else None for _ in range(2)]
+        caches.append(K.KVCache.of(*x, table, *sc))
+        outs.append(garbage(q.shape))
+    K.kv_cache_append(caches[0], q, k, v, None, i64(lengths), s, hq, 1e4, 1, outs[0])
+    for t0 in range(0, s, 500):
+        n = min(500, s - t0)
+        piece = [x[:, t0:t0 + n].contiguous() for x in (q, k, v)]
+        out = garbage(piece[0].shape)
+        K.kv_cache_append(caches[1], *piece, i64([t0] * b), i64([min(max(m - t0, 0), n) for m in lengths]), n, hq, 1e4, 1, out)
+        outs[1][:, t0:t0 + n] = out
+    assert torch.equal(outs[0], outs[1])
+    for x, y in zip(caches[0].tensors, caches[1].tensors):
+        assert (x is None and y is None) or torch.equal(x, y)
+    got = [garbage(k.shape) for _ in range(2)]
+    K.kv_cache_read(caches[0], None, i64(lengths), s, *got)
+    assert all((x[1] == 0).all() and (x[2, 1777:] == 0).all() for x in got)
+    if not e4m3:
+        assert torch.equal(got[1][0], v[0]) and torch.equal(got[1][2, :1777], v[2, :1777])

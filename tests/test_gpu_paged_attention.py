@@ -236,3 +236,72 @@ def test_a_cache_of_more_than_4_gib(K):
         got = run(K, K.KVCache.of(*big, table), q, [300 - s], None, 32, 0.09)
         ref = run(K, K.KVCache.of(*small, torch.arange(5, dtype=torch.int32, device="cuda")[None]), q, [300 - s], None, 32, 0.09)
         assert torch.equal(got[0], ref[0]) and torch.equal(got[1], ref[1])
+
+
+def ragged(rng, batch, longest, s, empty=True):
+    """(tokens before, new tokens) of each row, some with none."""
+    start, n = [int(x) for x in rng.integers(0, longest - s, batch)], [int(x) for x in rng.integers(0 if empty else 1, s + 1, batch)]
+    start[0], n[0], n[-1] = longest - s, s, 0 if empty else s
+    return start, n
+
+
+# batch, longest row, seq, query and KV heads, head_dim, page: more rows than are put in order, and fewer; keys cut into parts or not; 16, 32 and 128 rows to a workgroup
+RAGGED = [(70, 200, 1, 4, 2, 32, 16), (3, 3000, 2, 16, 8, 64, 16), (9, 1500, 1, 2, 1, 128, 32), (2, 5000, 3, 16, 2, 128, 128), (66, 150, 9, 4, 1, 32, 16), (5, 900, 40, 8, 8, 64, 16),
+          (2, 2600, 70, 4, 2, 128, 64), (1, 4500, 33, 4, 1, 32, 256)]
+
+
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("case", RAGGED, ids=str)
+def test_ragged_batches(K, case, e4m3):
+    batch, longest, s, hq, hkv, dh, page = case
+    rng = np.random.default_rng(batch + longest + e4m3)
+    start, n = ragged(rng, batch, longest, s, empty=batch > 1)
+    pages = Pages(rng, [a + m for a, m in zip(start, n)], hkv, dh, page, e4m3, columns=-(-longest // page) + 3)
+    qb = bits(rng, (batch, s, hq, dh), 2.0)
+    o, lse = run(K, pages.device(K), spoiled(dev_bf16(qb), n), start, n, hq, dh ** -0.5)
+    check(o, lse, og.attention(pages.oracle(), si.bf16_bits_to_f64(qb), start, n, dh ** -0.5), dh)
+
+
+@pytest.mark.parametrize("s,hq,longest", [(1, 4, 3000), (7, 4, 3000), (60, 4, 3000), (60, 16, 200)])
+def test_missing_pages_and_parts(K, s, hq, longest):
+    """Whole parts of a row's keys lie in pages that do not exist, or single pages of each."""
+    rng = np.random.default_rng(s)
+    start = [longest - s, longest - s, longest // 2]
+    pages = Pages(rng, [a + s for a in start], 2, 64, 16, s == 7)
+    pages.table[0, 10:100] = -1
+    pages.table[1, rng.integers(0, pages.table.shape[1], 60)] = 1 << 20
+    pages.table[2, :20] = -7
+    qb = bits(rng, (3, s, hq, 64), 2.0)
+    o, lse = run(K, pages.device(K), dev_bf16(qb), start, None, hq, 0.125)
+    check(o, lse, og.attention(pages.oracle(), si.bf16_bits_to_f64(qb), start, None, 0.125), 64)
+
+
+@pytest.mark.parametrize("s,group,e4m3", [(2, 8, True), (20, 1, True), (10, 3, False), (150, 1, True), (100, 8, True), (130, 2, False)])
+def test_many_values_that_are_not_finite(K, s, group, e4m3):
+    """NaN and infinities strewn over the new tokens' keys and values: every element is NaN exactly where a token sees one that it depends on."""
+    rng = np.random.default_rng(s + group)
+    hkv, dh, start = 2, 64, 40
+    pages = Pages(rng, [start + s], hkv, dh, 16, e4m3)
+    qb = bits(rng, (1, s, group * hkv, dh), 2.0)
+    clean, clean_lse = run(K, pages.device(K), dev_bf16(qb), [start], None, group * hkv, 0.125)
+    odd_v, odd_k = np.full((hkv, dh), 10 ** 9), np.full(hkv, 10 ** 9)            # the first position of each
+    for _ in range(12):
+        t, j, d, w = int(rng.integers(s)), int(rng.integers(hkv)), int(rng.integers(dh)), int(rng.integers(4) > 0)
+        p = start + t
+        pages.codes[w][pages.table[0, p // 16], j, p % 16, d] = 0x7F if e4m3 else (0x7FC0 if rng.integers(2) else 0xFF80)
+        if w:
+            odd_v[j, d] = min(odd_v[j, d], p)
+        else:
+            odd_k[j] = min(odd_k[j], p)
+    o, lse = run(K, pages.device(K), dev_bf16(qb), [start], None, group * hkv, 0.125)
+    o, clean = host_f64(o)[0], host_f64(clean)[0]
+    p = start + np.arange(s)[:, None, None]
+    # an infinite key makes a score of either sign of infinity, or NaN: with +infinity and NaN the token has no result, with -infinity the key has no weight
+    for h in range(group * hkv):
+        j = h // group
+        by_v, by_k = p[:, 0] >= odd_v[j], (p[:, 0] >= odd_k[j]) & np.ones((s, dh), bool)
+        assert np.all(~np.isfinite(o[:, h])[by_v & ~by_k])
+        untouched = ~by_v & ~by_k
+        assert np.array_equal(o[:, h][untouched], clean[:, h][untouched])
+        rows = ~by_k[:, 0]
+        assert torch.equal(lse[0, h].cpu()[rows], clean_lse[0, h].cpu()[rows])
