@@ -5,8 +5,8 @@
 // One pass over the keys with the running maximum and sum.  The query heads of a KV head's group share its keys, so a matrix product's rows are (token,
 // head of the group) pairs, row = token * group + head: the keys of a group are read once for all of them.
 //
-// tile_kernel: workgroup = 128 rows of one (batch row, KV head), four waves of 32; score tiles S^T[key][row] = K Q^T on v_mfma_f32_32x32x16_bf16, whose
-// layout is that of the next product's operand, O^T[d][row] += V^T P^T.  Tiles of 64 keys stream to LDS, double buffered; a wave loads the 16 keys of
+// tile_kernel: workgroup = 128 rows of one (batch row, KV head), four waves of 32 (or 256 rows, eight waves); score tiles S^T[key][row] = K Q^T on v_mfma_f32_32x32x16_bf16, whose
+// layout is that of the next product's operand, O^T[d][row] += V^T P^T.  Tiles of 64 (128) keys stream to LDS, double buffered; a wave loads the 16 keys of
 // its own part of the tile, which lie in one page (a page has 16 tokens or a multiple), so a tile needs one page number a wave.  Loads go to LDS
 // directly; a wave then writes its 16 keys of e4m3, in their place, as the bf16 values that they stand for.  The keys can be split over workgroups, whose sums
 // combine_kernel joins.
@@ -21,7 +21,7 @@
 namespace dl {
 
 constexpr float kNoKey = -1e30f;       // a maximum before the first key: finite, so that exp2(-inf - m) is 0 and not NaN
-constexpr int kTileRows = 128, kTileKeys = 64;
+constexpr int kSubKeys = 64;             // keys whose scores a wave has at a time
 
 struct AttendArgs {
   PagedCache cache;
@@ -125,9 +125,9 @@ __device__ __forceinline__ Keys16 keys16(const PagedCache& c, int b, int hk, int
 
 // LDS addresses of a lane's operands in a tile of RowTile's layout.  Its swizzle is an XOR of chunk numbers, so that the steps along head_dim are XORs of one address
 // and steps of 16 rows an offset: key(kk, i) of keys 32 i + lane % 32, step kk; value(t2, ks) of columns 32 t2 .., keys 16 ks .., as frag_cols.
-template <int DH>
+template <int DH, int NW>
 struct Operands {
-  using Tile = RowTile<kTileKeys, DH, 4>;
+  using Tile = RowTile<16 * NW, DH, NW>;
   uint32_t k, v;
   __device__ __forceinline__ Operands(uint32_t tiles, int lane) {
     const int row = lane & 31, grp = lane >> 4, s = lane & 15, vrow = ((grp >> 1) << 2) + (s >> 2), col = ((grp & 1) << 4) + ((s & 3) << 2);
@@ -168,9 +168,10 @@ __device__ __forceinline__ bool any_not_finite(const bf16x8& v) {
   return odd;
 }
 
-template <int DH, bool E4M3>
-__global__ __launch_bounds__(256, 2) void tile_kernel(const AttendArgs a) {
-  using Tile = RowTile<kTileKeys, DH, 4>;
+template <int DH, bool E4M3, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void tile_kernel(const AttendArgs a) {
+  constexpr int kTileRows = 32 * NW, kTileKeys = 16 * NW;
+  using Tile = RowTile<kTileKeys, DH, NW>;
   constexpr int STAGE = 2 * Tile::BYTES;
   // e4m3: a wave's 16 keys as they are held; CHUNK bytes a lane and load, LANES of them a key
   constexpr int HELD = 16 * DH, CHUNK = HELD < 1024 ? 8 : 16, NLOAD = HELD / (64 * CHUNK), LANES = DH / CHUNK, ROWS = 64 / LANES;
@@ -206,7 +207,7 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttendArgs a) {
   if (t0 < t1) {
     // pages that do not exist take their keys out of the sum: looked for once, so that no tile has to ask where all are there
     bool missing = false;
-    for (int i = (t0 * kTileKeys >> c.shift) + threadIdx.x, n = (min(end, t1 * kTileKeys) - 1) >> c.shift; i <= n; i += 256)
+    for (int i = (t0 * kTileKeys >> c.shift) + threadIdx.x, n = (min(end, t1 * kTileKeys) - 1) >> c.shift; i <= n; i += 64 * NW)
       missing |= (uint32_t)c.table[(int64_t)b * c.columns + i] >= (uint32_t)c.n_pages;
     if (threadIdx.x <= DH) first_odd[threadIdx.x] = threadIdx.x < DH ? 0x7fffffff : 0;
     missing = any_of_workgroup(missing, reinterpret_cast<int*>(smem));
@@ -291,18 +292,20 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttendArgs a) {
       }
     };
 
-    const Operands<DH> operands(lds_address(smem), lane);
+    const Operands<DH, NW> operands(lds_address(smem), lane);
     load(t0, 0);
     arrived(t0, 0);
     __syncthreads();
     int stage = 0;
     for (int t = t0; t < t1; ++t) {
       if (t + 1 < t1) load(t + 1, stage ^ 1);
-      const int kv0 = t * kTileKeys;
+#pragma unroll
+      for (int sub = 0; sub < kTileKeys / kSubKeys; ++sub) {
+      const int kv0 = t * kTileKeys + sub * kSubKeys;
       if (kv0 <= lim1) {
-      Operands<DH> at = operands;
-      at.k += stage * STAGE;
-      at.v += stage * STAGE;
+      Operands<DH, NW> at = operands;
+      at.k += stage * STAGE + sub * (kSubKeys * Tile::ROW_B);
+      at.v += stage * STAGE + sub * (kSubKeys * Tile::ROW_B);
       asm volatile("" : "+v"(at.k), "+v"(at.v));                 // their XORs are formed here, and take no registers across the loop
       // the wave that has products to issue goes first, so that the other one's exponentials fall beside them and not beside its own products
       __builtin_amdgcn_s_setprio(1);
@@ -318,7 +321,7 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttendArgs a) {
           s[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at.key(kk, i), qf[kk], s[i], 0, 0, 0);
       __builtin_amdgcn_s_setprio(0);
       // keys after the row's own position (only on tiles that reach past this wave's first row)
-      if (kv0 + kTileKeys - 1 > lim0) mask_rows_above<2>(s, lim - kv0 - (half << 2), -INFINITY);
+      if (kv0 + kSubKeys - 1 > lim0) mask_rows_above<2>(s, lim - kv0 - (half << 2), -INFINITY);
       if (missing) {
 #pragma unroll
         for (int g = 0; g < 4; ++g)
@@ -361,6 +364,7 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttendArgs a) {
         for (int t2 = 0; t2 < DH / 32; ++t2) oacc[t2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at.value(t2, ks), pf, oacc[t2], 0, 0, 0);
       }
       __builtin_amdgcn_s_setprio(0);
+      }
       }
       if (t + 1 < t1) arrived(t + 1, stage ^ 1);
       __syncthreads();
@@ -790,8 +794,9 @@ __global__ __launch_bounds__(1024) void combine_kernel(const AttendArgs a, int64
   if (a.lse && d == 0) a.lse[((int64_t)b * a.Hq + at.h) * a.seq + at.t] = sum != 0.f ? (m + log2f(sum)) * kLn2 : -INFINITY;
 }
 
-// Which way a call goes: rows of a workgroup (16 or 32: rows_kernel; 128: tile_kernel), tiles of a pair's rows, and parts of a tile's keys.  Up to 32 rows the cache's bytes
-// are what counts and rows_kernel is as fast as they come; tile_kernel's matrix products of 32 rows a wave are for more.  As many parts as fill the chip once: of rows_kernel
+// Which way a call goes: rows of a workgroup (16 or 32: rows_kernel; 128 or 256: tile_kernel), tiles of a pair's rows, and parts of a tile's keys.  Up to 32 rows the cache's bytes
+// are what counts and rows_kernel is as fast as they come; tile_kernel's matrix products of 32 rows a wave are for more.  Eight waves a workgroup make bf16 of e4m3 once for twice the rows
+// (two prompts of 8192 tokens, heads of 128: 1087 us, 1189 with four waves; bf16 itself 1102 and 1097), where that leaves every compute unit two workgroups to take.  As many parts as fill the chip once: of rows_kernel
 // the workgroups whose tiles the LDS holds (more of them, shorter, take longer: 8 rows over 16000 bf16 tokens 139 us in 4096 workgroups, 99 in 512),
 // of tile_kernel two a compute unit; none shorter than kKeysLeast, and one only where there is no more than twice that, which a second launch would cost more than it saves.
 struct AttendPlan { int rows, tiles, splits, least; int64_t pairs; };
@@ -801,10 +806,10 @@ static int rows_lds(int64_t dh, bool e4m3) { return 4 * 2 * (2 * 32 * (int)dh * 
 static AttendPlan attend_plan(int64_t batch, int64_t seq, int64_t Hkv, int64_t group, int64_t dh, bool e4m3, int64_t max_tokens) {
   AttendPlan p;
   const int64_t rows = seq * group, fit = 160 * 1024 / rows_lds(dh, e4m3);
-  p.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : kTileRows;
   p.pairs = batch * Hkv;
+  p.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : e4m3 && dh == 128 && p.pairs * ((rows + 255) / 256) >= 2 * kUnits ? 256 : 128;
   p.tiles = (int)((rows + p.rows - 1) / p.rows);
-  const int64_t wanted = kUnits * (p.rows == kTileRows || fit > 2 ? 2 : fit) / (p.pairs * p.tiles), most = most_splits(max_tokens);
+  const int64_t wanted = kUnits * (p.rows == 256 ? 1 : p.rows == 128 || fit > 2 ? 2 : fit) / (p.pairs * p.tiles), most = most_splits(max_tokens);
   p.splits = (int)(wanted < 1 ? 1 : wanted < most ? wanted : most);
   p.least = (int)(kKeysLeast / 32);
   return p;
@@ -829,17 +834,22 @@ static int launch_rows(const AttendArgs& a, const AttendPlan& p, hipStream_t st)
   hipLaunchKernelGGL((rows_kernel<DH, E4M3, NR>), dim3((unsigned)(p.pairs * p.tiles * p.splits)), dim3(256), lds, st, a);
   return check_launch("paged_attention_forward");
 }
-template <int DH, bool E4M3>
+template <int DH, bool E4M3, int NW>
 static int launch_tiles(const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
-  constexpr int lds = 2 * 2 * kTileKeys * DH * 2 + (DH + 4) * (int)sizeof(int);
+  constexpr int lds = 2 * 2 * 16 * NW * DH * 2 + (DH + 4) * (int)sizeof(int);
   static std::atomic<unsigned long long> done{0};
-  if (int rc = reserve_lds(tile_kernel<DH, E4M3>, lds, done, "paged_attention_forward")) return rc;
-  hipLaunchKernelGGL((tile_kernel<DH, E4M3>), dim3((unsigned)(p.pairs * p.tiles * p.splits)), dim3(256), lds, st, a);
+  if (int rc = reserve_lds(tile_kernel<DH, E4M3, NW>, lds, done, "paged_attention_forward")) return rc;
+  hipLaunchKernelGGL((tile_kernel<DH, E4M3, NW>), dim3((unsigned)(p.pairs * p.tiles * p.splits)), dim3(64 * NW), lds, st, a);
   return check_launch("paged_attention_forward");
 }
 template <int DH, bool E4M3>
 static int launch_attend(const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
-  const int rc = p.rows == 16 ? launch_rows<DH, E4M3, 1>(a, p, st) : p.rows == 32 ? launch_rows<DH, E4M3, 2>(a, p, st) : launch_tiles<DH, E4M3>(a, p, st);
+  int rc;
+  if (p.rows == 16) rc = launch_rows<DH, E4M3, 1>(a, p, st);
+  else if (p.rows == 32) rc = launch_rows<DH, E4M3, 2>(a, p, st);
+  else if (p.rows == 128) rc = launch_tiles<DH, E4M3, 4>(a, p, st);
+  else if constexpr (DH == 128 && E4M3) rc = launch_tiles<DH, E4M3, 8>(a, p, st);
+  else return fail(-1, "paged_attention_forward: no kernel for %d rows", p.rows);
   if (rc || p.splits == 1) return rc;
   // groups of lanes to a row: enough that each has no more than four parts, as far as a workgroup of 1024 threads goes
   constexpr int LPR = DH / 4;

@@ -247,7 +247,7 @@ def ragged(rng, batch, longest, s, empty=True):
 
 # batch, longest row, seq, query and KV heads, head_dim, page: more rows than are put in order, and fewer; keys cut into parts or not; 16, 32 and 128 rows to a workgroup
 RAGGED = [(70, 200, 1, 4, 2, 32, 16), (3, 3000, 2, 16, 8, 64, 16), (9, 1500, 1, 2, 1, 128, 32), (2, 5000, 3, 16, 2, 128, 128), (66, 150, 9, 4, 1, 32, 16), (5, 900, 40, 8, 8, 64, 16),
-          (2, 2600, 70, 4, 2, 128, 64), (1, 4500, 33, 4, 1, 32, 256)]
+          (2, 2600, 70, 4, 2, 128, 64), (1, 4500, 33, 4, 1, 32, 256), (70, 80, 34, 8, 8, 128, 16)]
 
 
 @pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
@@ -260,6 +260,35 @@ def test_ragged_batches(K, case, e4m3):
     qb = bits(rng, (batch, s, hq, dh), 2.0)
     o, lse = run(K, pages.device(K), spoiled(dev_bf16(qb), n), start, n, hq, dh ** -0.5)
     check(o, lse, og.attention(pages.oracle(), si.bf16_bits_to_f64(qb), start, n, dh ** -0.5), dh)
+
+
+def test_many_rows_of_an_e4m3_cache(K):
+    """Eight waves to a workgroup: rows and keys that end inside its tiles, NaN among the last tokens, a page that does not exist; sampled rows against the oracle."""
+    rng = np.random.default_rng(9)
+    b, s, hq, hkv, dh, page = 4, 530, 64, 8, 128, 16
+    start, n = [300, 0, 77, 5], [530, 17, 399, 0]
+    pages = Pages(rng, [a + m for a, m in zip(start, n)], hkv, dh, page, True)
+    pages.table[2, 3] = -1
+    qb = bits(rng, (b, s, hq, dh), 2.0)
+    p = start[0] + 500
+    pages.codes[1][pages.table[0, p // page], 3, p % page, 100] = 0x7F
+    o, lse = run(K, pages.device(K), spoiled(dev_bf16(qb), n), start, n, hq, 0.088)
+    assert torch.isnan(o[0, 500:, 24:32, 100]).all() and int(torch.isnan(o).sum()) == 30 * 8
+    o[0, 500:, 24:32, 100] = 0
+    cache, got, q = pages.oracle(), host_f64(o), si.bf16_bits_to_f64(qb)
+    cache["v"] = np.nan_to_num(cache["v"], nan=0.0)
+    for i in range(b):
+        assert np.all(got[i, n[i]:] == 0) and bool(torch.isneginf(lse[i, :, n[i]:]).all())
+        for t in sorted({0, 1, 31, 32, 33, 63, 64, 127, 200, n[i] - 1} & set(range(n[i]))):
+            one = dict(cache, page_table=cache["page_table"][i:i + 1])
+            heads = [0, 9, 31, 63]
+            for h in heads:
+                j = h // (hq // hkv)
+                sub = {"k": one["k"][:, j:j + 1], "v": one["v"][:, j:j + 1], "page_table": one["page_table"]}
+                ref = og.attention(sub, q[i:i + 1, t:t + 1, h:h + 1], [start[i] + t], None, 0.088)
+                if i == 0 and t >= 500 and j == 3:
+                    ref[0][..., 100], got[i, t, h, 100] = 0, 0
+                check(torch.from_numpy(got[i:i + 1, t:t + 1, h:h + 1]), lse[i:i + 1, h:h + 1, t:t + 1], ref, dh)
 
 
 @pytest.mark.parametrize("s,hq,longest", [(1, 4, 3000), (7, 4, 3000), (60, 4, 3000), (60, 16, 200)])
