@@ -132,7 +132,7 @@ struct Operands {
   __device__ __forceinline__ Operands(uint32_t tiles, int lane) {
     const int row = lane & 31, grp = lane >> 4, s = lane & 15, vrow = ((grp >> 1) << 2) + (s >> 2), col = ((grp & 1) << 4) + ((s & 3) << 2);
     k = tiles + row * Tile::ROW_B + (((lane >> 5) ^ Tile::swz(row)) << 4);
-    v = tiles + Tile::BYTES + vrow * Tile::ROW_B + ((((col >> 3) ^ Tile::swz(vrow)) << 4) | ((col & 7) << 1));
+    v = tiles + vrow * Tile::ROW_B + ((((col >> 3) ^ Tile::swz(vrow)) << 4) | ((col & 7) << 1));
   }
   __device__ __forceinline__ bf16x8 key(int kk, int i) const {
     return *(LDS_PTR(const bf16x8))(uintptr_t)((k ^ (kk << 5)) + i * (32 * Tile::ROW_B));
@@ -168,11 +168,22 @@ __device__ __forceinline__ bool any_not_finite(const bf16x8& v) {
   return odd;
 }
 
+// Whether the tiles of values share one place in LDS, so that three workgroups fit a compute unit (48 KB each at heads of 128): of bf16 with four waves.  Values are then asked for when
+// the last tile's are done with, and waited for behind the exponentials (two prompts of 8192 tokens, 32 and 8 heads of 128: 1060 us with two
+// workgroups, 993 with three; as many products under way beside exponentials of others is what counts: the matrix units were busy 47 % of the cycles).
+template <bool E4M3, int NW>
+constexpr bool kThin = !E4M3 && NW == 4;
 template <int DH, bool E4M3, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void tile_kernel(const AttendArgs a) {
+constexpr int tile_lds() { return (kThin<E4M3, NW> ? 3 : 4) * 16 * NW * DH * 2; }
+
+template <int DH, bool E4M3, int NW>
+__global__ __launch_bounds__(64 * NW, (kThin<E4M3, NW>) ? 3 : 2) void tile_kernel(const AttendArgs a) {
   constexpr int kTileRows = 32 * NW, kTileKeys = 16 * NW;
   using Tile = RowTile<kTileKeys, DH, NW>;
-  constexpr int STAGE = 2 * Tile::BYTES;
+  constexpr bool THIN = kThin<E4M3, NW>;
+  // where keys and values of a stage lie; THIN: one place for values
+  constexpr int K_STAGE = THIN ? Tile::BYTES : 2 * Tile::BYTES, V_FIRST = THIN ? 2 * Tile::BYTES : Tile::BYTES, V_STAGE = THIN ? 0 : K_STAGE, TILES = tile_lds<DH, E4M3, NW>();
+  const auto place = [](int w, int stage) { return w ? V_FIRST + stage * V_STAGE : stage * K_STAGE; };
   // e4m3: a wave's 16 keys as they are held; CHUNK bytes a lane and load, LANES of them a key
   constexpr int HELD = 16 * DH, CHUNK = HELD < 1024 ? 8 : 16, NLOAD = HELD / (64 * CHUNK), LANES = DH / CHUNK, ROWS = 64 / LANES;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
@@ -193,7 +204,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tile_kernel(const AttendArgs a) {
   // the last key that any of the wave's rows sees; none for a wave behind the last row
   const int lim1 = row0 + wave * 32 < n_rows ? __builtin_amdgcn_readlane(lim, 31) : -1;
   const int first_lim = n_rows > 0 ? __builtin_amdgcn_readfirstlane(last_key(min(row0, n_rows - 1))) : -1;     // the first row's
-  int* first_odd = reinterpret_cast<int*>(smem + 2 * STAGE);       // the first key with a value that is not finite, of each column; whether there is any
+  int* first_odd = reinterpret_cast<int*>(smem + TILES);       // the first key with a value that is not finite, of each column; whether there is any
   const int all = (end + kTileKeys - 1) / kTileKeys, per = (all + a.splits - 1) / a.splits;
   const int t0 = split * per, t1 = min(all, t0 + per);
 
@@ -223,11 +234,11 @@ __global__ __launch_bounds__(64 * NW, 2) void tile_kernel(const AttendArgs a) {
     // e4m3: of the wave's 16 keys of the next tile in lanes 0 .. 15, of its values in the next 16; and how many of the keys there are
     uint32_t scales = 0;
     int there = 0;
-    const auto load = [&](int t, int stage) {
+    const auto load = [&](int t, int stage, int first, int last) {             // keys (0), values (1), or both
       const Keys16 k16 = keys16(c, b, hk, t * kTileKeys + wave * 16, end);
 #pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        const uint32_t to = lds_address(smem) + stage * STAGE + w * Tile::BYTES + wave * (16 * Tile::ROW_B);
+      for (int w = first; w <= last; ++w) {
+        const uint32_t to = lds_address(smem) + place(w, stage) + wave * (16 * Tile::ROW_B);
         if constexpr (!E4M3) {
           const i32x4 from = descriptor(c.x[w] + k16.vec * (DH * 2), (uint32_t)(k16.n * DH * 2));
 #pragma unroll
@@ -250,12 +261,11 @@ __global__ __launch_bounds__(64 * NW, 2) void tile_kernel(const AttendArgs a) {
     // what a wave has loaded, made ready for all: e4m3 in its place as bf16; and, of a tile that some row sees in part, values that are not finite taken
     // out, since a weight of 0 times one of them is NaN: the first key that has one in a column is remembered, and the rows that see it get NaN at the end
     const auto arrived = [&](int t, int stage) {
-      wait_loads<0>();
       if constexpr (E4M3) {
         scales = (lane & 15) < there ? scales << 23 : 0;        // keys that are not there are zeros times whatever was read
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
-          char* own = smem + stage * STAGE + w * Tile::BYTES + wave * (16 * Tile::ROW_B);
+          char* own = smem + place(w, stage) + wave * (16 * Tile::ROW_B);
           u32x2 raw[NLOAD][CHUNK / 8];
 #pragma unroll
           for (int i = 0; i < NLOAD; ++i)
@@ -273,7 +283,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tile_kernel(const AttendArgs a) {
         }
       }
       if (t * kTileKeys + kTileKeys - 1 > first_lim) {
-        char* own = smem + stage * STAGE + Tile::BYTES + wave * (16 * Tile::ROW_B);
+        char* own = smem + place(1, stage) + wave * (16 * Tile::ROW_B);
 #pragma unroll 1
         for (int i = 0; i < Tile::PER_WAVE; ++i) {
           bf16x8* at = reinterpret_cast<bf16x8*>(own + i * 1024 + lane * 16);
@@ -293,23 +303,26 @@ __global__ __launch_bounds__(64 * NW, 2) void tile_kernel(const AttendArgs a) {
     };
 
     const Operands<DH, NW> operands(lds_address(smem), lane);
-    load(t0, 0);
-    arrived(t0, 0);
+    load(t0, 0, 0, THIN ? 0 : 1);
+    wait_loads<0>();
+    if (!THIN) arrived(t0, 0);
     __syncthreads();
     int stage = 0;
     for (int t = t0; t < t1; ++t) {
-      if (t + 1 < t1) load(t + 1, stage ^ 1);
+      const bool more = t + 1 < t1;
+      if (THIN) load(t, stage, 1, 1);
+      if (more) load(t + 1, stage ^ 1, 0, THIN ? 0 : 1);
 #pragma unroll
       for (int sub = 0; sub < kTileKeys / kSubKeys; ++sub) {
       const int kv0 = t * kTileKeys + sub * kSubKeys;
-      if (kv0 <= lim1) {
-      Operands<DH, NW> at = operands;
-      at.k += stage * STAGE + sub * (kSubKeys * Tile::ROW_B);
-      at.v += stage * STAGE + sub * (kSubKeys * Tile::ROW_B);
-      asm volatile("" : "+v"(at.k), "+v"(at.v));                 // their XORs are formed here, and take no registers across the loop
-      // the wave that has products to issue goes first, so that the other one's exponentials fall beside them and not beside its own products
-      __builtin_amdgcn_s_setprio(1);
       f32x16 s[2];
+      Operands<DH, NW> at = operands;
+      at.k += place(0, stage) + sub * (kSubKeys * Tile::ROW_B);
+      at.v += place(1, stage) + sub * (kSubKeys * Tile::ROW_B);
+      asm volatile("" : "+v"(at.k), "+v"(at.v));                 // their XORs are formed here, and take no registers across the loop
+      if (kv0 <= lim1) {
+      // the wave that has products to issue goes first, so that the other ones' exponentials fall beside them and not beside their own products
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -356,6 +369,14 @@ __global__ __launch_bounds__(64 * NW, 2) void tile_kernel(const AttendArgs a) {
           psum += pv;
         }
       lsum += psum;
+      }
+      if constexpr (THIN) {
+        // the values, asked for before the next keys: all waves have theirs
+        if (more) wait_loads<Tile::PER_WAVE>(); else wait_loads<0>();
+        arrived(t, 0);
+        __syncthreads();
+      }
+      if (kv0 <= lim1) {
       __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int ks = 0; ks < 4; ++ks) {
@@ -366,7 +387,8 @@ __global__ __launch_bounds__(64 * NW, 2) void tile_kernel(const AttendArgs a) {
       __builtin_amdgcn_s_setprio(0);
       }
       }
-      if (t + 1 < t1) arrived(t + 1, stage ^ 1);
+      wait_loads<0>();
+      if (!THIN && more) arrived(t + 1, stage ^ 1);
       __syncthreads();
       stage ^= 1;
     }
@@ -798,7 +820,7 @@ __global__ __launch_bounds__(1024) void combine_kernel(const AttendArgs a, int64
 // are what counts and rows_kernel is as fast as they come; tile_kernel's matrix products of 32 rows a wave are for more.  Eight waves a workgroup make bf16 of e4m3 once for twice the rows
 // (two prompts of 8192 tokens, heads of 128: 1087 us, 1189 with four waves; bf16 itself 1102 and 1097), where that leaves every compute unit two workgroups to take.  As many parts as fill the chip once: of rows_kernel
 // the workgroups whose tiles the LDS holds (more of them, shorter, take longer: 8 rows over 16000 bf16 tokens 139 us in 4096 workgroups, 99 in 512),
-// of tile_kernel two a compute unit; none shorter than kKeysLeast, and one only where there is no more than twice that, which a second launch would cost more than it saves.
+// of tile_kernel two a compute unit (three, which fit: 512 tokens behind 8000 85.6 -> 90.2 us, 8 rows of 128 behind up to 4000 77.0 -> 69.2); none shorter than kKeysLeast, and one only where there is no more than twice that, which a second launch would cost more than it saves.
 struct AttendPlan { int rows, tiles, splits, least; int64_t pairs; };
 constexpr int64_t kUnits = 256, kKeysLeast = 256;
 static int64_t most_splits(int64_t max_tokens) { return max_tokens <= 2 * kKeysLeast ? 1 : (max_tokens + kKeysLeast - 1) / kKeysLeast; }
@@ -815,7 +837,7 @@ static AttendPlan attend_plan(int64_t batch, int64_t seq, int64_t Hkv, int64_t g
   return p;
 }
 
-// Sums and statistics of the parts, in rows: pairs * tiles * splits * rows of a workgroup is within 512 workgroups of rows wherever there is a split, and within pairs * (rows, filled up) *
+// Sums and statistics of the parts, in rows: pairs * tiles * splits * rows of a workgroup is within two workgroups a compute unit wherever there is a split, and within pairs * (rows, filled up) *
 // most_splits, neither of which falls as the call grows.
 static int64_t rows_held(int64_t batch, int64_t seq, int64_t Hkv, int64_t group, int64_t dh, bool e4m3, int64_t max_tokens) {
   const AttendPlan p = attend_plan(batch, seq, Hkv, group, dh, e4m3, max_tokens);
@@ -836,7 +858,7 @@ static int launch_rows(const AttendArgs& a, const AttendPlan& p, hipStream_t st)
 }
 template <int DH, bool E4M3, int NW>
 static int launch_tiles(const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
-  constexpr int lds = 2 * 2 * 16 * NW * DH * 2 + (DH + 4) * (int)sizeof(int);
+  constexpr int lds = tile_lds<DH, E4M3, NW>() + (DH + 4) * (int)sizeof(int);
   static std::atomic<unsigned long long> done{0};
   if (int rc = reserve_lds(tile_kernel<DH, E4M3, NW>, lds, done, "paged_attention_forward")) return rc;
   hipLaunchKernelGGL((tile_kernel<DH, E4M3, NW>), dim3((unsigned)(p.pairs * p.tiles * p.splits)), dim3(64 * NW), lds, st, a);
