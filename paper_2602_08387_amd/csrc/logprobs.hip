@@ -4,16 +4,21 @@
 //   lse = M + ln S;  logp(v) = (z_v - M) - ln S;  entropy = ln S - U / S                          (no difference of large numbers)
 //   dx_v = ([v = target] dlp - p_v (dlp + dH (logp_v + entropy))) / temperature
 //
-// Forward: one pass, bound by the reading of the logits (2 bytes each; some 10 vector instructions an element, of which the exponential takes four).
-// A thread keeps S and U relative to its own running maximum, which it raises once in 32 elements.  Exponents are formed as (x - max) times a
-// constant: of a row that is all but certain S is then 1 and a little, exactly, where one FMA against the rounded product max * constant would be
-// off by that rounding (and infinite for a row masked with the type's lowest value).
+// Forward: one pass, bound by the reading of the logits (2 bytes each; some 10 vector instructions an element, of which the exponential takes four). A thread
+// keeps S and U relative to its own running maximum, which it raises once in 32 elements.  Exponents are formed as (x - max) times a constant: of a row that
+// is all but certain S is then 1 and a little, exactly, where one FMA against the rounded product max * constant would be off by that rounding (and infinite
+// for a row masked with the type's lowest value).
 //
-// The likeliest tokens: a wave keeps a list of 64 sorted over its lanes.  An element has to pass the list's n-th; those that do (some n ln(row / first
-// elements)) go to a buffer in LDS and are sorted into the list 64 at a time.  The first threshold is the n-th largest of the lanes' own maxima
-// over their first 32 elements.  An order without ties: a 64-bit key of the logit's bits as a whole number of the same order, then the lower index.
+// The likeliest tokens: a wave keeps a list of 64 sorted over its lanes.  An element has to pass the list's n-th, and a bound that the workgroup's waves
+// share: at first the n-th largest of the threads' maxima over their first 32 elements, then the least of what the waves have as their (n / 4)-th.  The few
+// that pass go to a buffer in LDS and from there into the list, one by one or sorted 64 at a time.  An order without ties: a 64-bit key of the logit's bits
+// as a whole number of the same order, then the lower index.
 //
 // Few rows are cut into parts, joined by a second kernel.
+//
+// Measured, 128256 tokens a row: 4096 rows 215 us without the likeliest, 222 with 5 (1.05 GB, 4.7 TB/s: memory), 255 with 20, 294 with 64 (vector
+// instructions); one row 13.9 with 20 (two launches, 8.7 and 5.7 us: loads, exchanges and barriers one after the other).  The gradient of 4096 rows 395 us
+// (2.1 GB, 5.3 TB/s: memory).
 #include "common.h"
 #include "kernels.h"
 #include "lane_exchange.h"
@@ -169,8 +174,8 @@ struct TopList {
   }
 };
 
-// WAVES: of a workgroup.  One wave takes a short part alone, without waiting for others and without joining their lists (64 rows of 32000, 20 likeliest: 13.8 us, 16.7
-// with four); of longer parts, or with many likeliest to sort, four share the work and their bounds.
+// WAVES: of a workgroup.  One wave takes a short part alone, without waiting for others and without joining their lists (64 rows of 32000, 20 likeliest: 13.8
+// us, 16.7 with four); of longer parts, or with many likeliest to sort, four share the work and their bounds.
 template <bool TOP, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 6) void logprobs_kernel(const LogprobsArgs a) {
   constexpr int kLpWaves = WAVES, kLpThreads = 64 * WAVES;

@@ -2,17 +2,23 @@
 //
 //   o = sum_s w_s v_s / sum_s w_s,  w_s = exp(scale q . k_s - m),  s = 0 .. the token's own position;   lse = m + log sum_s w_s
 //
-// One pass over the keys with the running maximum and sum.  The query heads of a KV head's group share its keys, so a matrix product's rows are (token,
-// head of the group) pairs, row = token * group + head: the keys of a group are read once for all of them.
+// One pass over the keys with the running maximum and sum.  The query heads of a KV head's group share its keys, so a matrix product's rows are (token, head
+// of the group) pairs, row = token * group + head: the keys of a group are read once for all of them.
 //
-// tile_kernel: workgroup = 128 rows of one (batch row, KV head), four waves of 32 (or 256 rows, eight waves); score tiles S^T[key][row] = K Q^T on v_mfma_f32_32x32x16_bf16, whose
-// layout is that of the next product's operand, O^T[d][row] += V^T P^T.  Tiles of 64 (128) keys stream to LDS, double buffered; a wave loads the 16 keys of
-// its own part of the tile, which lie in one page (a page has 16 tokens or a multiple), so a tile needs one page number a wave.  Loads go to LDS
-// directly; a wave then writes its 16 keys of e4m3, in their place, as the bf16 values that they stand for.  The keys can be split over workgroups, whose sums
-// combine_kernel joins.
+// tile_kernel: workgroup = 128 rows of one (batch row, KV head), four waves of 32 (or 256 rows, eight waves); score tiles S^T[key][row] = K Q^T on
+// v_mfma_f32_32x32x16_bf16, whose layout is that of the next product's operand, O^T[d][row] += V^T P^T.  Tiles of 64 (128) keys stream to LDS, double
+// buffered; a wave loads the 16 keys of its own part of the tile, which lie in one page (a page has 16 tokens or a multiple), so a tile needs one page number
+// a wave.  Loads go to LDS directly; a wave then writes its 16 keys of e4m3, in their place, as the bf16 values that they stand for.  The keys can be split
+// over workgroups, whose sums combine_kernel joins.
 //
-// Rows behind a tile's last key and pages that do not exist are behind the end of the buffer that a load is given, and read as zeros: what a page
-// holds behind a row's last token is never read.
+// Rows behind a tile's last key and pages that do not exist are behind the end of the buffer that a load is given, and read as zeros: what a page holds
+// behind a row's last token is never read.
+//
+// What bounds them (32 query and 8 KV heads of 128).  rows_kernel: memory, 256 rows of up to 4096 bf16 tokens in 373 us (5.6 TB/s of keys and values), one
+// row over 32768 e4m3 tokens in 20.5 (15 us, 4.6 TB/s, and 5 for joining 64 parts).  tile_kernel: two prompts of 8192 tokens in 1.00 to 1.06 ms (1040 to 1100
+// TFLOP/s), the clock at 1.7 GHz by the card's power limit; with two workgroups a compute unit the matrix units were busy 47 % of the cycles and the vector
+// units, exponentials above all, 43 %; the third workgroup brings more of that side by side.  The next tile's scores beside this tile's exponentials within a
+// wave: 6 % fewer cycles, at a lower clock, and no less time.
 #include "attention_tile.h"
 #include "common.h"
 #include "kernels.h"
@@ -67,10 +73,10 @@ __device__ __forceinline__ int row_of_rank(const AttendArgs& a, int rank, int la
   return __builtin_ctzll(__builtin_amdgcn_ballot_w64(lane < batch && above == rank));
 }
 
-// Workgroup -> (batch row, KV head, place in their queue of workgroups).  Ids go to the eight XCDs in turn, each with an L2 of its own: where the heads are a multiple of 8
-// a head's workgroups, which share its keys, stay on one XCD, and every XCD has as much of each batch row.  A queue's places are dealt to the heads in turn, long ones
-// first.  SORTED: the rows with most keys come first, since the last workgroups to start should be short ones (5 rows of 0 to 1037 tokens behind 1600 to
-// 8000, 8 heads: 381 us, 472 in the order of the rows); worth its microsecond where workgroups are long and of different length.
+// Workgroup -> (batch row, KV head, place in their queue of workgroups).  Ids go to the eight XCDs in turn, each with an L2 of its own: where the heads are a
+// multiple of 8 a head's workgroups, which share its keys, stay on one XCD, and every XCD has as much of each batch row.  A queue's places are dealt to the
+// heads in turn, long ones first.  SORTED: the rows with most keys come first, since the last workgroups to start should be short ones (5 rows of 0 to 1037
+// tokens behind 1600 to 8000, 8 heads: 381 us, 472 in the order of the rows); worth its microsecond where workgroups are long and of different length.
 struct Work { int b, hk, j; };
 template <bool SORTED>
 __device__ __forceinline__ Work work_of(const AttendArgs& a, int id, int queue, int lane) {
@@ -92,7 +98,8 @@ __device__ __forceinline__ i32x4 descriptor(const void* p, uint32_t bytes) {
   return i32x4{(int)(uint32_t)at, (int)((uint32_t)(at >> 32) & 0xffffu), (int)bytes, 0x00020000};
 }
 __device__ __forceinline__ void load_to_lds(const i32x4& from, uint32_t to, int offset) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(offset), "s"(from) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(offset), "s"(from)
+               : "memory");
 }
 // Until LEFT of them are under way.  The builtin tells the compiler that its own loads are done too (it does not read assembly, and would wait for them, and so for
 // the loads to LDS, at their next use).
@@ -123,8 +130,8 @@ __device__ __forceinline__ Keys16 keys16(const PagedCache& c, int b, int hk, int
   return {vector_of(c, page, hk, p), n < 16 ? n : 16};
 }
 
-// LDS addresses of a lane's operands in a tile of RowTile's layout.  Its swizzle is an XOR of chunk numbers, so that the steps along head_dim are XORs of one address
-// and steps of 16 rows an offset: key(kk, i) of keys 32 i + lane % 32, step kk; value(t2, ks) of columns 32 t2 .., keys 16 ks .., as frag_cols.
+// LDS addresses of a lane's operands in a tile of RowTile's layout.  Its swizzle is an XOR of chunk numbers, so that the steps along head_dim are XORs of one
+// address and steps of 16 rows an offset: key(kk, i) of keys 32 i + lane % 32, step kk; value(t2, ks) of columns 32 t2 .., keys 16 ks .., as frag_cols.
 template <int DH, int NW>
 struct Operands {
   using Tile = RowTile<16 * NW, DH, NW>;
@@ -168,9 +175,10 @@ __device__ __forceinline__ bool any_not_finite(const bf16x8& v) {
   return odd;
 }
 
-// Whether the tiles of values share one place in LDS, so that three workgroups fit a compute unit (48 KB each at heads of 128): of bf16 with four waves.  Values are then asked for when
-// the last tile's are done with, and waited for behind the exponentials (two prompts of 8192 tokens, 32 and 8 heads of 128: 1060 us with two
-// workgroups, 993 with three; as many products under way beside exponentials of others is what counts: the matrix units were busy 47 % of the cycles).
+// Whether the tiles of values share one place in LDS, so that three workgroups fit a compute unit (48 KB each at heads of 128): of bf16 with four waves.
+// Values are then asked for when the last tile's are done with, and waited for behind the exponentials (two prompts of 8192 tokens, 32 and 8 heads of 128:
+// 1060 us with two workgroups, 993 with three; as many products under way beside exponentials of others is what counts: the matrix units were busy 47 % of
+// the cycles).
 template <bool E4M3, int NW>
 constexpr bool kThin = !E4M3 && NW == 4;
 template <int DH, bool E4M3, int NW>
@@ -182,7 +190,8 @@ __global__ __launch_bounds__(64 * NW, (kThin<E4M3, NW>) ? 3 : 2) void tile_kerne
   using Tile = RowTile<kTileKeys, DH, NW>;
   constexpr bool THIN = kThin<E4M3, NW>;
   // where keys and values of a stage lie; THIN: one place for values
-  constexpr int K_STAGE = THIN ? Tile::BYTES : 2 * Tile::BYTES, V_FIRST = THIN ? 2 * Tile::BYTES : Tile::BYTES, V_STAGE = THIN ? 0 : K_STAGE, TILES = tile_lds<DH, E4M3, NW>();
+  constexpr int K_STAGE = THIN ? Tile::BYTES : 2 * Tile::BYTES, V_FIRST = THIN ? 2 * Tile::BYTES : Tile::BYTES, V_STAGE = THIN ? 0 : K_STAGE;
+  constexpr int TILES = tile_lds<DH, E4M3, NW>();
   const auto place = [](int w, int stage) { return w ? V_FIRST + stage * V_STAGE : stage * K_STAGE; };
   // e4m3: a wave's 16 keys as they are held; CHUNK bytes a lane and load, LANES of them a key
   constexpr int HELD = 16 * DH, CHUNK = HELD < 1024 ? 8 : 16, NLOAD = HELD / (64 * CHUNK), LANES = DH / CHUNK, ROWS = 64 / LANES;
@@ -314,78 +323,78 @@ __global__ __launch_bounds__(64 * NW, (kThin<E4M3, NW>) ? 3 : 2) void tile_kerne
       if (more) load(t + 1, stage ^ 1, 0, THIN ? 0 : 1);
 #pragma unroll
       for (int sub = 0; sub < kTileKeys / kSubKeys; ++sub) {
-      const int kv0 = t * kTileKeys + sub * kSubKeys;
-      f32x16 s[2];
-      Operands<DH, NW> at = operands;
-      at.k += place(0, stage) + sub * (kSubKeys * Tile::ROW_B);
-      at.v += place(1, stage) + sub * (kSubKeys * Tile::ROW_B);
-      asm volatile("" : "+v"(at.k), "+v"(at.v));                 // their XORs are formed here, and take no registers across the loop
-      if (kv0 <= lim1) {
-      // the wave that has products to issue goes first, so that the other ones' exponentials fall beside them and not beside their own products
-      __builtin_amdgcn_s_setprio(1);
+        const int kv0 = t * kTileKeys + sub * kSubKeys;
+        f32x16 s[2];
+        Operands<DH, NW> at = operands;
+        at.k += place(0, stage) + sub * (kSubKeys * Tile::ROW_B);
+        at.v += place(1, stage) + sub * (kSubKeys * Tile::ROW_B);
+        asm volatile("" : "+v"(at.k), "+v"(at.v));                 // their XORs are formed here, and take no registers across the loop
+        if (kv0 <= lim1) {
+          // the wave that has products to issue goes first, so that the other ones' exponentials fall beside them and not beside their own products
+          __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+          for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s[i][e] = 0.f;
+            for (int e = 0; e < 16; ++e) s[i][e] = 0.f;
 #pragma unroll
-      for (int kk = 0; kk < DH / 16; ++kk)
+          for (int kk = 0; kk < DH / 16; ++kk)
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-          s[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at.key(kk, i), qf[kk], s[i], 0, 0, 0);
-      __builtin_amdgcn_s_setprio(0);
-      // keys after the row's own position (only on tiles that reach past this wave's first row)
-      if (kv0 + kSubKeys - 1 > lim0) mask_rows_above<2>(s, lim - kv0 - (half << 2), -INFINITY);
-      if (missing) {
+            for (int i = 0; i < 2; ++i)
+              s[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at.key(kk, i), qf[kk], s[i], 0, 0, 0);
+          __builtin_amdgcn_s_setprio(0);
+          // keys after the row's own position (only on tiles that reach past this wave's first row)
+          if (kv0 + kSubKeys - 1 > lim0) mask_rows_above<2>(s, lim - kv0 - (half << 2), -INFINITY);
+          if (missing) {
 #pragma unroll
-        for (int g = 0; g < 4; ++g)
-          if (page_of_wave(c, b, kv0 + g * 16) < 0)
+            for (int g = 0; g < 4; ++g)
+              if (page_of_wave(c, b, kv0 + g * 16) < 0)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s[g >> 1][(g & 1) * 8 + e] = -INFINITY;
-      }
-      float mx = s[0][0];
+                for (int e = 0; e < 8; ++e) s[g >> 1][(g & 1) * 8 + e] = -INFINITY;
+          }
+          float mx = s[0][0];
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+          for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[i][e]);
-      mx = max_across_halves(mx) * a.scale_log2;
-      // raised only where some row's maximum grew by more than 2^8: weights stay below 256, and sum and result carry the same reference
-      if (__builtin_amdgcn_ballot_w64(mx > m + 8.0f) != 0) {
-        const float m_new = fmaxf(m, mx);
-        const float alpha = fast_exp2(m - m_new);
-        lsum *= alpha;
-        m = m_new;
+            for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[i][e]);
+          mx = max_across_halves(mx) * a.scale_log2;
+          // raised only where some row's maximum grew by more than 2^8: weights stay below 256, and sum and result carry the same reference
+          if (__builtin_amdgcn_ballot_w64(mx > m + 8.0f) != 0) {
+            const float m_new = fmaxf(m, mx);
+            const float alpha = fast_exp2(m - m_new);
+            lsum *= alpha;
+            m = m_new;
 #pragma unroll
-        for (int t2 = 0; t2 < DH / 32; ++t2)
+            for (int t2 = 0; t2 < DH / 32; ++t2)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) oacc[t2][e] *= alpha;
-      }
-      float psum = 0.f;
+              for (int e = 0; e < 16; ++e) oacc[t2][e] *= alpha;
+          }
+          float psum = 0.f;
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+          for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const float pv = fast_exp2(__builtin_fmaf(s[i][e], a.scale_log2, -m));
-          s[i][e] = pv;
-          psum += pv;
+            for (int e = 0; e < 16; ++e) {
+              const float pv = fast_exp2(__builtin_fmaf(s[i][e], a.scale_log2, -m));
+              s[i][e] = pv;
+              psum += pv;
+            }
+          lsum += psum;
         }
-      lsum += psum;
-      }
-      if constexpr (THIN) {
-        // the values, asked for before the next keys: all waves have theirs
-        if (more) wait_loads<Tile::PER_WAVE>(); else wait_loads<0>();
-        arrived(t, 0);
-        __syncthreads();
-      }
-      if (kv0 <= lim1) {
-      __builtin_amdgcn_s_setprio(1);
+        if constexpr (THIN) {
+          // the values, asked for before the next keys: all waves have theirs
+          if (more) wait_loads<Tile::PER_WAVE>(); else wait_loads<0>();
+          arrived(t, 0);
+          __syncthreads();
+        }
+        if (kv0 <= lim1) {
+          __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks) {
-        const bf16x8 pf = pack_slots(s[ks >> 1], (ks & 1) * 8);
+          for (int ks = 0; ks < 4; ++ks) {
+            const bf16x8 pf = pack_slots(s[ks >> 1], (ks & 1) * 8);
 #pragma unroll
-        for (int t2 = 0; t2 < DH / 32; ++t2) oacc[t2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at.value(t2, ks), pf, oacc[t2], 0, 0, 0);
-      }
-      __builtin_amdgcn_s_setprio(0);
-      }
+            for (int t2 = 0; t2 < DH / 32; ++t2) oacc[t2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at.value(t2, ks), pf, oacc[t2], 0, 0, 0);
+          }
+          __builtin_amdgcn_s_setprio(0);
+        }
       }
       wait_loads<0>();
       if (!THIN && more) arrived(t + 1, stage ^ 1);
@@ -446,8 +455,8 @@ __device__ __forceinline__ float sum_across_quarters(float x) {
   return x + __shfl_xor(x, 16, 64);
 }
 
-// A wave's tile of 32 keys, or values, in LDS as the cache holds it: rows of ROW_B bytes, 16-byte chunk c of row r at chunk c ^ swz(r).  Free of bank conflicts (the LDS serves
-// 256 B of banks a clock) for both of its reads:
+// A wave's tile of 32 keys, or values, in LDS as the cache holds it: rows of ROW_B bytes, 16-byte chunk c of row r at chunk c ^ swz(r).  Free of bank
+// conflicts (the LDS serves 256 B of banks a clock) for both of its reads:
 //   row reads: 16 lanes, 16 consecutive rows, one chunk;
 //   transposing reads: 32 lanes, which take 32 B (bf16) of rows 0 .. 7 or 8 .. 15 of 16, or 16 B (e4m3) of rows 0 .. 7 and 16 .. 23, or 8 .. 15 and 24 .. 31.
 template <int DH, bool E4M3>
@@ -470,15 +479,16 @@ struct HeldTile {
       const int offset = row * ROW_B + ch * 16 + at % 16;
       const uint32_t dst = to + (group * (LOADS / 2) + i) * (64 * WIDTH);
       if constexpr (WIDTH == 16) load_to_lds(from, dst, offset);
-      else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(dst)), "v"(offset), "s"(from) : "memory");
+      else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(dst)), "v"(offset), "s"(from)
+                        : "memory");
     }
   }
 };
 
-// Few rows (NR groups of 16), many keys: bound by the reading of the cache.  Each of the workgroup's four waves takes every fourth tile of 32 keys, which it loads to LDS for
-// itself, a tile ahead, so that the waves wait for nothing but their own loads; the four results are joined in LDS at the end.
-//   S[key][row] = K Q^T and O[d][row] += V^T P^T on v_mfma_f32_16x16x32_bf16: lane l has row l % 16 of its group, keys 4 (l / 16) .. + 3 of each half of the tile, and those are the
-//   slots that it gives the second product, whose other operand (transposing reads) is taken in that order.
+// Few rows (NR groups of 16), many keys: bound by the reading of the cache.  Each of the workgroup's four waves takes every fourth tile of 32 keys, which it
+// loads to LDS for itself, a tile ahead, so that the waves wait for nothing but their own loads; the four results are joined in LDS at the end.
+//   S[key][row] = K Q^T and O[d][row] += V^T P^T on v_mfma_f32_16x16x32_bf16: lane l has row l % 16 of its group, keys 4 (l / 16) .. + 3 of each
+//   half of the tile, and those are the slots that it gives the second product, whose other operand (transposing reads) is taken in that order.
 // e4m3 is read as it is held; scores and weights take the powers of two of their keys and values, exactly.
 template <int DH, bool E4M3, int NR>
 __global__ __launch_bounds__(256, NR == 1 ? 2 : 1) void rows_kernel(const AttendArgs a) {
@@ -536,8 +546,9 @@ __global__ __launch_bounds__(256, NR == 1 ? 2 : 1) void rows_kernel(const Attend
       if constexpr (E4M3) {
         // four lanes for each of (keys, values) x (first 16, last 16), from addresses of their own; where there are no keys, of others that take no part
         const uint8_t* from = (lane & 8 ? c.scale[1] : c.scale[0]) + (lane & 4 ? k16[1].vec : k16[0].vec) + (lane & 3) * 4;
+        const uint32_t to = __builtin_amdgcn_readfirstlane(own + stage * STAGE + 2 * Tile::BYTES);
         if (lane < 16)
-          asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(__builtin_amdgcn_readfirstlane(own + stage * STAGE + 2 * Tile::BYTES)), "v"(from) : "memory");
+          asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(to), "v"(from) : "memory");
       }
     };
     // a byte of 255 is no power of two, and may stand where there is no key: finite, so that a weight of 0 times it is 0
@@ -580,7 +591,8 @@ __global__ __launch_bounds__(256, NR == 1 ? 2 : 1) void rows_kernel(const Attend
 #pragma unroll
           for (int kk = 0; kk < DH / 32; ++kk) {
             bf16x8 kf;
-            if constexpr (E4M3) kf = unpack_e4m3(*(LDS_PTR(const u32x2))(uintptr_t)(tk + row * Tile::ROW_B + (((quarter >> 1) ^ Tile::swz(row)) << 4) + (quarter & 1) * 8), 1.f);
+            if constexpr (E4M3)
+              kf = unpack_e4m3(*(LDS_PTR(const u32x2))(uintptr_t)(tk + row * Tile::ROW_B + (((quarter >> 1) ^ Tile::swz(row)) << 4) + (quarter & 1) * 8), 1.f);
             else kf = *(LDS_PTR(const bf16x8))(uintptr_t)(tk + row * Tile::ROW_B + (((kk * 4 + quarter) ^ Tile::swz(row)) << 4));
 #pragma unroll
             for (int n = 0; n < NR; ++n) s[n][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[n][kk], s[n][g], 0, 0, 0);
@@ -612,12 +624,13 @@ __global__ __launch_bounds__(256, NR == 1 ? 2 : 1) void rows_kernel(const Attend
 #pragma unroll
             for (int n = 0; n < NR; ++n) s[n][g] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
       }
-      // a weight is the sum of two bf16: rounded to one it would add as much to the error as the rounding of the result does (2.3e-3 of a result, 1.7e-3 with two), and the
-      // matrix unit has little to do here (one row over 32768 e4m3 tokens 20.3 us with one, 20.7 with two)
+      // a weight is the sum of two bf16: rounded to one it would add as much to the error as the rounding of the result does (2.3e-3 of a result, 1.7e-3 with
+      // two), and the matrix unit has little to do here (one row over 32768 e4m3 tokens 20.3 us with one, 20.7 with two)
       bf16x8 pf[NR][2];
 #pragma unroll
       for (int n = 0; n < NR; ++n) {
-        float mx = fmaxf(fmaxf(fmaxf(s[n][0][0], s[n][0][1]), fmaxf(s[n][0][2], s[n][0][3])), fmaxf(fmaxf(s[n][1][0], s[n][1][1]), fmaxf(s[n][1][2], s[n][1][3]))) * a.scale_log2;
+        float mx = fmaxf(fmaxf(fmaxf(s[n][0][0], s[n][0][1]), fmaxf(s[n][0][2], s[n][0][3])),
+                         fmaxf(fmaxf(s[n][1][0], s[n][1][1]), fmaxf(s[n][1][2], s[n][1][3]))) * a.scale_log2;
         // the reference is raised only where some row's maximum grew by more than 2^8; until then the lanes of a row need not know each other's
         if (__builtin_amdgcn_ballot_w64(mx > m[n] + 8.0f) != 0) {
           const float m_new = fmaxf(m[n], max_across_quarters(mx)), alpha = fast_exp2(m[n] - m_new);
@@ -642,7 +655,8 @@ __global__ __launch_bounds__(256, NR == 1 ? 2 : 1) void rows_kernel(const Attend
       const auto value = [&](int t) {
         if constexpr (E4M3) {
           const int row = (lr >> 1) < 4 ? quarter * 4 + (lr >> 1) : 16 + quarter * 4 + (lr >> 1) - 4;
-          return unpack_e4m3(__builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((LDS_PTR(i32x2))(uintptr_t)(tv + row * Tile::ROW_B + ((t ^ Tile::swz(row)) << 4) + (lr & 1) * 8))), 1.f);
+          const uintptr_t from = tv + row * Tile::ROW_B + ((t ^ Tile::swz(row)) << 4) + (lr & 1) * 8;
+          return unpack_e4m3(__builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((LDS_PTR(i32x2))from)), 1.f);
         } else {
           const int row = quarter * 4 + (lr >> 2), ch = t * 2 + ((lr & 3) >> 1), in = (lr & 1) * 8;
           bf16x8 x;
@@ -661,7 +675,8 @@ __global__ __launch_bounds__(256, NR == 1 ? 2 : 1) void rows_kernel(const Attend
             for (int i = 0; i < 2; ++i) acc[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[n][i], acc[n][t], 0, 0, 0);
         }
       } else {
-        // a weight of 0 times a value that is not finite is NaN: of a tile that some row does not see whole, such values are counted apart, for the rows that see them
+        // a weight of 0 times a value that is not finite is NaN: of a tile that some row does not see whole, such values are counted apart, for the rows that
+        // see them
 #pragma unroll
         for (int t = 0; t < DH / 16; ++t) {
           bf16x8 vf = value(t), count;
@@ -738,7 +753,8 @@ __global__ __launch_bounds__(256, NR == 1 ? 2 : 1) void rows_kernel(const Attend
   }
 }
 
-// Joins the parts of split rows.  DH / 4 lanes hold a row; `side` such groups of lanes share a row's parts, four of which they have under way at a time, and are joined in LDS.
+// Joins the parts of split rows.  DH / 4 lanes hold a row; `side` such groups of lanes share a row's parts, four of which they have under way at a time, and
+// are joined in LDS.
 template <int DH>
 __global__ __launch_bounds__(1024) void combine_kernel(const AttendArgs a, int64_t rows, int rows_per_tile, int side) {
   constexpr int LPR = DH / 4;
@@ -816,11 +832,13 @@ __global__ __launch_bounds__(1024) void combine_kernel(const AttendArgs a, int64
   if (a.lse && d == 0) a.lse[((int64_t)b * a.Hq + at.h) * a.seq + at.t] = sum != 0.f ? (m + log2f(sum)) * kLn2 : -INFINITY;
 }
 
-// Which way a call goes: rows of a workgroup (16 or 32: rows_kernel; 128 or 256: tile_kernel), tiles of a pair's rows, and parts of a tile's keys.  Up to 32 rows the cache's bytes
-// are what counts and rows_kernel is as fast as they come; tile_kernel's matrix products of 32 rows a wave are for more.  Eight waves a workgroup make bf16 of e4m3 once for twice the rows
-// (two prompts of 8192 tokens, heads of 128: 1087 us, 1189 with four waves; bf16 itself 1102 and 1097), where that leaves every compute unit two workgroups to take.  As many parts as fill the chip once: of rows_kernel
-// the workgroups whose tiles the LDS holds (more of them, shorter, take longer: 8 rows over 16000 bf16 tokens 139 us in 4096 workgroups, 99 in 512),
-// of tile_kernel two a compute unit (three, which fit: 512 tokens behind 8000 85.6 -> 90.2 us, 8 rows of 128 behind up to 4000 77.0 -> 69.2); none shorter than kKeysLeast, and one only where there is no more than twice that, which a second launch would cost more than it saves.
+// Which way a call goes: rows of a workgroup (16 or 32: rows_kernel; 128 or 256: tile_kernel), tiles of a pair's rows, and parts of a tile's keys.  Up to 32
+// rows the cache's bytes are what counts and rows_kernel is as fast as they come; tile_kernel's matrix products of 32 rows a wave are for more.  Eight waves
+// a workgroup make bf16 of e4m3 once for twice the rows (two prompts of 8192 tokens, heads of 128: 1087 us, 1189 with four waves; bf16 itself 1102 and 1097),
+// where that leaves every compute unit two workgroups to take.  As many parts as fill the chip once: of rows_kernel the workgroups whose tiles the LDS holds
+// (more of them, shorter, take longer: 8 rows over 16000 bf16 tokens 139 us in 4096 workgroups, 99 in 512), of tile_kernel two a compute unit (three, which
+// fit: 512 tokens behind 8000 85.6 -> 90.2 us, 8 rows of 128 behind up to 4000 77.0 -> 69.2); none shorter than kKeysLeast, and one only where there is no
+// more than twice that, which a second launch would cost more than it saves.
 struct AttendPlan { int rows, tiles, splits, least; int64_t pairs; };
 constexpr int64_t kUnits = 256, kKeysLeast = 256;
 static int64_t most_splits(int64_t max_tokens) { return max_tokens <= 2 * kKeysLeast ? 1 : (max_tokens + kKeysLeast - 1) / kKeysLeast; }
@@ -837,8 +855,8 @@ static AttendPlan attend_plan(int64_t batch, int64_t seq, int64_t Hkv, int64_t g
   return p;
 }
 
-// Sums and statistics of the parts, in rows: pairs * tiles * splits * rows of a workgroup is within two workgroups a compute unit wherever there is a split, and within pairs * (rows, filled up) *
-// most_splits, neither of which falls as the call grows.
+// Sums and statistics of the parts, in rows: pairs * tiles * splits * rows of a workgroup is within two workgroups a compute unit wherever there is a split,
+// and within pairs * (rows, filled up) * most_splits, neither of which falls as the call grows.
 static int64_t rows_held(int64_t batch, int64_t seq, int64_t Hkv, int64_t group, int64_t dh, bool e4m3, int64_t max_tokens) {
   const AttendPlan p = attend_plan(batch, seq, Hkv, group, dh, e4m3, max_tokens);
   const int64_t rows = p.pairs * p.tiles, most = most_splits(max_tokens), bound = 2 * kUnits * p.rows;
