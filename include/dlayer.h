@@ -376,8 +376,8 @@ int linear_attention_step(const void* q, const void* k, const void* v, const flo
  * dropped, and what is read from there is not there.  Rows may share pages that nothing is written to (a common prefix).  start and
  * lengths are those of the token mixing above: start[b] tokens of row b are in the cache before the call, its lengths[b] new ones have
  * positions start[b] ...; NULL: 0, and seq.  What a page holds behind a row's last token is never read, padding neither.
- * The cache may exceed 4 GiB.  batch, seq: any positive numbers; max_pages * page_size and seq * n_q_heads stay below 2^31, batch *
- * n_kv_heads (times seq * (Hq / Hkv) / 16, rounded up) of the attention below 2^24.
+ * The cache may exceed 4 GiB.  batch, seq: any positive numbers; max_pages * page_size is at most 2^31 - 4096, seq * n_q_heads below 2^31 - 256,
+ * batch * n_kv_heads (times seq * (Hq / Hkv) / 16, rounded up) of the attention below 2^24.
  * ------------------------------------------------------------------------------------------ */
 
 #define DLAYER_CACHE_BF16 0

@@ -744,7 +744,8 @@ static int cache_ok(const char* who, const dlayer_kv_cache* c, int64_t seq, bool
           "%s: page_size must be a power of two from 16 to 4096", who);
   REQUIRE(c->dtype == DLAYER_CACHE_BF16 || c->dtype == DLAYER_CACHE_E4M3, "%s: unknown cache dtype", who);
   REQUIRE(c->n_kv_heads < 65536 && seq < ((int64_t)1 << 31) && (int64_t)c->batch * seq < ((int64_t)1 << 40), "%s: batch, seq or head count too large", who);
-  REQUIRE((int64_t)c->max_pages * c->page_size < (int64_t)1 << 31, "%s: a row's pages hold 2^31 tokens or more", who);
+  // the kernels count a row's keys, filled up to whole tiles, in 32 bits
+  REQUIRE((int64_t)c->max_pages * c->page_size <= ((int64_t)1 << 31) - 4096, "%s: a row's pages hold more than 2^31 - 4096 tokens", who);
   if (!memory) return 0;
   REQUIRE(c->k && c->v && aligned16(c->k) && aligned16(c->v), "%s: the cache's k or v is null or not 16-byte aligned", who);
   REQUIRE(c->page_table != nullptr, "%s: page_table is null", who);

@@ -42,6 +42,16 @@ def test_caches(K, changes):
     refused(K, "paged_attention_forward", c, A[0], None, None, S, HQ, 0.1, A[1], None, A[2], None)
 
 
+@pytest.mark.parametrize("page", [16, 4096])
+def test_the_longest_row(K, page):
+    """A row's keys, filled up to whole tiles of at most 128, are counted in 32 bits."""
+    columns = ((1 << 31) - 4096) // page
+    assert K.paged_attention_workspace_bytes(cache(K, page_size=page, max_pages=columns), 1, HKV) > 0
+    assert K.paged_attention_workspace_bytes(cache(K, page_size=page, max_pages=columns + 1), 1, HKV) == 0
+    c = C.byref(cache(K, page_size=page, max_pages=columns + 1))
+    assert "2^31" in refused(K, "paged_attention_forward", c, A[0], None, None, S, HQ, 0.1, A[1], None, A[2], None)
+
+
 def test_append(K):
     c = C.byref(cache(K))
     call = lambda *a: refused(K, "kv_cache_append", *a, None)  # noqa: E731

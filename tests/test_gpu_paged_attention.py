@@ -238,6 +238,22 @@ def test_a_cache_of_more_than_4_gib(K):
         assert torch.equal(got[0], ref[0]) and torch.equal(got[1], ref[1])
 
 
+@pytest.mark.parametrize("hq", [1, 64])
+def test_the_longest_row(K, hq):
+    """2^31 - 4096 tokens, all pages of the table the same one: what one page gives, and as often as it is there.  A lane adds up to 2^18 weights (1 at the
+    most) in fp32: the sum, which grows evenly, is off by at most 2^18 / 2 roundings of 2^-24 of it, 2^-7, and so is the lse; the products' sums
+    have 2^17 additions or fewer; weights and result are rounded to bf16."""
+    dh, page, columns = 32, 4096, (1 << 19) - 1
+    rng = np.random.default_rng(hq)
+    k, v, q = bits(rng, (1, 1, page, dh)), bits(rng, (1, 1, page, dh), mean=1.0), bits(rng, (1, 1, hq, dh))
+    cache = K.KVCache.of(dev_bf16(k), dev_bf16(v), torch.zeros((1, columns), dtype=torch.int32, device="cuda"))
+    o, lse = run(K, cache, dev_bf16(q), [page * columns - 1], None, hq, dh ** -0.5)
+    ref_o, ref_lse, mag, _ = og.attention({"k": si.bf16_bits_to_f64(k), "v": si.bf16_bits_to_f64(v), "page_table": np.zeros((1, 1), np.int64)},
+                                          si.bf16_bits_to_f64(q), [page - 1], None, dh ** -0.5)
+    assert np.abs(host_f64(o) - ref_o).max() <= ((2.0 ** -7 + 2.0 ** -7 + 2.0 ** -8 + 2.0 ** -7) * mag).max()
+    assert np.abs(host_f64(lse) - ref_lse - np.log(columns)).max() <= 2.0 ** -7 + 2.0 ** -18
+
+
 def ragged(rng, batch, longest, s, empty=True):
     """(tokens before, new tokens) of each row, some with none."""
     start, n = [int(x) for x in rng.integers(0, longest - s, batch)], [int(x) for x in rng.integers(0 if empty else 1, s + 1, batch)]
