@@ -397,7 +397,8 @@ typedef struct dlayer_kv_cache {
  * rope_base > 0: keys are rotated to their positions on the way (angle and pairings as in dlayer_cfg, evaluated in fp64), and the queries
  * q [B*S, Hq, dh] bf16 beside them, into q_out (may be q; padding is written as 0); q and q_out may both be NULL (n_q_heads is then
  * ignored).  rope_base 0: no rotation (of keys rotated before, as by qk_norm_rope_forward), q and q_out NULL.
- * Rounded once, from fp32, into the cache's type.  No two rows of the batch may write to one page; k and v must not overlap the cache.       */
+ * Rounded once, from fp32, into the cache's type.  No two rows of the batch may write to one page, nor a row to a page that its table names
+ * twice; k, v, q and q_out must not overlap the cache, nor q_out k or v.                                     */
 int kv_cache_append(const dlayer_kv_cache* cache, const void* q, const void* k, const void* v, const int64_t* start,
                     const int64_t* lengths, int64_t seq, int64_t n_q_heads, float rope_base, int32_t rope_layout, void* q_out,
                     void* stream);
@@ -412,9 +413,9 @@ int kv_cache_read(const dlayer_kv_cache* cache, const int64_t* start, const int6
  *   o = sum_s exp(scale q . k_s - lse) v_s,   lse = log sum_s exp(scale q . k_s)
  * with query head h reading KV head h / (Hq / Hkv).  One new token a row (generation) or many (a prompt, or a piece of one).
  * q, o [B*S, Hq, dh] bf16, lse [B, Hq, S] f32 or NULL.  A token that sees nothing, and padding, have o = 0 and lse = -infinity.
- * scale > 0.  A key or value that is not finite shows in the results of those tokens that see it, and of no others.  Weights are rounded to bf16
- * for their product with the values, sums are fp32 and divided at the end: values beyond some 1e33 may overflow in them.  o must not overlap q or
- * the cache.
+ * 0 < scale < 1e30; scores (scale q . k) below -5e29 count as none.  A key or value that is not finite shows in the results of those tokens that
+ * see it, and of no others.  Weights are rounded to bf16 for their product with the values, sums are fp32 and divided at the end: values beyond
+ * some 1e33 may overflow in them.  o and lse must not overlap q, the cache or each other.
  * workspace: paged_attention_workspace_bytes(cache, seq, n_q_heads), which reads the sizes of cache only and does not fall as batch, seq
  * or max_pages grows.                                                                                        */
 size_t paged_attention_workspace_bytes(const dlayer_kv_cache* cache, int64_t seq, int64_t n_q_heads);
@@ -429,7 +430,8 @@ int paged_attention_forward(const dlayer_kv_cache* cache, const void* q, const i
  * logprobs is NULL.  logprobs, entropy, lse [T] f32; top_ids [T, n_top] int64 and top_logprobs [T, n_top] f32: the n_top (0 .. 64, at
  * most V) likeliest tokens, likeliest first, of equal logits the lower index first.  Any output may be NULL; top_ids and top_logprobs are where n_top is 0.
  * Sums in fp32.  Logits of -infinity have probability 0; a row of nothing else has lse and logprobs of -infinity and entropy 0.  A row
- * that holds NaN or +infinity has NaN for results; NaN are not among its top_ids (which end in -1 where others are too few).
+ * that holds NaN or +infinity has NaN for results; NaN are not among its top_ids (which end in -1 where others are too few).  Results must not
+ * overlap logits or targets.  0 < inverse_temperature < 1e30.
  * T below 2^22, V and ld below 2^24 (and T * ld of the gradient below 2^37).  workspace: token_logprobs_workspace_bytes(T, V, n_top), at most
  * 528 KiB; it does not fall as T, V or n_top grows. */
 size_t token_logprobs_workspace_bytes(int64_t T, int64_t V, int64_t n_top);
@@ -440,8 +442,9 @@ int token_logprobs_forward(const void* logits, const int64_t* targets, int64_t T
 /* Gradient of logprobs and entropy: given d_logprobs and d_entropy [T] f32 (either may be NULL for zeros), the logits and targets of the forward and
  * the lse and entropy that it left,
  *   dlogits_v = inverse_temperature * (d_logprobs * [v == target] - p_v * (d_logprobs + d_entropy * (log p_v + entropy)))
- * dlogits [T, ld] bf16, may be logits; written as 0: columns behind the vocabulary, rows that are not scored, and rows of which a mask of -infinity
- * or of bf16's lowest value has left nothing (an lse of -1e30 or less).
+ * dlogits [T, ld] bf16, may be logits and must not overlap the other inputs; written as 0: columns behind the vocabulary, rows that are not
+ * scored, and rows of which a mask of -infinity or of bf16's lowest value has left nothing (an lse of -1e30 or less).  p is formed from lse, whose
+ * own rounding (2^-24 of it) it carries: z of some 1e4 and more leave p good to 1e-3 and less.
  * entropy may be NULL where d_entropy is, targets (every row counts) where d_logprobs is.                       */
 int token_logprobs_backward(const void* logits, const int64_t* targets, const float* lse, const float* entropy,
                             const float* d_logprobs, const float* d_entropy, int64_t T, int64_t V, int64_t ld,

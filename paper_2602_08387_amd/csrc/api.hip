@@ -755,6 +755,13 @@ static int cache_ok(const char* who, const dlayer_kv_cache* c, int64_t seq, bool
     REQUIRE(c->k_scale && c->v_scale && aligned16(c->k_scale) && aligned16(c->v_scale), "%s: an e4m3 cache needs k_scale and v_scale, 16-byte aligned", who);
   else
     REQUIRE(!c->k_scale && !c->v_scale, "%s: a bf16 cache has no k_scale and v_scale", who);
+  const uint64_t entries = (uint64_t)c->batch * c->max_pages * sizeof(int32_t);
+  REQUIRE(!overlap(c->k_scale, vectors, c->v_scale, vectors), "%s: the cache's k_scale and v_scale overlap", who);
+  for (const void* x : {c->k, c->v})
+    REQUIRE(!overlap(x, held, c->k_scale, vectors) && !overlap(x, held, c->v_scale, vectors) && !overlap(x, held, c->page_table, entries),
+            "%s: the cache's k and v overlap its k_scale, v_scale or page_table", who);
+  REQUIRE(!overlap(c->page_table, entries, c->k_scale, vectors) && !overlap(c->page_table, entries, c->v_scale, vectors),
+          "%s: the cache's page_table overlaps k_scale or v_scale", who);
   return 0;
 }
 static CacheCall cache_call(const dlayer_kv_cache* c, const int64_t* start, const int64_t* lengths) {
@@ -818,9 +825,12 @@ int paged_attention_forward(const dlayer_kv_cache* cache, const void* q, const i
                             float scale, void* o, float* lse, void* workspace, void* stream) {
   TRY(paged_shape_ok("paged_attention_forward", cache, seq, n_q_heads, true));
   REQUIRE_PTR(q); REQUIRE_PTR(o); REQUIRE_PTR(workspace);
-  REQUIRE(scale > 0.f && scale < INFINITY, "paged_attention_forward: scale must be positive and finite");
+  REQUIRE(scale > 0.f && scale < 1e30f, "paged_attention_forward: scale must be positive and below 1e30");
   const uint64_t of_q = heads_bytes(cache->batch, seq, n_q_heads, cache->head_dim);
   REQUIRE(!overlap(o, of_q, q, of_q) && !over_cache(cache, o, of_q), "paged_attention_forward: o must not overlap q or the cache");
+  const uint64_t of_lse = (uint64_t)cache->batch * seq * n_q_heads * sizeof(float);
+  REQUIRE(!overlap(lse, of_lse, q, of_q) && !overlap(lse, of_lse, o, of_q) && !over_cache(cache, lse, of_lse),
+          "paged_attention_forward: lse must not overlap q, o or the cache");
   TRY(check_device());
   return launch_paged_attention(cache_call(cache, start, lengths), q, seq, n_q_heads, scale, o, lse, workspace, (hipStream_t)stream);
 }
@@ -840,10 +850,15 @@ int token_logprobs_forward(const void* logits, const int64_t* targets, int64_t T
                            float* logprobs, float* entropy, float* lse, int64_t* top_ids, float* top_logprobs, void* workspace, void* stream) {
   TRY(logprobs_ok("token_logprobs_forward", T, V, ld));
   REQUIRE_PTR(logits); REQUIRE_PTR(workspace);
-  REQUIRE(inverse_temperature > 0.f && inverse_temperature < INFINITY, "token_logprobs_forward: inverse_temperature must be positive and finite");
+  REQUIRE(inverse_temperature > 0.f && inverse_temperature < 1e30f, "token_logprobs_forward: inverse_temperature must be positive and below 1e30");
   REQUIRE(n_top >= 0 && n_top <= 64 && n_top <= V, "token_logprobs_forward: n_top must be 0 .. 64 and at most V");
   REQUIRE(targets || !logprobs, "token_logprobs_forward: logprobs is of targets, which is null");
   REQUIRE(n_top || (!top_ids && !top_logprobs), "token_logprobs_forward: top_ids and top_logprobs are null where n_top is 0");
+  const struct { const void* p; uint64_t bytes; } out[] = {{logprobs, (uint64_t)T * 4}, {entropy, (uint64_t)T * 4}, {lse, (uint64_t)T * 4},
+                                                           {top_ids, (uint64_t)T * n_top * 8}, {top_logprobs, (uint64_t)T * n_top * 4}};
+  for (const auto& x : out)
+    REQUIRE(!overlap(x.p, x.bytes, logits, (uint64_t)T * ld * 2) && !overlap(x.p, x.bytes, targets, (uint64_t)T * 8),
+            "token_logprobs_forward: results must not overlap logits or targets");
   TRY(check_device());
   return launch_token_logprobs_fwd(LogprobsCall{logits, targets, T, V, ld, inverse_temperature}, (int)n_top, logprobs, entropy, lse, top_ids, top_logprobs,
                                    workspace, (hipStream_t)stream);
@@ -853,13 +868,16 @@ int token_logprobs_backward(const void* logits, const int64_t* targets, const fl
                             const float* d_entropy, int64_t T, int64_t V, int64_t ld, float inverse_temperature, void* dlogits, void* stream) {
   TRY(logprobs_ok("token_logprobs_backward", T, V, ld));
   REQUIRE_PTR(logits); REQUIRE_PTR(dlogits);
-  REQUIRE(inverse_temperature > 0.f && inverse_temperature < INFINITY, "token_logprobs_backward: inverse_temperature must be positive and finite");
+  REQUIRE(inverse_temperature > 0.f && inverse_temperature < 1e30f, "token_logprobs_backward: inverse_temperature must be positive and below 1e30");
   REQUIRE(lse != nullptr, "token_logprobs_backward: lse is null");
   REQUIRE(d_logprobs || d_entropy, "token_logprobs_backward: neither d_logprobs nor d_entropy is given");
   REQUIRE(T * ((ld + 8191) / 8192) < (int64_t)1 << 24, "token_logprobs_backward: T * ld reaches 2^37");      // a launch's threads, as above
   REQUIRE(targets || !d_logprobs, "token_logprobs_backward: d_logprobs is of targets, which is null");
   REQUIRE(entropy || !d_entropy, "token_logprobs_backward: d_entropy needs the forward's entropy");
   REQUIRE(!shifted(dlogits, logits, (uint64_t)T * ld * 2), "token_logprobs_backward: dlogits must be logits or not overlap it");
+  for (const void* x : {(const void*)lse, (const void*)entropy, (const void*)d_logprobs, (const void*)d_entropy})
+    REQUIRE(!overlap(dlogits, (uint64_t)T * ld * 2, x, (uint64_t)T * 4) && !overlap(dlogits, (uint64_t)T * ld * 2, targets, (uint64_t)T * 8),
+            "token_logprobs_backward: dlogits must not overlap targets, lse, entropy, d_logprobs or d_entropy");
   TRY(check_device());
   return launch_token_logprobs_bwd(LogprobsCall{logits, targets, T, V, ld, inverse_temperature}, lse, entropy, d_logprobs, d_entropy, dlogits,
                                    (hipStream_t)stream);

@@ -124,6 +124,33 @@ def test_logprobs(K):
     call(A[0], A[1], A[2], A[3], A[4], A[5], (1 << 22) - 1, 40000, 40000, 1.0, A[0])
 
 
+def test_memory_in_common(K):
+    """Buffers that a call would write to while others of its workgroups read them."""
+    held, scales, table = PAGES * HKV * PAGE * DH, PAGES * HKV * PAGE, B * COLUMNS * 4
+    for changes in (dict(v_scale=4 << 32, k_scale=(4 << 32) + 16), dict(k_scale=1 << 32), dict(v_scale=(2 << 32) + held - 16), dict(k_scale=(1 << 32) - scales + 16),
+                    dict(page_table=(2 << 32) + 64), dict(page_table=(4 << 32) + scales - 4), dict(k=(5 << 32) + table - 16)):
+        assert "overlap" in refused(K, "kv_cache_read", C.byref(cache(K, **changes)), None, None, S, A[0], A[1], None), changes
+    c, of_q = C.byref(cache(K)), B * S * HQ * DH * 2
+    for lse in (A[0] + of_q - 4, A[1], (1 << 32) + 4, (5 << 32) + 4, A[1] - 4):
+        assert "overlap" in refused(K, "paged_attention_forward", c, A[0], None, None, S, HQ, 0.1, A[1], lse, A[2], None)
+    T, V, ld, n = 5, 1001, 1008, 4
+    for i in range(5):
+        for at in (A[0] + T * ld * 2 - 4, A[1] + T * 8 - 8):
+            out = list(A[2:7])
+            out[i] = at
+            assert "overlap" in refused(K, "token_logprobs_forward", A[0], A[1], T, V, ld, 1.0, n, *out, A[7], None)
+    for i in range(1, 6):
+        inputs = list(A[:6])
+        inputs[i] = A[6] + 8
+        assert "overlap" in refused(K, "token_logprobs_backward", *inputs, T, V, ld, 1.0, A[6], None)
+
+
+def test_factors_whose_exponents_would_overflow(K):
+    assert "1e30" in refused(K, "paged_attention_forward", C.byref(cache(K)), A[0], None, None, S, HQ, 3e38, A[1], A[3], A[2], None)
+    assert "1e30" in refused(K, "token_logprobs_forward", A[0], A[1], 5, 1001, 1008, 3e38, 4, *A[2:7], A[7], None)
+    assert "1e30" in refused(K, "token_logprobs_backward", *A[:6], 5, 1001, 1008, 3e38, A[6], None)
+
+
 def test_workspaces_do_not_fall(K):
     size = lambda s=S, hq=HQ, **ch: K.paged_attention_workspace_bytes(cache(K, k=0, v=0, page_table=0, **ch), s, hq)  # noqa: E731
     for field, values in (("batch", (1, 2, 7, 8, 64, 65, 511, 512, 513, 4000)), ("max_pages", (1, 2, 3, 15, 16, 17, 100, 5000))):
