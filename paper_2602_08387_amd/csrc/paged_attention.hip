@@ -520,22 +520,6 @@ __global__ __launch_bounds__(256, NR == 1 ? 2 : 1) void rows_kernel(const Attend
     for (int t = 0; t < DH / 16; ++t) acc[n][t] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   if (u0 < u1) {
-    bool missing = false;
-    for (int i = (u0 * 32 >> c.shift) + threadIdx.x, n = (min(end, u1 * 32) - 1) >> c.shift; i <= n; i += 256)
-      missing |= (uint32_t)c.table[(int64_t)b * c.columns + i] >= (uint32_t)c.n_pages;
-    missing = any_of_workgroup(missing, reinterpret_cast<int*>(smem));
-
-    bf16x8 qf[NR][DH / 32];
-#pragma unroll
-    for (int n = 0; n < NR; ++n) {
-      const RowPlace at = row_place(a, hk, min(row0 + n * 16 + lr, n_rows - 1));
-      const bf16_t* qp = a.q + (((int64_t)b * a.seq + at.t) * a.Hq + at.h) * DH;
-      // e4m3: a 16-byte read of a key holds the slots of two steps
-#pragma unroll
-      for (int kk = 0; kk < DH / 32; ++kk)
-        qf[n][kk] = *reinterpret_cast<const bf16x8*>(qp + (E4M3 && DH >= 64 ? (kk >> 1) * 64 + quarter * 16 + (kk & 1) * 8 : kk * 32 + quarter * 8));
-    }
-
     const uint32_t own = lds_address(smem) + wave * (2 * STAGE);
     const auto load = [&](int u, int stage) {
       const Keys16 k16[2] = {keys16(c, b, hk, u * 32, end), keys16(c, b, hk, u * 32 + 16, end)};
@@ -551,11 +535,30 @@ __global__ __launch_bounds__(256, NR == 1 ? 2 : 1) void rows_kernel(const Attend
           asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(to), "v"(from) : "memory");
       }
     };
+    // the first tile is on its way before anything else is looked at
+    int u = u0 + wave, stage = 0;
+    if (u < u1) load(u, 0);
+
+    bf16x8 qf[NR][DH / 32];
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+      const RowPlace at = row_place(a, hk, min(row0 + n * 16 + lr, n_rows - 1));
+      const bf16_t* qp = a.q + (((int64_t)b * a.seq + at.t) * a.Hq + at.h) * DH;
+      // e4m3: a 16-byte read of a key holds the slots of two steps
+#pragma unroll
+      for (int kk = 0; kk < DH / 32; ++kk)
+        qf[n][kk] = *reinterpret_cast<const bf16x8*>(qp + (E4M3 && DH >= 64 ? (kk >> 1) * 64 + quarter * 16 + (kk & 1) * 8 : kk * 32 + quarter * 8));
+    }
+
+    // pages that do not exist: every wave looks for itself, without waiting for others
+    bool missing = false;
+    for (int i = (u0 * 32 >> c.shift) + lane, n = (min(end, u1 * 32) - 1) >> c.shift; i <= n; i += 64)
+      missing |= (uint32_t)c.table[(int64_t)b * c.columns + i] >= (uint32_t)c.n_pages;
+    missing = __builtin_amdgcn_ballot_w64(missing) != 0;
+
     // a byte of 255 is no power of two, and may stand where there is no key: finite, so that a weight of 0 times it is 0
     const auto scale_of = [](uint32_t four, int e) { return __uint_as_float(min((four >> (8 * e)) & 0xffu, 254u) << 23); };
 
-    int u = u0 + wave, stage = 0;
-    if (u < u1) load(u, 0);
     for (; u < u1; u += 4) {
       wait_loads<0>();
       if (u + 4 < u1) load(u + 4, stage ^ 1);
@@ -756,48 +759,48 @@ __global__ __launch_bounds__(256, NR == 1 ? 2 : 1) void rows_kernel(const Attend
 // Joins the parts of split rows.  DH / 4 lanes hold a row; `side` such groups of lanes share a row's parts, four of which they have under way at a time, and
 // are joined in LDS.
 template <int DH>
-__global__ __launch_bounds__(1024) void combine_kernel(const AttendArgs a, int64_t rows, int rows_per_tile, int side) {
+__global__ __launch_bounds__(1024) void combine_kernel(const AttendArgs a, int rows, int rows_per_tile, int side) {
   constexpr int LPR = DH / 4;
   __shared__ float stats[1024 / LPR][2], scaled[1024 / LPR];
   __shared__ f32x4 sums[1024];
   const PagedCache& c = a.cache;
   const int group = threadIdx.x / LPR, lane = threadIdx.x % LPR, here = blockDim.x / LPR;
-  const int64_t i = (int64_t)blockIdx.x * (here / side) + group / side;      // (pair, row of the pair)
+  const int i = blockIdx.x * (here / side) + group / side, within = min(i, rows - 1);      // (pair, row of the pair)
   const int per_pair = a.seq * a.group, d = lane * 4;
-  const int64_t pair = i / per_pair;
-  const int r = (int)(i % per_pair), b = (int)(pair / c.heads), hk = (int)(pair % c.heads);
-  const int64_t first = (pair * a.tiles + r / rows_per_tile) * a.splits;
+  const int pair = within / per_pair, r = within - pair * per_pair, b = pair / c.heads, hk = pair - b * c.heads;
+  const int at0 = (pair * a.tiles + r / rows_per_tile) * a.splits * rows_per_tile + r % rows_per_tile;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   float m = kNoKey, sum = 0.f;
-  if (i < rows && r < row_length(a.lengths, b, a.seq) * a.group) {
-    const int64_t at0 = first * rows_per_tile + r % rows_per_tile;
-    for (int s0 = group % side; s0 < a.splits; s0 += 4 * side) {
-      float ms[4], ls[4], top = m;
-      f32x4 x[4];
+  for (int s0 = group % side; s0 < a.splits; s0 += 4 * side) {
+    float ms[4], ls[4], top = m;
+    f32x4 x[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int s = min(s0 + k * side, a.splits - 1);
-        const int64_t at = at0 + (int64_t)s * rows_per_tile;
-        ms[k] = a.stats[at * 2];
-        ls[k] = s0 + k * side < a.splits ? a.stats[at * 2 + 1] : 0.f;
-        x[k] = *reinterpret_cast<const f32x4*>(a.sums + at * DH + d);        // of a part without keys: whatever is there, and not used
-      }
-#pragma unroll
-      for (int k = 0; k < 4; ++k) top = ls[k] == 0.f ? top : fmaxf(top, ms[k]);
-      const float old = sum == 0.f ? 0.f : fast_exp2(m - top);
-      sum *= old;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[e] = old == 0.f ? 0.f : acc[e] * old;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        if (ls[k] == 0.f) continue;
-        const float w = fast_exp2(ms[k] - top);
-        sum += w * ls[k];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[e] += w * x[k][e];
-      }
-      m = top;
+    for (int k = 0; k < 4; ++k) {
+      const int at = at0 + min(s0 + k * side, a.splits - 1) * rows_per_tile;
+      ms[k] = a.stats[at * 2];
+      ls[k] = s0 + k * side < a.splits ? a.stats[at * 2 + 1] : 0.f;
+      x[k] = *reinterpret_cast<const f32x4*>(a.sums + at * DH + d);        // of a part without keys: whatever is there, and not used
     }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) top = ls[k] == 0.f ? top : fmaxf(top, ms[k]);
+    const float old = sum == 0.f ? 0.f : fast_exp2(m - top);
+    sum *= old;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] = old == 0.f ? 0.f : acc[e] * old;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (ls[k] == 0.f) continue;
+      const float w = fast_exp2(ms[k] - top);
+      sum += w * ls[k];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] += w * x[k][e];
+    }
+    m = top;
+  }
+  // of padding, whose length is asked for beside the parts: nothing, whatever they hold
+  if (r >= row_length(a.lengths, b, a.seq) * a.group) {
+    sum = 0.f;
+    acc = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   if (side > 1) {
     const int own = group - group % side;              // of the row's groups the first
@@ -896,8 +899,8 @@ static int launch_attend(const AttendArgs& a, const AttendPlan& p, hipStream_t s
   int side = 1;
   while (side < 1024 / LPR && side * 4 < p.splits) side *= 2;
   const int threads = side * LPR > 256 ? side * LPR : 256, per = threads / (side * LPR);
-  const int64_t rows = p.pairs * a.seq * a.group;
-  hipLaunchKernelGGL((combine_kernel<DH>), dim3((unsigned)((rows + per - 1) / per)), dim3(threads), 0, st, a, rows, p.rows, side);
+  const int64_t rows = p.pairs * a.seq * a.group;              // with parts, the sums of 512 workgroups of 128 rows at most: indices fit 32 bits
+  hipLaunchKernelGGL((combine_kernel<DH>), dim3((unsigned)((rows + per - 1) / per)), dim3(threads), 0, st, a, (int)rows, p.rows, side);
   return check_launch("paged_attention_forward, joining parts");
 }
 
