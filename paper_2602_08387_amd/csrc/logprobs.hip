@@ -48,6 +48,11 @@ __device__ __forceinline__ bool row_counts(const LogprobsArgs& a, int64_t row) {
   return t >= 0 && t < a.V;
 }
 
+// The logit of a row's target; asked for early, since it takes two loads one after the other.
+__device__ __forceinline__ float scored_logit(const LogprobsArgs& a, int64_t row) {
+  return a.logprobs ? (float)a.logits[row * a.ld + a.targets[row]] : 0.f;
+}
+
 // Keys: larger for a larger logit, for equal ones for the lower index; 0 is below every key.  -0 and 0 are equal.
 __device__ __forceinline__ uint64_t key_of(uint32_t bits, int index) {
   const int s = (int)(int16_t)bits, order = s >= 0 ? s : -32768 - s;
@@ -98,13 +103,13 @@ __device__ __forceinline__ Sums relative_to(const Sums& v, float top, float inve
   return {top, f * v.s, f * (v.u + d * v.s)};
 }
 
-// A row's results from its sums; list: its likeliest, one a lane of the calling wave.
-__device__ __forceinline__ void finish_row(const LogprobsArgs& a, int64_t row, const Sums& v, uint64_t list, int lane) {
+// A row's results from its sums; scored: its target's logit; list: its likeliest, one a lane of the calling wave.
+__device__ __forceinline__ void finish_row(const LogprobsArgs& a, int64_t row, float scored, const Sums& v, uint64_t list, int lane) {
   const bool empty = v.m == -INFINITY && v.s == 0.f;    // nothing but -inf
   const float log_s = empty ? 0.f : logf(v.s);
   const auto logp = [&](float x) { return x == -INFINITY ? (v.s == v.s ? -INFINITY : v.s) : (x - v.m) * a.inverse - log_s; };
   if (lane == 0) {
-    if (a.logprobs) a.logprobs[row] = logp((float)a.logits[row * a.ld + a.targets[row]]);
+    if (a.logprobs) a.logprobs[row] = logp(scored);
     if (a.entropy) a.entropy[row] = empty ? 0.f : log_s - kLpLn2 * (v.u / v.s);
     if (a.lse) a.lse[row] = empty ? -INFINITY : v.m * a.inverse + log_s;
   }
@@ -194,7 +199,6 @@ __global__ __launch_bounds__(64 * WAVES, 6) void logprobs_kernel(const LogprobsA
   const u32x4* in = reinterpret_cast<const u32x4*>(a.logits + row * a.ld);
   const int whole = a.V >> 3, vectors = (a.V + 7) >> 3;          // the last vector may hold columns behind the vocabulary
   const int first = part * a.per_part, end = min(vectors, first + a.per_part);
-
   Sums v{-INFINITY, 0.f, 0.f};
   TopList top;
   top.buffer = buffer[TOP ? wave : 0];
@@ -316,7 +320,7 @@ __global__ __launch_bounds__(64 * WAVES, 6) void logprobs_kernel(const LogprobsA
     for (int i = 1; i < kLpWaves; ++i) list = join_descending(list, lists[i][lane], lane);
   }
   if (a.parts == 1) {
-    finish_row(a, row, sum, list, lane);
+    finish_row(a, row, scored_logit(a, row), sum, list, lane);
   } else {
     const int64_t at = row * a.parts + part;
     if (lane == 0) *reinterpret_cast<f32x4*>(a.part_sums + at * 4) = f32x4{sum.m, sum.s, sum.u, 0.f};
@@ -324,38 +328,47 @@ __global__ __launch_bounds__(64 * WAVES, 6) void logprobs_kernel(const LogprobsA
   }
 }
 
-// Joins the parts of a row: a workgroup a row, whose waves take some lists each and then halve their number.
+// Joins the parts of a row: a workgroup a row, whose waves take some lists each and then halve their number; the last wave joins the sums.  What can be asked
+// for without knowing more is asked for first: the time is that of loads and exchanges one after the other.
 constexpr int kLpJoinWaves = 16;
 template <bool TOP>
 __global__ __launch_bounds__(64 * kLpJoinWaves) void logprobs_join_kernel(const LogprobsArgs a) {
   __shared__ uint64_t lists[TOP ? kLpJoinWaves / 2 : 1][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  __shared__ float joined[3];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const int64_t row = blockIdx.x;
+  uint64_t some[4];
+  const uint64_t* from = a.part_top + row * a.parts * a.n_top + lane;
+  const auto load = [&](int i0) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) some[k] = lane < a.n_top && i0 + k * waves < a.parts ? from[(int64_t)(i0 + k * waves) * a.n_top] : 0;
+  };
+  if constexpr (TOP) load(wave);
+  const f32x4* parts = reinterpret_cast<const f32x4*>(a.part_sums) + row * a.parts;
+  const f32x4 own = wave == waves - 1 && lane < a.parts ? parts[lane] : f32x4{-INFINITY, 0.f, 0.f, 0.f};
   if (!row_counts(a, row)) {
     finish_uncounted(a, row);
     return;
   }
-  Sums sum{-INFINITY, 0.f, 0.f};
-  if (wave == 0) {
-    const f32x4* parts = reinterpret_cast<const f32x4*>(a.part_sums) + row * a.parts;
-    float m = -INFINITY;
-    for (int i = lane; i < a.parts; i += 64) m = fmaxf(m, parts[i][0]);
-    sum.m = wave_max(m);
-    for (int i = lane; i < a.parts; i += 64) {
-      const Sums p = relative_to(Sums{parts[i][0], parts[i][1], parts[i][2]}, sum.m, a.inverse_log2e);
+  const float scored = wave == 0 ? scored_logit(a, row) : 0.f;
+  if (wave == waves - 1) {
+    float m = own[0];
+    for (int i = lane + 64; i < a.parts; i += 64) m = fmaxf(m, parts[i][0]);
+    m = wave_max(m);
+    Sums sum = relative_to(Sums{own[0], own[1], own[2]}, m, a.inverse_log2e);
+    for (int i = lane + 64; i < a.parts; i += 64) {
+      const Sums p = relative_to(Sums{parts[i][0], parts[i][1], parts[i][2]}, m, a.inverse_log2e);
       sum.s += p.s;
       sum.u += p.u;
     }
     sum.s = wave_sum(sum.s);
     sum.u = wave_sum(sum.u);
+    if (lane == 0) { joined[0] = m; joined[1] = sum.s; joined[2] = sum.u; }
   }
   uint64_t list = 0;
   if constexpr (TOP) {
-    const uint64_t* from = a.part_top + row * a.parts * a.n_top + lane;
     for (int i0 = wave; i0 < a.parts; i0 += 4 * waves) {
-      uint64_t some[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) some[k] = lane < a.n_top && i0 + k * waves < a.parts ? from[(int64_t)(i0 + k * waves) * a.n_top] : 0;
+      if (i0 != wave) load(i0);
 #pragma unroll
       for (int k = 0; k < 4; ++k) list = join_descending(list, some[k], lane);
     }
@@ -365,8 +378,10 @@ __global__ __launch_bounds__(64 * kLpJoinWaves) void logprobs_join_kernel(const 
       if (wave < half) list = join_descending(list, lists[wave][lane], lane);
       __syncthreads();
     }
+  } else {
+    __syncthreads();
   }
-  if (wave == 0) finish_row(a, row, sum, list, lane);
+  if (wave == 0) finish_row(a, row, scored, Sums{joined[0], joined[1], joined[2]}, list, lane);
 }
 
 // Parts of a row: where there are fewer rows than fill the chip, of no less than four vectors a lane of a wave.
