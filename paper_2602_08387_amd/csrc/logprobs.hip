@@ -4,7 +4,7 @@
 //   lse = M + ln S;  logp(v) = (z_v - M) - ln S;  entropy = ln S - U / S                          (no difference of large numbers)
 //   dx_v = ([v = target] dlp - p_v (dlp + dH (logp_v + entropy))) / temperature
 //
-// Forward: one pass, bound by the reading of the logits (2 bytes each; some 10 vector instructions an element, of which the exponential takes four). A thread
+// Forward: one pass, bound by the reading of the logits (2 bytes each; some 11 issue slots of the vector units an element, of which the exponential takes four). A thread
 // keeps S and U relative to its own running maximum, which it raises once in 32 elements.  Exponents are formed as (x - max) times a constant: of a row that
 // is all but certain S is then 1 and a little, exactly, where one FMA against the rounded product max * constant would be off by that rounding (and infinite
 // for a row masked with the type's lowest value).
@@ -16,8 +16,8 @@
 //
 // Few rows are cut into parts, joined by a second kernel.
 //
-// Measured, 128256 tokens a row: 4096 rows 215 us without the likeliest, 222 with 5 (1.05 GB, 4.7 TB/s: memory), 255 with 20, 294 with 64 (vector
-// instructions); one row 13.9 with 20 (two launches, 8.7 and 5.7 us: loads, exchanges and barriers one after the other).  The gradient of 4096 rows 395 us
+// Measured, 128256 tokens a row: 4096 rows 188 us without the likeliest (1.05 GB, 5.6 TB/s: memory), 210 with 5, 250 with 20, 294 with 64 (vector
+// instructions); one row 13.7 with 20 (two launches, 8.5 and 5.4 us: loads, exchanges and barriers one after the other).  The gradient of 4096 rows 395 us
 // (2.1 GB, 5.3 TB/s: memory).
 #include "common.h"
 #include "kernels.h"
@@ -180,9 +180,10 @@ struct TopList {
 };
 
 // WAVES: of a workgroup.  One wave takes a short part alone, without waiting for others and without joining their lists (64 rows of 32000, 20 likeliest: 13.8
-// us, 16.7 with four); of longer parts, or with many likeliest to sort, four share the work and their bounds.
+// us, 16.7 with four); of longer parts, or with many likeliest to sort, four share the work and their bounds.  Registers for five waves a SIMD: for six
+// some go to memory (4096 rows of 128256, 5 likeliest 219 us, 210 with five; 64 likeliest 286 and 294).
 template <bool TOP, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 6) void logprobs_kernel(const LogprobsArgs a) {
+__global__ __launch_bounds__(64 * WAVES, 5) void logprobs_kernel(const LogprobsArgs a) {
   constexpr int kLpWaves = WAVES, kLpThreads = 64 * WAVES;
   __shared__ float red[kLpWaves][4];
   __shared__ int bound, quarter[kLpWaves];   // the largest of the waves' n-th, and the (n / 4)-th of each
@@ -223,14 +224,24 @@ __global__ __launch_bounds__(64 * WAVES, 6) void logprobs_kernel(const LogprobsA
           if (c * 8 + e >= a.V) w[i][e >> 1] = (e & 1) ? (w[i][e >> 1] & 0xffffu) | 0xff800000u : (w[i][e >> 1] & 0xffff0000u) | 0xff80u;
       }
     }
-    float vmax[kLpUnroll], mx = -INFINITY;
+    const auto logit = [&](int i, int e) { return __uint_as_float((e & 1) ? w[i][e >> 1] & 0xffff0000u : w[i][e >> 1] << 16); };
+    // the largest, one instruction for two elements, which lets NaN through; a wave that has one looks again without
+    float vmax[kLpUnroll], mx;
 #pragma unroll
     for (int i = 0; i < kLpUnroll; ++i) {
-      float t = -INFINITY;
+      vmax[i] = logit(i, 0);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) t = fmaxf(t, fmaxf(__uint_as_float(w[i][e] << 16), __uint_as_float(w[i][e] & 0xffff0000u)));
-      vmax[i] = t;
-      mx = fmaxf(mx, t);
+      for (int e = 1; e < 8; ++e) vmax[i] = __builtin_elementwise_maximum(vmax[i], logit(i, e));
+      mx = i ? __builtin_elementwise_maximum(mx, vmax[i]) : vmax[i];
+    }
+    if (__builtin_amdgcn_ballot_w64(mx != mx)) {
+#pragma unroll
+      for (int i = 0; i < kLpUnroll; ++i) {
+        vmax[i] = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) vmax[i] = fmaxf(vmax[i], logit(i, e));
+        mx = i ? fmaxf(mx, vmax[i]) : vmax[i];
+      }
     }
     if (mx > v.m) v = relative_to(v, mx, a.inverse_log2e);
     const float ref = v.m == -INFINITY ? 0.f : v.m;
@@ -238,8 +249,7 @@ __global__ __launch_bounds__(64 * WAVES, 6) void logprobs_kernel(const LogprobsA
     for (int i = 0; i < kLpUnroll; ++i)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float x = __uint_as_float((e & 1) ? w[i][e >> 1] & 0xffff0000u : w[i][e >> 1] << 16);
-        const float t = (x - ref) * a.inverse_log2e, p = __builtin_amdgcn_exp2f(t);
+        const float t = (logit(i, e) - ref) * a.inverse_log2e, p = __builtin_amdgcn_exp2f(t);
         v.s += p;
         v.u = __builtin_fmaf(p, fmaxf(t, -1e4f), v.u);           // t may be -inf where p is 0
       }

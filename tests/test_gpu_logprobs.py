@@ -292,3 +292,20 @@ def test_nothing_is_written_around_the_outputs(K):
         for x, m in zip(out + [d], sizes + [T * ld]):
             assert (x[:guard] == 7).all() and (x[guard + m:] == 7).all()
         assert (ws[:guard] == 77).all() and (ws[guard + nbytes:] == 77).all()
+
+
+@pytest.mark.parametrize("T,V,n_top", [(1, 33000, 20), (1, 3000, 5), (1100, 20000, 5)])
+def test_nan_of_every_kind_hide_no_token(K, T, V, n_top):
+    """Quiet and signalling NaN of both signs among the logits, one of them beside the likeliest: the row's sums are NaN, its likeliest those of the rest."""
+    rng = np.random.default_rng(V)
+    b = si.f32_to_bf16_bits((rng.standard_normal((T, V)) * 2.5).astype(np.float32))
+    z, best = si.bf16_bits_to_f64(b), int(np.argmax(si.bf16_bits_to_f64(b)[0]))
+    where = [best ^ 1, 17, V // 2 | 1, V - 1]
+    where = [w if w != best else w - 2 for w in where]
+    b[0, where] = 0x7F81, 0xFF81, 0x7FC0, 0xFFFF
+    got = forward(K, dev_bf16(b), torch.full((T,), best, device="cuda"), V, 1.0, n_top)
+    assert all(x[0].isnan() for x in got[:3]) and got[4][0].isnan().all()
+    z[0, where] = -np.inf
+    assert np.array_equal(got[3][0].cpu().numpy(), np.argsort(-z[0], kind="stable")[:n_top])
+    if T > 1:
+        assert all(x[1:].isfinite().all() for x in got[:3])
