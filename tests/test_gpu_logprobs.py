@@ -2,8 +2,8 @@
 
 Tolerances.  A row's exponents t = z - max are formed in fp32: off by a few units of 2^-24 of t, and the sums of up to 2^18 terms in blocks are off by 2^-18 at the
 very most; lse and log-probabilities by that and by their own rounding, 2^-23 of their parts' magnitude: 4e-6 + 3e-7 * (|z| + |max|).  Entropy = ln S - U / S, both at least 0 and
-so no more than it: each is off by 2^-18 of itself, and ln S by 2^-23 more, since S is 1 and a little in a row that is all but certain and holds no more than its own rounding
-of that little.  1e-5 * entropy + 2.5e-7.  Gradient: p is off by 2^-24 of |z| + |lse| and a few units, its products round, then one rounding to bf16
+so no more than it: each is off by 2^-18 of itself, and ln S by some units of 2^-24 more, since S is 1 and a little in a row that is all but certain and every addition to it rounds
+by as much; either way, so that four are allowed for.  1e-5 * entropy + 2.5e-7.  Gradient: p is off by 2^-24 of |z| + |lse| and a few units, its products round, then one rounding to bf16
 (2^-8 of the value), of a sum whose two terms at the target may cancel: 2^-8 |d| + 4e-6 * (1 + |z| + |lse|) of the terms' magnitudes.
 """
 import numpy as np
