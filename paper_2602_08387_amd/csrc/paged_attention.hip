@@ -14,11 +14,11 @@
 // Rows behind a tile's last key and pages that do not exist are behind the end of the buffer that a load is given, and read as zeros: what a page holds
 // behind a row's last token is never read.
 //
-// What bounds them (32 query and 8 KV heads of 128).  rows_kernel: memory, 256 rows of up to 4096 bf16 tokens in 373 us (5.6 TB/s of keys and values), one
-// row over 32768 e4m3 tokens in 20.5 (15 us, 4.6 TB/s, and 5 for joining 64 parts).  tile_kernel: two prompts of 8192 tokens in 1.00 to 1.06 ms (1040 to 1100
-// TFLOP/s), the clock at 1.7 GHz by the card's power limit; with two workgroups a compute unit the matrix units were busy 47 % of the cycles and the vector
-// units, exponentials above all, 43 %; the third workgroup brings more of that side by side.  The next tile's scores beside this tile's exponentials within a
-// wave: 6 % fewer cycles, at a lower clock, and no less time.
+// What bounds them (32 query and 8 KV heads of 128).  rows_kernel: memory, 256 rows of up to 4096 bf16 tokens in 374 us (5.8 TB/s of keys and values), one
+// row over 32768 e4m3 tokens in 20.1 (15.5 us, 4.4 TB/s, and 4.6 for joining 64 parts).  tile_kernel: two prompts of 8192 tokens in 1.00 to 1.06 ms (1040 to
+// 1100 TFLOP/s), the clock at 1.6 to 1.7 GHz by the card's power limit, the matrix units busy 59 % of the cycles (47 % with two workgroups a compute unit) and
+// the vector units, exponentials above all, 54 %.  The next tile's scores beside this tile's exponentials within a wave: 6 % fewer cycles, at a lower clock,
+// and no less time.
 #include "attention_tile.h"
 #include "common.h"
 #include "kernels.h"
@@ -177,8 +177,8 @@ __device__ __forceinline__ bool any_not_finite(const bf16x8& v) {
 
 // Whether the tiles of values share one place in LDS, so that three workgroups fit a compute unit (48 KB each at heads of 128): of bf16 with four waves.
 // Values are then asked for when the last tile's are done with, and waited for behind the exponentials (two prompts of 8192 tokens, 32 and 8 heads of 128:
-// 1060 us with two workgroups, 993 with three; as many products under way beside exponentials of others is what counts: the matrix units were busy 47 % of
-// the cycles).
+// 1060 us with two workgroups, 993 with three: products of some beside exponentials of others is what counts).  Over e4m3 this loses (two prompts 1079 us with
+// eight waves, 1243 so): bf16 is made of e4m3 between scores and products then, and for half as many rows.
 template <bool E4M3, int NW>
 constexpr bool kThin = !E4M3 && NW == 4;
 template <int DH, bool E4M3, int NW>
