@@ -99,7 +99,7 @@ __device__ __forceinline__ i32x4 descriptor(const void* p, uint32_t bytes) {
 }
 __device__ __forceinline__ void load_to_lds(const i32x4& from, uint32_t to, int offset) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(offset), "s"(from)
-               : "memory");
+               : "memory", "m0");
 }
 // Until LEFT of them are under way.  The builtin tells the compiler that its own loads are done too (it does not read assembly, and would wait for them, and so for
 // the loads to LDS, at their next use).
@@ -480,7 +480,7 @@ struct HeldTile {
       const uint32_t dst = to + (group * (LOADS / 2) + i) * (64 * WIDTH);
       if constexpr (WIDTH == 16) load_to_lds(from, dst, offset);
       else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(dst)), "v"(offset), "s"(from)
-                        : "memory");
+                        : "memory", "m0");
     }
   }
 };
@@ -532,7 +532,7 @@ __global__ __launch_bounds__(256, NR == 1 ? 2 : 1) void rows_kernel(const Attend
         const uint8_t* from = (lane & 8 ? c.scale[1] : c.scale[0]) + (lane & 4 ? k16[1].vec : k16[0].vec) + (lane & 3) * 4;
         const uint32_t to = __builtin_amdgcn_readfirstlane(own + stage * STAGE + 2 * Tile::BYTES);
         if (lane < 16)
-          asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(to), "v"(from) : "memory");
+          asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(to), "v"(from) : "memory", "m0");
       }
     };
     // the first tile is on its way before anything else is looked at

@@ -1,0 +1,32 @@
+"""What the compiler makes of the paged attention's assembly (compiled for gfx950 here, nothing is run)."""
+import os
+import re
+import shutil
+import subprocess
+
+import pytest
+
+from paper_2602_08387_amd import build as b
+
+HIPCC = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
+SOURCE = os.path.join(b.CSRC, "paged_attention.hip")
+
+
+def _compiled(folder, *args):
+    out = folder / "out"
+    r = subprocess.run([HIPCC, *b.FLAGS, "--offload-device-only", "-S", *args, SOURCE, "-o", str(out)], capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-3000:]
+    return out.read_text()
+
+
+@pytest.fixture(scope="module")
+def ir(tmp_path_factory):
+    return _compiled(tmp_path_factory.mktemp("ir"), "-emit-llvm")
+
+
+def test_loads_to_lds_say_that_they_write_m0(ir):
+    """The assembly sets m0; where that is not declared, the compiler may keep a value of its own in it across the block."""
+    blocks = re.findall(r'asm sideeffect "([^"]*)", "([^"]*)"', ir)
+    setting = [(text, constraints) for text, constraints in blocks if "m0" in text]
+    assert len(setting) > 100 and all(" lds" in text or "_lds_" in text for text, _ in setting)
+    assert all("~{m0}" in constraints.split(",") for _, constraints in setting), setting[0]
