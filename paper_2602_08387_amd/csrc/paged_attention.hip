@@ -90,7 +90,8 @@ __device__ __forceinline__ Work work_of(const AttendArgs& a, int id, int queue, 
 
 // Memory to LDS without registers between, 16 bytes a lane: lane l's go to `to` + 16 l.  As assembly, which names no register as an output: behind the builtin the
 // compiler waits for all such loads in front of every transposing read, of which it does not know that it stays clear of the stage being
-// filled.  The kernels wait for them themselves (wait_loads), so nothing counts on the compiler here.
+// filled.  The kernels wait for them themselves (wait_loads), so nothing counts on the compiler here.  Nor does it count the distance that a buffer load keeps
+// from a vector instruction that wrote its descriptor, as one does that brings a spilled scalar register back: five wait states, of which writing m0 is one.
 typedef int32_t i32x2 __attribute__((ext_vector_type(2)));
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ i32x4 descriptor(const void* p, uint32_t bytes) {
@@ -98,7 +99,7 @@ __device__ __forceinline__ i32x4 descriptor(const void* p, uint32_t bytes) {
   return i32x4{(int)(uint32_t)at, (int)((uint32_t)(at >> 32) & 0xffffu), (int)bytes, 0x00020000};
 }
 __device__ __forceinline__ void load_to_lds(const i32x4& from, uint32_t to, int offset) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(offset), "s"(from)
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(offset), "s"(from)
                : "memory", "m0");
 }
 // Until LEFT of them are under way.  The builtin tells the compiler that its own loads are done too (it does not read assembly, and would wait for them, and so for
@@ -479,7 +480,7 @@ struct HeldTile {
       const int offset = row * ROW_B + ch * 16 + at % 16;
       const uint32_t dst = to + (group * (LOADS / 2) + i) * (64 * WIDTH);
       if constexpr (WIDTH == 16) load_to_lds(from, dst, offset);
-      else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(dst)), "v"(offset), "s"(from)
+      else asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(dst)), "v"(offset), "s"(from)
                         : "memory", "m0");
     }
   }

@@ -30,3 +30,23 @@ def test_loads_to_lds_say_that_they_write_m0(ir):
     setting = [(text, constraints) for text, constraints in blocks if "m0" in text]
     assert len(setting) > 100 and all(" lds" in text or "_lds_" in text for text, _ in setting)
     assert all("~{m0}" in constraints.split(",") for _, constraints in setting), setting[0]
+
+
+def _blocks(code):
+    """Instructions of each assembly block."""
+    return [[line.strip() for line in text.splitlines() if line.strip()] for text in re.findall(r";;?#ASMSTART\n(.*?);;?#ASMEND", code, re.S)]
+
+
+@pytest.fixture(scope="module")
+def code(tmp_path_factory):
+    return _compiled(tmp_path_factory.mktemp("code"))
+
+
+def test_loads_to_lds_keep_their_distance_from_who_wrote_their_descriptor(code):
+    """A buffer load reads its descriptor's scalar registers right only five wait states behind a vector instruction that wrote them, such as the one that
+    brings a spilled register back.  The compiler counts none in front of an instruction that it does not see: the block holds them itself."""
+    loads = [block for block in _blocks(code) if block and block[-1].startswith("buffer_load")]
+    assert len(loads) > 100
+    for block in loads:
+        states = sum(int(op.split()[1], 0) + 1 if op.startswith("s_nop") else 1 for op in block[:-1])
+        assert states >= 5, block
