@@ -109,6 +109,12 @@ __device__ __forceinline__ void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory");
   if constexpr (LEFT == 0) __builtin_amdgcn_s_waitcnt(0x0f70);
 }
+// Until no load and no read of LDS of this wave is: in front of loads to a place that the wave has read from, where no barrier lies between.  Its reads may have been
+// issued without having been served (what uses them can be moved behind).
+__device__ __forceinline__ void wait_loads_and_reads() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0070);
+}
 __device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(LDS_PTR(const char))p; }
 
 // Whether x holds for a thread of the workgroup; word: of LDS.
@@ -561,7 +567,7 @@ __global__ __launch_bounds__(256, NR == 1 ? 2 : 1) void rows_kernel(const Attend
     const auto scale_of = [](uint32_t four, int e) { return __uint_as_float(min((four >> (8 * e)) & 0xffu, 254u) << 23); };
 
     for (; u < u1; u += 4) {
-      wait_loads<0>();
+      wait_loads_and_reads();
       if (u + 4 < u1) load(u + 4, stage ^ 1);
       const uint32_t tk = own + stage * STAGE, tv = tk + Tile::BYTES;
       const int kv0 = u * 32;

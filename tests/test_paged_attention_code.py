@@ -50,3 +50,15 @@ def test_loads_to_lds_keep_their_distance_from_who_wrote_their_descriptor(code):
     for block in loads:
         states = sum(int(op.split()[1], 0) + 1 if op.startswith("s_nop") else 1 for op in block[:-1])
         assert states >= 5, block
+
+
+def test_a_wave_is_done_with_a_stage_before_it_loads_into_it(code):
+    """rows_kernel's waves load a stage that they read from a round before, without a barrier between: what they read has to be waited for in the source, and not where the
+    compiler happens to use it."""
+    kernels = re.findall(r"^(_ZN2dl11rows_kernel\w+):", code, re.M)
+    assert len(kernels) == 12, kernels
+    for name in kernels:
+        blocks = [b for b in _blocks(code[code.index(f"\n{name}:"):].split(".Lfunc_end")[0]) if b]
+        waits = [i for i, b in enumerate(blocks) if b[0].startswith("s_waitcnt")]
+        assert waits and all("vmcnt(0)" in blocks[i][0] and "lgkmcnt(0)" in blocks[i][0] for i in waits), (name, [blocks[i] for i in waits])
+        assert any("_load" in b[-1] for b in blocks[waits[-1]:]), name
