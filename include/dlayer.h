@@ -415,7 +415,7 @@ int kv_cache_read(const dlayer_kv_cache* cache, const int64_t* start, const int6
  * q, o [B*S, Hq, dh] bf16, lse [B, Hq, S] f32 or NULL.  A token that sees nothing, and padding, have o = 0 and lse = -infinity.
  * 0 < scale < 1e30; scores (scale q . k) below -5e29 count as none.  A key or value that is not finite shows in the results of those tokens that
  * see it, and of no others.  Weights are rounded to bf16 for their product with the values, sums are fp32 and divided at the end: values beyond
- * some 1e33 may overflow in them.  o and lse must not overlap q, the cache or each other.
+ * some 1e33 may overflow in them.  o, lse and workspace must not overlap q, the cache or each other, nor workspace start or lengths.
  * workspace: paged_attention_workspace_bytes(cache, seq, n_q_heads), which reads the sizes of cache only and does not fall as batch, seq
  * or max_pages grows.                                                                                        */
 size_t paged_attention_workspace_bytes(const dlayer_kv_cache* cache, int64_t seq, int64_t n_q_heads);
@@ -430,8 +430,8 @@ int paged_attention_forward(const dlayer_kv_cache* cache, const void* q, const i
  * logprobs is NULL.  logprobs, entropy, lse [T] f32; top_ids [T, n_top] int64 and top_logprobs [T, n_top] f32: the n_top (0 .. 64, at
  * most V) likeliest tokens, likeliest first, of equal logits the lower index first.  Any output may be NULL; top_ids and top_logprobs are where n_top is 0.
  * Sums in fp32.  Logits of -infinity have probability 0; a row of nothing else has lse and logprobs of -infinity and entropy 0.  A row
- * that holds NaN or +infinity has NaN for results; NaN are not among its top_ids (which end in -1 where others are too few).  Results must not
- * overlap logits or targets.  0 < inverse_temperature < 1e30.
+ * that holds NaN or +infinity has NaN for results; NaN are not among its top_ids (which end in -1 where others are too few).  Results and workspace
+ * must not overlap logits or targets, nor workspace the results.  0 < inverse_temperature < 1e30.
  * T below 2^22, V and ld below 2^24 (and T * ld of the gradient below 2^37).  workspace: token_logprobs_workspace_bytes(T, V, n_top), at most
  * 528 KiB; it does not fall as T, V or n_top grows. */
 size_t token_logprobs_workspace_bytes(int64_t T, int64_t V, int64_t n_top);

@@ -831,6 +831,11 @@ int paged_attention_forward(const dlayer_kv_cache* cache, const void* q, const i
   const uint64_t of_lse = (uint64_t)cache->batch * seq * n_q_heads * sizeof(float);
   REQUIRE(!overlap(lse, of_lse, q, of_q) && !overlap(lse, of_lse, o, of_q) && !over_cache(cache, lse, of_lse),
           "paged_attention_forward: lse must not overlap q, o or the cache");
+  const uint64_t of_ws = paged_attention_workspace(cache->batch, seq, n_q_heads, cache->n_kv_heads, cache->head_dim, cache->dtype == DLAYER_CACHE_E4M3,
+                                                   (int64_t)cache->max_pages * cache->page_size), of_rows = (uint64_t)cache->batch * sizeof(int64_t);
+  REQUIRE(!overlap(workspace, of_ws, q, of_q) && !overlap(workspace, of_ws, o, of_q) && !overlap(workspace, of_ws, lse, of_lse) && !over_cache(cache, workspace, of_ws) &&
+              !overlap(workspace, of_ws, start, of_rows) && !overlap(workspace, of_ws, lengths, of_rows),
+          "paged_attention_forward: workspace must not overlap q, start, lengths, o, lse or the cache");
   TRY(check_device());
   return launch_paged_attention(cache_call(cache, start, lengths), q, seq, n_q_heads, scale, o, lse, workspace, (hipStream_t)stream);
 }
@@ -859,6 +864,10 @@ int token_logprobs_forward(const void* logits, const int64_t* targets, int64_t T
   for (const auto& x : out)
     REQUIRE(!overlap(x.p, x.bytes, logits, (uint64_t)T * ld * 2) && !overlap(x.p, x.bytes, targets, (uint64_t)T * 8),
             "token_logprobs_forward: results must not overlap logits or targets");
+  const uint64_t of_ws = token_logprobs_workspace(T, V, n_top);
+  REQUIRE(!overlap(workspace, of_ws, logits, (uint64_t)T * ld * 2) && !overlap(workspace, of_ws, targets, (uint64_t)T * 8),
+          "token_logprobs_forward: workspace must not overlap logits or targets");
+  for (const auto& x : out) REQUIRE(!overlap(workspace, of_ws, x.p, x.bytes), "token_logprobs_forward: workspace must not overlap the results");
   TRY(check_device());
   return launch_token_logprobs_fwd(LogprobsCall{logits, targets, T, V, ld, inverse_temperature}, (int)n_top, logprobs, entropy, lse, top_ids, top_logprobs,
                                    workspace, (hipStream_t)stream);

@@ -185,3 +185,18 @@ def test_handles_of_tensors_that_do_not_fit(K):
             K.KVCache.of(*args)
     with pytest.raises(K.DLayerError, match="GPU"):
         K.KVCache.of(k, k, table)
+
+
+def test_workspaces_in_common(K):
+    """A workspace that lies over what the call reads or writes, at either end."""
+    c, of_q, of_rows = cache(K), B * S * HQ * DH * 2, B * 8
+    bytes_ = K.paged_attention_workspace_bytes(c, S, HQ)
+    for at, size in ((A[0], of_q), (A[1], of_q), (A[3], B * S * HQ * 4), (A[4], of_rows), (A[5], of_rows), (1 << 32, PAGES * HKV * PAGE * DH), (2 << 32, PAGES * HKV * PAGE * DH),
+                     (3 << 32, PAGES * HKV * PAGE), (4 << 32, PAGES * HKV * PAGE), (5 << 32, B * COLUMNS * 4)):
+        for ws in (at - bytes_ // 16 * 16 + 16, (at + size - 1) // 16 * 16):
+            assert "workspace" in refused(K, "paged_attention_forward", C.byref(c), A[0], A[4], A[5], S, HQ, 0.1, A[1], A[3], ws, None), (hex(at), hex(ws))
+    T, V, ld, n = 5, 10001, 10008, 4
+    bytes_ = K.token_logprobs_workspace_bytes(T, V, n)
+    for at, size in ((A[0], T * ld * 2), (A[1], T * 8), (A[2], T * 4), (A[3], T * 4), (A[4], T * 4), (A[5], T * n * 8), (A[6], T * n * 4)):
+        for ws in (at - bytes_ // 16 * 16 + 16, (at + size - 1) // 16 * 16):
+            assert "workspace" in refused(K, "token_logprobs_forward", A[0], A[1], T, V, ld, 1.0, n, *A[2:7], ws, None), (hex(at), hex(ws))
