@@ -431,7 +431,7 @@ int paged_attention_forward(const dlayer_kv_cache* cache, const void* q, const i
  * most V) likeliest tokens, likeliest first, of equal logits the lower index first.  Any output may be NULL; top_ids and top_logprobs are where n_top is 0.
  * Sums in fp32.  Logits of -infinity have probability 0; a row of nothing else has lse and logprobs of -infinity and entropy 0.  A row
  * that holds NaN or +infinity has NaN for results; NaN are not among its top_ids (which end in -1 where others are too few).  Results and workspace
- * must not overlap logits or targets, nor workspace the results.  0 < inverse_temperature < 1e30.
+ * must not overlap logits, targets or each other.  0 < inverse_temperature < 1e30.
  * T below 2^22, V and ld below 2^24 (and T * ld of the gradient below 2^37).  workspace: token_logprobs_workspace_bytes(T, V, n_top), at most
  * 528 KiB; it does not fall as T, V or n_top grows. */
 size_t token_logprobs_workspace_bytes(int64_t T, int64_t V, int64_t n_top);

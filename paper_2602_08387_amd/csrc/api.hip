@@ -864,6 +864,8 @@ int token_logprobs_forward(const void* logits, const int64_t* targets, int64_t T
   for (const auto& x : out)
     REQUIRE(!overlap(x.p, x.bytes, logits, (uint64_t)T * ld * 2) && !overlap(x.p, x.bytes, targets, (uint64_t)T * 8),
             "token_logprobs_forward: results must not overlap logits or targets");
+  for (const auto& x : out)
+    for (const auto& y : out) REQUIRE(&x == &y || !overlap(x.p, x.bytes, y.p, y.bytes), "token_logprobs_forward: results must not overlap each other");
   const uint64_t of_ws = token_logprobs_workspace(T, V, n_top);
   REQUIRE(!overlap(workspace, of_ws, logits, (uint64_t)T * ld * 2) && !overlap(workspace, of_ws, targets, (uint64_t)T * 8),
           "token_logprobs_forward: workspace must not overlap logits or targets");

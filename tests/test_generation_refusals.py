@@ -200,3 +200,16 @@ def test_workspaces_in_common(K):
     for at, size in ((A[0], T * ld * 2), (A[1], T * 8), (A[2], T * 4), (A[3], T * 4), (A[4], T * 4), (A[5], T * n * 8), (A[6], T * n * 4)):
         for ws in (at - bytes_ // 16 * 16 + 16, (at + size - 1) // 16 * 16):
             assert "workspace" in refused(K, "token_logprobs_forward", A[0], A[1], T, V, ld, 1.0, n, *A[2:7], ws, None), (hex(at), hex(ws))
+
+
+def test_results_in_common(K):
+    """Any two of the log-probabilities' results, the second at either end of the first."""
+    T, V, ld, n = 5, 1001, 1008, 4
+    sizes = [T * 4, T * 4, T * 4, T * n * 8, T * n * 4]
+    for i in range(5):
+        for j in range(5):
+            for at in (A[2 + i], A[2 + i] + sizes[i] - 4, A[2 + i] - sizes[j] + 4):
+                out = list(A[2:7])
+                out[j] = at
+                if i != j:
+                    assert "overlap" in refused(K, "token_logprobs_forward", A[0], A[1], T, V, ld, 1.0, n, *out, A[7], None), (i, j)
