@@ -398,13 +398,13 @@ typedef struct dlayer_kv_cache {
  * q [B*S, Hq, dh] bf16 beside them, into q_out (may be q; padding is written as 0); q and q_out may both be NULL (n_q_heads is then
  * ignored).  rope_base 0: no rotation (of keys rotated before, as by qk_norm_rope_forward), q and q_out NULL.
  * Rounded once, from fp32, into the cache's type.  No two rows of the batch may write to one page, nor a row to a page that its table names
- * twice; k, v, q and q_out must not overlap the cache, nor q_out k or v.                                     */
+ * twice; k, v, q and q_out must not overlap the cache, nor q_out k or v, nor start or lengths the cache or q_out.   */
 int kv_cache_append(const dlayer_kv_cache* cache, const void* q, const void* k, const void* v, const int64_t* start,
                     const int64_t* lengths, int64_t seq, int64_t n_q_heads, float rope_base, int32_t rope_layout, void* q_out,
                     void* stream);
 
 /* Keys and values of positions start[b] .. start[b] + lengths[b] - 1 back from the cache: k, v [B*S, Hkv, dh] bf16, the values that are held; 0 for
- * padding and where the cache holds nothing.                                                                 */
+ * padding and where the cache holds nothing.  k and v must not overlap the cache, start, lengths or each other.                           */
 int kv_cache_read(const dlayer_kv_cache* cache, const int64_t* start, const int64_t* lengths, int64_t seq, void* k, void* v,
                   void* stream);
 
@@ -415,7 +415,7 @@ int kv_cache_read(const dlayer_kv_cache* cache, const int64_t* start, const int6
  * q, o [B*S, Hq, dh] bf16, lse [B, Hq, S] f32 or NULL.  A token that sees nothing, and padding, have o = 0 and lse = -infinity.
  * 0 < scale < 1e30; scores (scale q . k) below -5e29 count as none.  A key or value that is not finite shows in the results of those tokens that
  * see it, and of no others.  Weights are rounded to bf16 for their product with the values, sums are fp32 and divided at the end: values beyond
- * some 1e33 may overflow in them.  o, lse and workspace must not overlap q, the cache or each other, nor workspace start or lengths.
+ * some 1e33 may overflow in them.  o, lse and workspace must not overlap q, start, lengths, the cache or each other.
  * workspace: paged_attention_workspace_bytes(cache, seq, n_q_heads), which reads the sizes of cache only and does not fall as batch, seq
  * or max_pages grows.                                                                                        */
 size_t paged_attention_workspace_bytes(const dlayer_kv_cache* cache, int64_t seq, int64_t n_q_heads);

@@ -735,6 +735,12 @@ int linear_attention_step(const void* q, const void* k, const void* v, const flo
                                       (hipStream_t)stream);
 }
 
+// Bytes of k_scale (or v_scale), one a vector, and of k (or v).
+struct CacheBytes { uint64_t vectors, held; };
+static CacheBytes cache_bytes(const dlayer_kv_cache* c) {
+  const uint64_t vectors = (uint64_t)c->n_pages * c->n_kv_heads * c->page_size;
+  return {vectors, vectors * c->head_dim * (c->dtype == DLAYER_CACHE_E4M3 ? 1 : 2)};
+}
 // The cache's sizes; and, where its memory is used, its pointers.
 static int cache_ok(const char* who, const dlayer_kv_cache* c, int64_t seq, bool memory) {
   REQUIRE(c != nullptr, "%s: cache is null", who);
@@ -749,7 +755,7 @@ static int cache_ok(const char* who, const dlayer_kv_cache* c, int64_t seq, bool
   if (!memory) return 0;
   REQUIRE(c->k && c->v && aligned16(c->k) && aligned16(c->v), "%s: the cache's k or v is null or not 16-byte aligned", who);
   REQUIRE(c->page_table != nullptr, "%s: page_table is null", who);
-  const uint64_t vectors = (uint64_t)c->n_pages * c->n_kv_heads * c->page_size, held = vectors * c->head_dim * (c->dtype == DLAYER_CACHE_E4M3 ? 1 : 2);
+  const auto [vectors, held] = cache_bytes(c);
   REQUIRE(!overlap(c->k, held, c->v, held), "%s: the cache's k and v overlap", who);
   if (c->dtype == DLAYER_CACHE_E4M3)
     REQUIRE(c->k_scale && c->v_scale && aligned16(c->k_scale) && aligned16(c->v_scale), "%s: an e4m3 cache needs k_scale and v_scale, 16-byte aligned", who);
@@ -769,9 +775,14 @@ static CacheCall cache_call(const dlayer_kv_cache* c, const int64_t* start, cons
                    c->dtype == DLAYER_CACHE_E4M3, start, lengths};
 }
 static bool over_cache(const dlayer_kv_cache* c, const void* p, uint64_t bytes) {
-  const uint64_t vectors = (uint64_t)c->n_pages * c->n_kv_heads * c->page_size, held = vectors * c->head_dim * (c->dtype == DLAYER_CACHE_E4M3 ? 1 : 2);
+  const auto [vectors, held] = cache_bytes(c);
   return overlap(p, bytes, c->k, held) || overlap(p, bytes, c->v, held) || overlap(p, bytes, c->k_scale, vectors) || overlap(p, bytes, c->v_scale, vectors) ||
          overlap(p, bytes, c->page_table, (uint64_t)c->batch * c->max_pages * sizeof(int32_t));
+}
+// Whether `bytes` from p, which a call writes, lie over the rows' places that all of its workgroups read.
+static bool over_rows(const dlayer_kv_cache* c, const int64_t* start, const int64_t* lengths, const void* p, uint64_t bytes) {
+  const uint64_t rows = (uint64_t)c->batch * sizeof(int64_t);
+  return overlap(p, bytes, start, rows) || overlap(p, bytes, lengths, rows);
 }
 
 int kv_cache_append(const dlayer_kv_cache* cache, const void* q, const void* k, const void* v, const int64_t* start, const int64_t* lengths, int64_t seq,
@@ -783,6 +794,10 @@ int kv_cache_append(const dlayer_kv_cache* cache, const void* q, const void* k, 
   REQUIRE(rope_layout == 0 || rope_layout == 1, "kv_cache_append: rope_layout must be 0 or 1");
   const uint64_t of_kv = heads_bytes(cache->batch, seq, cache->n_kv_heads, cache->head_dim);
   REQUIRE(!over_cache(cache, k, of_kv) && !over_cache(cache, v, of_kv), "kv_cache_append: k and v must not overlap the cache");
+  const auto [vectors, held] = cache_bytes(cache);
+  for (const void* x : {cache->k, cache->v}) REQUIRE(!over_rows(cache, start, lengths, x, held), "kv_cache_append: start and lengths must not overlap the cache");
+  for (const void* x : {cache->k_scale, cache->v_scale})
+    REQUIRE(!over_rows(cache, start, lengths, x, vectors), "kv_cache_append: start and lengths must not overlap the cache");
   if (q) {
     REQUIRE(rope_base > 0.f, "kv_cache_append: q is given to be rotated, but rope_base is 0");
     REQUIRE(n_q_heads > 0 && n_q_heads < 65536, "kv_cache_append: n_q_heads must be positive and below 65536");
@@ -791,6 +806,7 @@ int kv_cache_append(const dlayer_kv_cache* cache, const void* q, const void* k, 
     REQUIRE(!shifted(q_out, q, of_q), "kv_cache_append: q_out must be q or not overlap it");
     REQUIRE(!overlap(q_out, of_q, k, of_kv) && !overlap(q_out, of_q, v, of_kv) && !over_cache(cache, q_out, of_q) && !over_cache(cache, q, of_q),
             "kv_cache_append: q and q_out must not overlap the cache, nor q_out k or v");
+    REQUIRE(!over_rows(cache, start, lengths, q_out, of_q), "kv_cache_append: q_out must not overlap start or lengths");
   }
   TRY(check_device());
   return launch_kv_cache_append(cache_call(cache, start, lengths), q, k, v, seq, n_q_heads, rope_base, rope_layout, q_out, (hipStream_t)stream);
@@ -801,6 +817,7 @@ int kv_cache_read(const dlayer_kv_cache* cache, const int64_t* start, const int6
   REQUIRE_PTR(k); REQUIRE_PTR(v);
   const uint64_t of_kv = heads_bytes(cache->batch, seq, cache->n_kv_heads, cache->head_dim);
   REQUIRE(!over_cache(cache, k, of_kv) && !over_cache(cache, v, of_kv) && !overlap(k, of_kv, v, of_kv), "kv_cache_read: k and v must not overlap the cache or each other");
+  REQUIRE(!over_rows(cache, start, lengths, k, of_kv) && !over_rows(cache, start, lengths, v, of_kv), "kv_cache_read: k and v must not overlap start or lengths");
   TRY(check_device());
   return launch_kv_cache_read(cache_call(cache, start, lengths), seq, k, v, (hipStream_t)stream);
 }
@@ -831,10 +848,12 @@ int paged_attention_forward(const dlayer_kv_cache* cache, const void* q, const i
   const uint64_t of_lse = (uint64_t)cache->batch * seq * n_q_heads * sizeof(float);
   REQUIRE(!overlap(lse, of_lse, q, of_q) && !overlap(lse, of_lse, o, of_q) && !over_cache(cache, lse, of_lse),
           "paged_attention_forward: lse must not overlap q, o or the cache");
+  REQUIRE(!over_rows(cache, start, lengths, o, of_q) && !over_rows(cache, start, lengths, lse, of_lse),
+          "paged_attention_forward: o and lse must not overlap start or lengths");
   const uint64_t of_ws = paged_attention_workspace(cache->batch, seq, n_q_heads, cache->n_kv_heads, cache->head_dim, cache->dtype == DLAYER_CACHE_E4M3,
-                                                   (int64_t)cache->max_pages * cache->page_size), of_rows = (uint64_t)cache->batch * sizeof(int64_t);
+                                                   (int64_t)cache->max_pages * cache->page_size);
   REQUIRE(!overlap(workspace, of_ws, q, of_q) && !overlap(workspace, of_ws, o, of_q) && !overlap(workspace, of_ws, lse, of_lse) && !over_cache(cache, workspace, of_ws) &&
-              !overlap(workspace, of_ws, start, of_rows) && !overlap(workspace, of_ws, lengths, of_rows),
+              !over_rows(cache, start, lengths, workspace, of_ws),
           "paged_attention_forward: workspace must not overlap q, start, lengths, o, lse or the cache");
   TRY(check_device());
   return launch_paged_attention(cache_call(cache, start, lengths), q, seq, n_q_heads, scale, o, lse, workspace, (hipStream_t)stream);

@@ -213,3 +213,21 @@ def test_results_in_common(K):
                 out[j] = at
                 if i != j:
                     assert "overlap" in refused(K, "token_logprobs_forward", A[0], A[1], T, V, ld, 1.0, n, *out, A[7], None), (i, j)
+
+
+def test_rows_places_in_common(K):
+    """start and lengths under what a call writes."""
+    c, of_q, of_kv, rows = C.byref(cache(K)), B * S * HQ * DH * 2, B * S * HKV * DH * 2, B * 8
+    held, scales = PAGES * HKV * PAGE * DH, PAGES * HKV * PAGE
+    for at, size in ((A[3], of_q), (1 << 32, held), (2 << 32, held), (3 << 32, scales), (4 << 32, scales)):
+        for x in (at - rows + 8, at + size - 8):
+            for places in ((x, None), (None, x)):
+                assert "overlap" in refused(K, "kv_cache_append", c, A[0], A[1], A[2], *places, S, HQ, 1e4, 0, A[3], None), hex(x)
+    for at, size in ((A[0], of_kv), (A[1], of_kv)):
+        for x in (at - rows + 8, at + size - 8):
+            for places in ((x, None), (None, x)):
+                assert "overlap" in refused(K, "kv_cache_read", c, *places, S, A[0], A[1], None), hex(x)
+    for at, size in ((A[1], of_q), (A[3], B * S * HQ * 4)):
+        for x in (at - rows + 8, at + size - 8):
+            for places in ((x, None), (None, x)):
+                assert "overlap" in refused(K, "paged_attention_forward", c, A[0], *places, S, HQ, 0.1, A[1], A[3], A[2], None), hex(x)
