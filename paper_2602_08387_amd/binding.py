@@ -173,6 +173,26 @@ def _p(t):
     return t.data_ptr()
 
 
+def _typed(kind):
+    """_p for arguments whose elements the library reads or writes as `kind`: it would go past the end of a tensor of a narrower type."""
+    want = None
+
+    def pointer(t, name):
+        nonlocal want
+        if t is None:
+            return None
+        if t.dtype is not want:
+            import torch
+            want = getattr(torch, kind)
+            if t.dtype is not want:
+                raise DLayerError(f"{name} must be {kind}, not {t.dtype}")
+        return _p(t)
+    return pointer
+
+
+_i64, _f32, _bf16 = _typed("int64"), _typed("float32"), _typed("bfloat16")
+
+
 _current_stream = None
 
 
@@ -380,12 +400,13 @@ def linear_attention_step(q, k, v, log_decay, lengths, state, batch, n_q_heads, 
 
 
 def kv_cache_append(cache, q, k, v, start, lengths, seq, n_q_heads, rope_base, rope_layout, q_out, stream=None):
-    _check(lib.kv_cache_append(C.byref(cache), _p(q), _p(k), _p(v), _p(start), _p(lengths), seq, n_q_heads, rope_base, rope_layout, _p(q_out),
-                               _stream(stream)), "kv_cache_append")
+    _check(lib.kv_cache_append(C.byref(cache), _bf16(q, "q"), _bf16(k, "k"), _bf16(v, "v"), _i64(start, "start"), _i64(lengths, "lengths"), seq,
+                               n_q_heads, rope_base, rope_layout, _bf16(q_out, "q_out"), _stream(stream)), "kv_cache_append")
 
 
 def kv_cache_read(cache, start, lengths, seq, k, v, stream=None):
-    _check(lib.kv_cache_read(C.byref(cache), _p(start), _p(lengths), seq, _p(k), _p(v), _stream(stream)), "kv_cache_read")
+    _check(lib.kv_cache_read(C.byref(cache), _i64(start, "start"), _i64(lengths, "lengths"), seq, _bf16(k, "k"), _bf16(v, "v"), _stream(stream)),
+           "kv_cache_read")
 
 
 def paged_attention_workspace_bytes(cache, seq, n_q_heads) -> int:
@@ -393,8 +414,8 @@ def paged_attention_workspace_bytes(cache, seq, n_q_heads) -> int:
 
 
 def paged_attention_forward(cache, q, start, lengths, seq, n_q_heads, scale, o, lse, workspace, stream=None):
-    _check(lib.paged_attention_forward(C.byref(cache), _p(q), _p(start), _p(lengths), seq, n_q_heads, scale, _p(o), _p(lse), _p(workspace),
-                                       _stream(stream)), "paged_attention_forward")
+    _check(lib.paged_attention_forward(C.byref(cache), _bf16(q, "q"), _i64(start, "start"), _i64(lengths, "lengths"), seq, n_q_heads, scale,
+                                       _bf16(o, "o"), _f32(lse, "lse"), _p(workspace), _stream(stream)), "paged_attention_forward")
 
 
 def token_logprobs_workspace_bytes(T, V, n_top=0) -> int:
@@ -403,13 +424,15 @@ def token_logprobs_workspace_bytes(T, V, n_top=0) -> int:
 
 def token_logprobs_forward(logits, targets, T, V, ld, inverse_temperature, n_top, logprobs, entropy, lse, top_ids, top_logprobs, workspace,
                            stream=None):
-    _check(lib.token_logprobs_forward(_p(logits), _p(targets), T, V, ld, inverse_temperature, n_top, _p(logprobs), _p(entropy), _p(lse),
-                                      _p(top_ids), _p(top_logprobs), _p(workspace), _stream(stream)), "token_logprobs_forward")
+    _check(lib.token_logprobs_forward(_bf16(logits, "logits"), _i64(targets, "targets"), T, V, ld, inverse_temperature, n_top,
+                                      _f32(logprobs, "logprobs"), _f32(entropy, "entropy"), _f32(lse, "lse"), _i64(top_ids, "top_ids"),
+                                      _f32(top_logprobs, "top_logprobs"), _p(workspace), _stream(stream)), "token_logprobs_forward")
 
 
 def token_logprobs_backward(logits, targets, lse, entropy, d_logprobs, d_entropy, T, V, ld, inverse_temperature, dlogits, stream=None):
-    _check(lib.token_logprobs_backward(_p(logits), _p(targets), _p(lse), _p(entropy), _p(d_logprobs), _p(d_entropy), T, V, ld,
-                                       inverse_temperature, _p(dlogits), _stream(stream)), "token_logprobs_backward")
+    _check(lib.token_logprobs_backward(_bf16(logits, "logits"), _i64(targets, "targets"), _f32(lse, "lse"), _f32(entropy, "entropy"),
+                                       _f32(d_logprobs, "d_logprobs"), _f32(d_entropy, "d_entropy"), T, V, ld, inverse_temperature,
+                                       _bf16(dlogits, "dlogits"), _stream(stream)), "token_logprobs_backward")
 
 
 def swiglu_forward(g, u, n, a, stream=None):

@@ -231,3 +231,26 @@ def test_rows_places_in_common(K):
         for x in (at - rows + 8, at + size - 8):
             for places in ((x, None), (None, x)):
                 assert "overlap" in refused(K, "paged_attention_forward", c, A[0], *places, S, HQ, 0.1, A[1], A[3], A[2], None), hex(x)
+
+
+def test_tensors_of_other_types(K):
+    """A tensor of a narrower type than the call reads or writes ends before the call does: each tensor in turn, before any address is looked at."""
+    import torch
+    i64, f32, bf16 = (torch.empty(8, dtype=t) for t in (torch.int64, torch.float32, torch.bfloat16))
+    c = cache(K)
+    calls = ((K.kv_cache_append, (c, bf16, bf16, bf16, i64, i64, S, HQ, 1e4, 0, bf16), ("q", "k", "v", "start", "lengths", "q_out")),
+             (K.kv_cache_read, (c, i64, i64, S, bf16, bf16), ("start", "lengths", "k", "v")),
+             (K.paged_attention_forward, (c, bf16, i64, i64, S, HQ, 0.1, bf16, f32, bf16), ("q", "start", "lengths", "o", "lse")),
+             (K.token_logprobs_forward, (bf16, i64, 5, 1001, 1008, 1.0, 4, f32, f32, f32, i64, f32, bf16),
+              ("logits", "targets", "logprobs", "entropy", "lse", "top_ids", "top_logprobs")),
+             (K.token_logprobs_backward, (bf16, i64, f32, f32, f32, f32, 5, 1001, 1008, 1.0, bf16),
+              ("logits", "targets", "lse", "entropy", "d_logprobs", "d_entropy", "dlogits")))
+    narrower = {torch.int64: torch.int32, torch.float32: torch.bfloat16, torch.bfloat16: torch.uint8}
+    for call, good, names in calls:
+        at = [i for i, x in enumerate(good) if isinstance(x, torch.Tensor)][:len(names)]
+        for i, name in zip(at, names):
+            # the others are left out, so that nothing but this one's type is to be refused
+            args = [None if j in at and j != i else x for j, x in enumerate(good)]
+            args[i] = torch.empty(8, dtype=narrower[good[i].dtype])
+            with pytest.raises(K.DLayerError, match=f"^{name} must be"):
+                call(*args)
