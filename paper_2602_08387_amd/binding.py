@@ -181,11 +181,12 @@ def _typed(kind):
         nonlocal want
         if t is None:
             return None
+        if t.dtype is want and t.is_cuda and t.is_contiguous():      # no call more than need be: a small append takes no longer than its call does
+            return t.data_ptr()
+        import torch
+        want = getattr(torch, kind)
         if t.dtype is not want:
-            import torch
-            want = getattr(torch, kind)
-            if t.dtype is not want:
-                raise DLayerError(f"{name} must be {kind}, not {t.dtype}")
+            raise DLayerError(f"{name} must be {kind}, not {t.dtype}")
         return _p(t)
     return pointer
 
