@@ -350,3 +350,42 @@ def test_many_values_that_are_not_finite(K, s, group, e4m3):
         assert np.array_equal(o[:, h][untouched], clean[:, h][untouched])
         rows = ~by_k[:, 0]
         assert torch.equal(lse[0, h].cpu()[rows], clean_lse[0, h].cpu()[rows])
+
+
+# tokens, heads of a group, KV heads, head_dim, e4m3: one, few and many rows of a KV head, and eight waves to a workgroup
+BAD_KEYS = [(1, 4, 2, 64, True), (1, 4, 2, 128, False), (6, 4, 2, 64, True), (20, 1, 2, 32, True), (30, 3, 2, 64, True), (70, 4, 2, 128, True), (150, 1, 2, 64, False), (130, 8, 64, 128, True)]
+
+
+@pytest.mark.parametrize("longest", [50, 1500])
+@pytest.mark.parametrize("case", BAD_KEYS, ids=str)
+def test_a_key_that_is_nan_leaves_no_result_where_it_is_seen(K, case, longest):
+    """NaN in one element of a key, before the call's tokens or among them: every token that sees the key has NaN for its whole result and its statistic, every
+    other token, and every other KV head, what the oracle has."""
+    s, group, hkv, dh, e4m3 = case
+    rng = np.random.default_rng(s + longest)
+    start, hq = longest, group * hkv
+    if hkv > 2:
+        start = 40                                        # the oracle's time
+    pages = Pages(rng, [start + s], hkv, dh, 16, e4m3)
+    bad = [(0, start + s // 2), (1, start // 3)]          # KV head, position
+    for j, p in bad:
+        pages.codes[0][pages.table[0, p // 16], j, p % 16, int(rng.integers(dh))] = 0xFF if e4m3 else 0x7FC1
+    qb = bits(rng, (1, s, hq, dh), 2.0)
+    o, lse = run(K, pages.device(K), dev_bf16(qb), [start], None, hq, dh ** -0.5)
+    o, lse = host_f64(o), host_f64(lse)
+    p = start + np.arange(s)
+    for j, at in bad:
+        sees = p >= at
+        heads = slice(j * group, (j + 1) * group)
+        assert np.isnan(o[0, sees][:, heads]).all() and np.isnan(lse[0, heads][:, sees]).all() and sees.any()
+        o[0][np.ix_(sees, range(j * group, (j + 1) * group))] = 0
+        lse[0][np.ix_(range(j * group, (j + 1) * group), sees)] = 0
+    cache, q = pages.oracle(), si.bf16_bits_to_f64(qb)
+    for h in range(0, hq, max(1, hq // 8)):
+        j = h // group
+        one = {"k": cache["k"][:, j:j + 1], "v": cache["v"][:, j:j + 1], "page_table": cache["page_table"]}
+        ref = og.attention(one, q[:, :, h:h + 1], [start], None, dh ** -0.5)
+        nan = np.isnan(ref[1])
+        assert np.array_equal(np.isnan(ref[0]).all(-1)[0, :, 0], nan[0, 0]) and (not nan.any() or j < 2)
+        ref = [np.where(np.isnan(x), 0.0, x) for x in ref]
+        check(torch.from_numpy(o[:, :, h:h + 1]), torch.from_numpy(lse[:, h:h + 1]), ref, dh)
