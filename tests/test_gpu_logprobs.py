@@ -309,3 +309,46 @@ def test_nan_of_every_kind_hide_no_token(K, T, V, n_top):
     assert np.array_equal(got[3][0].cpu().numpy(), np.argsort(-z[0], kind="stable")[:n_top])
     if T > 1:
         assert all(x[1:].isfinite().all() for x in got[:3])
+
+
+@pytest.mark.parametrize("V", [40, 517, 2048, 33000])
+@pytest.mark.parametrize("which", ["both", "logprobs", "entropy"])
+def test_gradient_of_rows_of_every_kind_element_by_element(K, V, which):
+    """The bound of the gradient in its terms' magnitudes, which are those of p: the tails of a row are held to theirs, and not to the row's largest."""
+    rng = np.random.default_rng(V)
+    ld = -(-V // 8) * 8
+    padded = np.full((16, ld), 0x7F80, np.uint16)         # +infinity behind the vocabulary
+    padded[:, :V] = b = rows_of_every_kind(V, rng)
+    z, logits = si.bf16_bits_to_f64(b), dev_bf16(padded)
+    targets = rng.integers(0, V, 16)
+    targets[4], targets[9], targets[12] = V - 1, 3, int(np.argmin(z[12]))
+    t = torch.from_numpy(targets).cuda()
+    dl = rng.standard_normal(16).astype(np.float32) if which != "entropy" else None
+    dh = rng.standard_normal(16).astype(np.float32) if which != "logprobs" else None
+    _, h, lse, *_ = forward(K, logits, t, V)
+    dev = lambda a: None if a is None else torch.from_numpy(a).cuda()  # noqa: E731
+    d = garbage((16, ld))
+    K.token_logprobs_backward(logits, t, lse, h if dh is not None else None, dev(dl), dev(dh), 16, V, ld, 1.0, d)
+    got = host_f64(d)
+    assert np.all(got[:, V:] == 0)
+    got = got[:, :V]
+    ref = og.logprobs_gradient(z, targets, 1.0, dl, dh)
+    r = og.logprobs(z, targets, 1.0, 0)
+    left = ~(r[2] <= -1e30)                               # rows of which the mask has left something
+    assert left.sum() == 14 and np.all(got[~left] == 0)
+    got, ref, z, at = got[left], ref[left], z[left], targets[left]
+    lse64, entropy = r[2][left][:, None], r[1][left][:, None]
+    p = np.exp(z - lse64)
+    logp = np.where(p > 0, z - lse64, 0.0)
+    size = np.where(p > 0, np.abs(z), 0.0) + np.abs(lse64)
+    terms = np.zeros_like(p)
+    if dl is not None:
+        terms += p * np.abs(dl[left])[:, None]
+        terms[np.arange(len(at)), at] += np.abs(dl[left])
+    if dh is not None:
+        terms += p * np.abs(dh[left])[:, None] * (np.abs(logp) + entropy)
+    # 1e-37: what fp32's exponential leaves of p below its smallest normal number, 2^-126.  The entropy is without the p |log p| of such tokens, each at most
+    # 2^-126 * 126 ln 2 (p |log p| falls with p), of which a row has up to V: in the row that is all but certain they are all of it (2.4e-33 of V 33000)
+    lost = V * 2.0 ** -126 * 126 * np.log(2) * p * (np.abs(dh[left])[:, None] if dh is not None else 0)
+    bound = 2.0 ** -8 * np.abs(ref) + 4e-6 * (1 + size) * terms + 1e-37 * (1 + size) + lost
+    assert np.all(np.abs(got - ref) <= 1.001 * bound), np.max(np.abs(got - ref) / bound)
