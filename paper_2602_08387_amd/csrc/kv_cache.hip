@@ -5,7 +5,7 @@
 //   read     2^e times what is held, in bf16: exact
 //
 // Both move bytes and little else: two prompts of 8192 tokens (32 and 8 heads of 128, rotated) into an e4m3 cache in 92 us (0.37 GB, 4.0 TB/s), into a bf16
-// one in 91 (4.4), back from e4m3 in 25 (0.10 GB, 4.0); one token in 3.7, the launch.  Two groups of vectors under way at a time take 92 us, one 94.5, four
+// one in 91 (4.4), back from e4m3 in 25 (0.10 GB, 4.0); one token in 3.6, the launch.  Two groups of vectors under way at a time take 92 us, one 94.5, four
 // 92; in one loop over all groups, whose kind decides what is read from the kernel's arguments, it was 126.  A head's vector is dh / 8 lanes of 16 bytes, so
 // a wave holds 4 to 16 vectors and the vector's largest magnitude and, for split pairs, the other member of a pair come from lane exchanges (DPP).  A wave
 // takes a token's heads (or, of few tokens, a part of them), so that its angles are evaluated once: in fp64, one pair a lane, handed on through LDS as fp32.

@@ -16,8 +16,8 @@
 //
 // Few rows are cut into parts, joined by a second kernel.
 //
-// Measured, 128256 tokens a row: 4096 rows 188 us without the likeliest (1.05 GB, 5.6 TB/s: memory), 210 with 5, 250 with 20, 294 with 64 (vector
-// instructions); one row 13.7 with 20 (two launches, 8.5 and 5.4 us: loads, exchanges and barriers one after the other).  The gradient of 4096 rows 395 us
+// Measured, 128256 tokens a row: 4096 rows 186 us without the likeliest (1.05 GB, 5.6 TB/s: memory), 216 with 5, 250 with 20, 292 with 64 (vector
+// instructions); one row 13.7 with 20 (two launches, 8.4 and 5.4 us: loads, exchanges and barriers one after the other).  The gradient of 4096 rows 395 us
 // (2.1 GB, 5.3 TB/s: memory).
 #include "common.h"
 #include "kernels.h"
@@ -181,7 +181,7 @@ struct TopList {
 
 // WAVES: of a workgroup.  One wave takes a short part alone, without waiting for others and without joining their lists (64 rows of 32000, 20 likeliest: 13.8
 // us, 16.7 with four); of longer parts, or with many likeliest to sort, four share the work and their bounds.  Registers for five waves a SIMD: for six
-// some go to memory (4096 rows of 128256, 5 likeliest 219 us, 210 with five; 64 likeliest 286 and 294).
+// some go to memory (4096 rows of 128256, 5 likeliest 4 % slower; 64 likeliest 3 % faster).
 template <bool TOP, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 5) void logprobs_kernel(const LogprobsArgs a) {
   constexpr int kLpWaves = WAVES, kLpThreads = 64 * WAVES;

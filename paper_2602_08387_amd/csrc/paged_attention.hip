@@ -14,11 +14,11 @@
 // Rows behind a tile's last key and pages that do not exist are behind the end of the buffer that a load is given, and read as zeros: what a page holds
 // behind a row's last token is never read.
 //
-// What bounds them (32 query and 8 KV heads of 128).  rows_kernel: memory, 256 rows of up to 4096 bf16 tokens in 374 us (5.8 TB/s of keys and values), one
-// row over 32768 e4m3 tokens in 20.1 (15.5 us, 4.4 TB/s, and 4.6 for joining 64 parts).  tile_kernel: two prompts of 8192 tokens in 1.00 to 1.06 ms (1040 to
-// 1100 TFLOP/s), the clock at 1.6 to 1.7 GHz by the card's power limit, the matrix units busy 59 % of the cycles (47 % with two workgroups a compute unit) and
-// the vector units, exponentials above all, 54 %.  The next tile's scores beside this tile's exponentials within a wave: 6 % fewer cycles, at a lower clock,
-// and no less time.
+// What bounds them (32 query and 8 KV heads of 128).  rows_kernel: memory, 256 rows of up to 4096 bf16 tokens in 378 us (5.7 TB/s of keys and values), one
+// row over 32768 e4m3 tokens in 20.0 (traced apart 16.2 us for the reading, 4.2 TB/s, and 4.5 for joining 64 parts).  tile_kernel: two prompts of 8192 tokens
+// in 1.00 to 1.06 ms (1040 to 1100 TFLOP/s), the clock at 1.6 to 1.7 GHz by the card's power limit, the matrix units busy 58 % of the cycles (47 % with two
+// workgroups a compute unit) and the vector units, exponentials above all, 53 %.  The next tile's scores beside this tile's exponentials within a wave: 6 %
+// fewer cycles, at a lower clock, and no less time.
 #include "attention_tile.h"
 #include "common.h"
 #include "kernels.h"
@@ -109,8 +109,8 @@ __device__ __forceinline__ void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory");
   if constexpr (LEFT == 0) __builtin_amdgcn_s_waitcnt(0x0f70);
 }
-// Until no load and no read of LDS of this wave is: in front of loads to a place that the wave has read from, where no barrier lies between.  Its reads may have been
-// issued without having been served (what uses them can be moved behind).
+// Until no load and no read of LDS of this wave is: in front of loads to a place that the wave has read from, where no barrier lies between.  Its reads may have
+// been issued without having been served (what uses them can be moved behind).
 __device__ __forceinline__ void wait_loads_and_reads() {
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
   __builtin_amdgcn_s_waitcnt(0x0070);
@@ -183,9 +183,9 @@ __device__ __forceinline__ bool any_not_finite(const bf16x8& v) {
 }
 
 // Whether the tiles of values share one place in LDS, so that three workgroups fit a compute unit (48 KB each at heads of 128): of bf16 with four waves.
-// Values are then asked for when the last tile's are done with, and waited for behind the exponentials (two prompts of 8192 tokens, 32 and 8 heads of 128:
-// 1060 us with two workgroups, 993 with three: products of some beside exponentials of others is what counts).  Over e4m3 this loses (two prompts 1079 us with
-// eight waves, 1243 so): bf16 is made of e4m3 between scores and products then, and for half as many rows.
+// Values are then asked for when the last tile's are done with, and waited for behind the exponentials (two prompts of 8192 tokens, 32 and 8 heads of 128, in
+// one run: 1060 us with two workgroups, 993 with three: products of some beside exponentials of others is what counts).  Over e4m3 this takes 15 % longer than
+// eight waves do: bf16 is made of e4m3 between scores and products then, and for half as many rows.
 template <bool E4M3, int NW>
 constexpr bool kThin = !E4M3 && NW == 4;
 template <int DH, bool E4M3, int NW>
@@ -396,6 +396,9 @@ __global__ __launch_bounds__(64 * NW, (kThin<E4M3, NW>) ? 3 : 2) void tile_kerne
           __builtin_amdgcn_s_setprio(1);
 #pragma unroll
           for (int ks = 0; ks < 4; ++ks) {
+            // a weight is rounded to bf16, as in the layer's own attention: results are off by 2.1e-3 to 2.4e-3 of their norm where their own rounding
+            // makes it 1.65e-3.  The sum of two bf16, which rows_kernel takes, brings that back and costs half of the matrix work again: two prompts of 8192 tokens
+            // 1041 -> 1480 us (e4m3 1088 -> 1480), 512 behind 8000 87 -> 118
             const bf16x8 pf = pack_slots(s[ks >> 1], (ks & 1) * 8);
 #pragma unroll
             for (int t2 = 0; t2 < DH / 32; ++t2) oacc[t2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at.value(t2, ks), pf, oacc[t2], 0, 0, 0);
@@ -844,11 +847,14 @@ __global__ __launch_bounds__(1024) void combine_kernel(const AttendArgs a, int r
 
 // Which way a call goes: rows of a workgroup (16 or 32: rows_kernel; 128 or 256: tile_kernel), tiles of a pair's rows, and parts of a tile's keys.  Up to 32
 // rows the cache's bytes are what counts and rows_kernel is as fast as they come; tile_kernel's matrix products of 32 rows a wave are for more.  Eight waves
-// a workgroup make bf16 of e4m3 once for twice the rows (two prompts of 8192 tokens, heads of 128: 1087 us, 1189 with four waves; bf16 itself 1102 and 1097),
-// where that leaves every compute unit two workgroups to take.  As many parts as fill the chip once: of rows_kernel the workgroups whose tiles the LDS holds
+// a workgroup make bf16 of e4m3 once for twice the rows (two prompts of 8192 tokens, heads of 128: 1088 us, 1211 with four waves; 5 rows of up to 1037 behind
+// up to 8009 360 and 404; bf16 itself, whose four waves share the place of their values, 1053 and 1041), where that leaves every compute unit two workgroups to
+// take.  As many parts as fill the chip once: of rows_kernel the workgroups whose tiles the LDS holds
 // (more of them, shorter, take longer: 8 rows over 16000 bf16 tokens 139 us in 4096 workgroups, 99 in 512), of tile_kernel two a compute unit (three, which
-// fit: 512 tokens behind 8000 85.6 -> 90.2 us, 8 rows of 128 behind up to 4000 77.0 -> 69.2); none shorter than kKeysLeast, and one only where there is no
-// more than twice that, which a second launch would cost more than it saves.
+// fit: 512 tokens behind 8000 85.6 -> 90.2 us, 8 rows of 128 behind up to 4000 77.0 -> 69.2), and no more than the table's tokens hold kKeysLeast; one only
+// where they hold no more than two, which a second launch would cost more than it saves.  Of a row shorter than its table rows_kernel's parts are kKeysLeast long
+// all the same, and the others have none; tile_kernel's are equal shares, however short: kKeysLeast for it too is slower (64 tokens behind 1000, a table of
+// 131072: 22.9 -> 25.5 us, behind 40: 20.7 -> 22.2), since the longest part lasts longer and joining walks over all parts either way.
 struct AttendPlan { int rows, tiles, splits, least; int64_t pairs; };
 constexpr int64_t kUnits = 256, kKeysLeast = 256;
 static int64_t most_splits(int64_t max_tokens) { return max_tokens <= 2 * kKeysLeast ? 1 : (max_tokens + kKeysLeast - 1) / kKeysLeast; }
